@@ -510,6 +510,156 @@ msi_status msi_timing_read(msi_plan* plan, double* ms, uint64_t* launches, int r
 /* Number of kernels the library launched since the plan was created. */
 uint64_t msi_kernel_launches(const msi_plan* plan);
 
+/* ---------------------------------------------------------------------------
+ * Key-value cache in 8 bits (a library convenience: the paper leaves KV state
+ * to the native runtime).  What a decode stack needs between two MoE layers:
+ * the keys and values of each sequence, held in blocks of P tokens with one
+ * scale for each block and head, the attention that reads them, and eviction
+ * by the attention weight that blocks have received.  As with slots, a block
+ * keeps its address while it is held; a sequence names its blocks by a table.
+ *
+ * The cache is one layer's; every buffer is the caller's and on the device,
+ * and all its state (lengths, tables, free blocks) lives there, so that a
+ * decode loop needs no host round trip and can be captured in a graph.  Calls
+ * are asynchronous on `stream`; calls on one cache must be ordered on the GPU
+ * (one stream, or events).  The handle itself holds no device memory and is
+ * not changed by calls; it may be used from several host threads.
+ *
+ * Values.  A block's rows are rounded once, from their 16-bit originals, with
+ * a = max(|x|, 1e-20) over the block's P x D values of one head:
+ *   MSI_KV_Q8:   byte q in 1..255 stands for scale * (q - 128),
+ *                q - 128 = round(x * (127 / a)), scale = a * fl(1/127)
+ *   MSI_KV_E4M3: byte is an e4m3 number y standing for scale * y,
+ *                y = e4m3(x * (448 / a)), scale = a * fl(1/448)
+ * in fp32, ties to even.  Rows of the last two blocks are also kept in bf16
+ * (`recent`), and a block that grows or shrinks is rounded anew from them: what
+ * the cache holds does not depend on how many rows came with each call.  A
+ * block with an infinity or a NaN gets the scale NaN: every query row that
+ * reads it is NaN, rows that see none of its tokens are not touched by it.
+ *
+ * Errors found on the GPU (lengths, sequence numbers or row offsets out of
+ * range, no free block) raise the cache's status word and fail closed: the
+ * call that finds one changes nothing else, and while the word is not 0 append,
+ * evict and release change nothing and attention writes NaN to every row.  (A
+ * table entry out of range is found block by block: its block alone is skipped,
+ * rows that would read it are NaN.)  msi_kv_status reads and clears the word.
+ * ------------------------------------------------------------------------- */
+enum { MSI_KV_Q8 = 0, MSI_KV_E4M3 = 1 };
+
+/* Limits: n_seqs <= 1024, 1 <= n_kv_heads <= 64, head_dim 64, 128 or 256,
+ * block_tokens 16, 32, 64 or 128, max_blocks * block_tokens <= 2^28,
+ * n_blocks < 2^21, at most 2^27 rows a call; other shapes return
+ * MSI_ERR_UNSUPPORTED.  Device buffers (K = n_kv_heads, P = block_tokens,
+ * D = head_dim), each 16-byte aligned: */
+typedef struct {
+  int n_seqs, max_blocks, n_blocks, n_kv_heads, head_dim, block_tokens, format;
+  void* k_codes;       /* [n_blocks, K, P, D] bytes */
+  void* v_codes;       /* the same */
+  float* k_scale;      /* [n_blocks, K] */
+  float* v_scale;      /* [n_blocks, K] */
+  void* recent;        /* bf16 [n_seqs, 2 (k, v), K, 2P, D]: the row of position p at p mod 2P */
+  int32_t* table;      /* [n_seqs, max_blocks] the sequence's blocks in order */
+  int32_t* seq_state;  /* [n_seqs, 4] tokens held; next position (tokens held and evicted);
+                          first position with a row in `recent`; 0 */
+  int32_t* free_ids;   /* [n_blocks] free blocks, taken from the end of the first control[0] */
+  int32_t* control;    /* [8] free blocks; status word; counters that are 0 between calls */
+  float* weight;       /* [n_blocks] attention weight received (see MSI_KV_OBSERVE) */
+} msi_kv_desc;
+
+typedef struct msi_kv msi_kv; /* opaque, owned by the library */
+
+/* Create a handle (validates and copies the description; touches no device
+ * memory) for the current device.  Calls with another device current return
+ * MSI_ERR_INVALID_ARG.  The buffers must outlive the handle's last call. */
+msi_status msi_kv_create(const msi_kv_desc* desc, msi_kv** out);
+msi_status msi_kv_destroy(msi_kv* kv);
+
+/* Empty the cache: no tokens, every block free (block 0 is taken first),
+ * status and weights 0. */
+msi_status msi_kv_init(msi_kv* kv, msi_stream stream);
+
+/* Append rows to n sequences.  seqs: device int32 [n] distinct sequence numbers
+ * (NULL: 0 .. n-1).  cu: device int32 [n + 1]; rows cu[b] .. cu[b+1]-1 of k and
+ * v (device bf16 [n_rows, K, D], rows row_stride elements apart, a multiple of
+ * 8; 16-byte aligned) become the tokens from start[b] on of sequence seqs[b].
+ * start: device int32 [n], NULL: at each sequence's end.  Tokens held from
+ * start[b] on are dropped first (rejected draft tokens) and blocks left empty
+ * are freed; start[b] must be a multiple of P or lie at a token whose block's
+ * earlier rows are still in `recent` (the last two blocks).  New blocks are
+ * taken from the end of free_ids, for b ascending, and their weights cleared;
+ * dropped ones are put there after that.  Device errors: MSI_ERR_NOT_RESIDENT
+ * (too few free blocks, or a table that is full), MSI_ERR_INVALID_ARG; then
+ * nothing is appended to any sequence. */
+msi_status msi_kv_append(msi_kv* kv, int n, const int32_t* seqs, const int32_t* cu,
+                         const int32_t* start, const void* k, const void* v, int64_t row_stride,
+                         int n_rows, msi_stream stream);
+
+/* Attention flags. */
+enum {
+  MSI_KV_OBSERVE = 1 /* weight[block] += the sum over its tokens, all heads and the call's query rows
+                        of the attention weights; for calls in decode form only (below) */
+};
+
+/* One attention call (host struct of device pointers and plain values). */
+typedef struct {
+  int n;                /* sequences */
+  const int32_t* seqs;  /* [n] or NULL: 0 .. n-1 */
+  const int32_t* cu;    /* [n + 1] row offsets of q */
+  int n_rows;           /* rows of q and out */
+  int max_rows;         /* most rows of one sequence */
+  int n_heads;          /* query heads, a multiple of K: head h reads key-value head h / (n_heads / K) */
+  const void* q;        /* bf16 [n_rows, n_heads, D], 16-byte aligned */
+  int64_t q_stride;     /* elements between rows, a multiple of 8 */
+  void* out;            /* bf16 [n_rows, n_heads, D], 16-byte aligned */
+  int64_t out_stride;
+  float* lse;           /* [n_rows, n_heads] natural log of the sum of exp(score), or NULL */
+  float scale;          /* score = scale * q . k, finite and > 0 */
+  float softcap;        /* > 0: score = softcap * tanh(score / softcap); 0: none */
+  int window;           /* > 0: a row sees at most this many tokens, its own among them; 0: all */
+  unsigned flags;
+} msi_kv_attention_args;
+
+/* Device workspace of one call (256-byte aligned, not shared by calls that may
+ * overlap).  *decode_form (may be NULL) receives 1 where the call runs in decode
+ * form: max_rows * n_heads / K at most 32, and at most 16 for D = 256. */
+msi_status msi_kv_workspace_size(const msi_kv* kv, const msi_kv_attention_args* args, size_t* bytes,
+                                 int* decode_form);
+
+/* Attention of the last rows of each sequence over what it holds: with L tokens
+ * held and r = cu[b+1] - cu[b] rows, row i stands at token L - r + i and sees
+ * the tokens up to it (append first, then attend).  A row that sees no token
+ * gives 0 and lse -inf.  Scores, sums and statistics are fp32; the attention
+ * weights are rounded to fp16 before they multiply the values.  MSI_KV_OBSERVE
+ * outside decode form returns MSI_ERR_UNSUPPORTED. */
+msi_status msi_kv_attention(msi_kv* kv, const msi_kv_attention_args* args, void* workspace,
+                            size_t workspace_bytes, msi_stream stream);
+
+/* Evict: each of n sequences that holds more than `keep` blocks keeps its first
+ * `sinks` blocks, its last `recent` (>= 1, the one being filled among them) and,
+ * of the others, those with the greatest weight (ties: the earlier block);
+ * sinks + recent <= keep.  Kept blocks stay where they are and in order; the
+ * others go to the end of free_ids, for b ascending in table order.  Positions
+ * are not changed: attention counts the tokens held. */
+msi_status msi_kv_evict(msi_kv* kv, int n, const int32_t* seqs, int keep, int sinks, int recent,
+                        msi_stream stream);
+
+/* End n sequences: all their blocks are freed, their positions start again at 0. */
+msi_status msi_kv_release(msi_kv* kv, int n, const int32_t* seqs, msi_stream stream);
+
+/* Read values back: rows cu[b] .. cu[b+1]-1 of k_out and v_out (bf16
+ * [n_rows, K, D], packed, 16-byte aligned) receive the tokens from first[b] on
+ * (NULL: from 0) of sequence seqs[b], as held.  Device error
+ * MSI_ERR_INVALID_ARG for tokens that are not held: their rows are NaN. */
+msi_status msi_kv_read(msi_kv* kv, int n, const int32_t* seqs, const int32_t* first,
+                       const int32_t* cu, int n_rows, void* k_out, void* v_out, msi_stream stream);
+
+/* Wait for `stream`, return the cache's status word (an msi_status value) and
+ * clear it. */
+msi_status msi_kv_status(msi_kv* kv, msi_stream stream, int* device_status);
+
+/* Number of kernels launched through the handle. */
+uint64_t msi_kv_kernel_launches(const msi_kv* kv);
+
 /* Text of a status code; text of the last CUDA error seen by the library. */
 const char* msi_status_string(msi_status s);
 const char* msi_last_cuda_error(void);

@@ -1,7 +1,7 @@
 """Convenience wrapper over the C ABI for PyTorch callers.
 
 PyTorch supplies device memory, pinned host memory and streams; every step of
-the MoE layer forward runs in libmsi.so's CUDA kernels.  This module only
+the MoE layer forward and of the key-value cache runs in libmsi.so's CUDA kernels.  This module only
 marshals tensors into pointers and checks status codes.
 """
 from __future__ import annotations
@@ -361,6 +361,167 @@ class Source:
     def close(self):
         if getattr(self, "h", None) is not None and self.h.value:
             N.check(N.lib().msi_source_close(self.h), "msi_source_close")
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KvCache:
+    """One layer's key-value cache in 8 bits (see include/msi.h, msi_kv_desc):
+    paged blocks with a scale for each block and head, append, attention over
+    them, eviction by the attention weight received.
+
+    ``buffers`` gives tensors to use in place of new ones (by the names of
+    ``BUFFERS``, shapes as in msi_kv_desc; a cache that a program restores or
+    shares): if it is given, it has to name all of them, and the cache is not
+    emptied.  Every index argument is an int32 CUDA tensor; ``seqs`` None means
+    sequences 0, 1, ...  Nothing here waits for the GPU but ``status``."""
+
+    BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "recent", "table", "seq_state", "free_ids", "control",
+               "weight")
+
+    def __init__(self, *, n_seqs, max_blocks, n_blocks, n_kv_heads, head_dim, block_tokens=32, fmt=N.MSI_KV_Q8,
+                 buffers=None, stream=None):
+        lib = N.lib()
+        K, P, D = n_kv_heads, block_tokens, head_dim
+        self.n_seqs, self.K, self.P, self.D, self.fmt = n_seqs, K, P, D, fmt
+        shapes = {"k_codes": ((n_blocks, K, P, D), torch.uint8), "v_codes": ((n_blocks, K, P, D), torch.uint8),
+                  "k_scale": ((n_blocks, K), torch.float32), "v_scale": ((n_blocks, K), torch.float32),
+                  "recent": ((n_seqs, 2, K, 2 * P, D), torch.bfloat16), "table": ((n_seqs, max_blocks), torch.int32),
+                  "seq_state": ((n_seqs, 4), torch.int32), "free_ids": ((n_blocks,), torch.int32),
+                  "control": ((8,), torch.int32), "weight": ((n_blocks,), torch.float32)}
+        for name, (shape, dtype) in shapes.items():
+            if buffers is None:
+                t = torch.empty(shape, dtype=dtype, device="cuda")
+            else:
+                t = buffers[name]
+                if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+                    raise ValueError("%s: a contiguous CUDA tensor %s of %s is needed" % (name, shape, dtype))
+            setattr(self, name, t)
+        d = N.msi_kv_desc(n_seqs, max_blocks, n_blocks, K, D, P, fmt, *[getattr(self, n).data_ptr() for n in self.BUFFERS])
+        h = ctypes.c_void_p()
+        N.check(lib.msi_kv_create(ctypes.byref(d), ctypes.byref(h)), "msi_kv_create")
+        self.h = h
+        self._ws = None
+        self._need = {}
+        if buffers is None:
+            self.init(stream)
+
+    @staticmethod
+    def _index(t, name, n=None):
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise ValueError("%s: a contiguous int32 CUDA vector%s is needed" % (name, "" if n is None else " of %d" % n))
+        return t.data_ptr()
+
+    def _rows(self, t, name, heads):
+        if (t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 3 or t.shape[1:] != (heads, self.D)
+                or (t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D)))):
+            raise ValueError("%s: bf16 CUDA rows [n, %d, %d], each contiguous, are needed" % (name, heads, self.D))
+        return t.data_ptr() if t.shape[0] else None
+
+    @staticmethod
+    def _used_on(stream, *tensors):
+        """Tensors made here on the current stream and used on another one."""
+        if stream is not None:
+            for t in tensors:
+                t.record_stream(stream)
+
+    def init(self, stream=None):
+        """Empty the cache: every block free, no tokens, status 0."""
+        N.check(N.lib().msi_kv_init(self.h, _stream(stream)), "msi_kv_init")
+
+    def append(self, k, v, cu, seqs=None, start=None, stream=None):
+        """Rows cu[b] .. cu[b+1] of k and v [n, kv_heads, head_dim] (rows may be
+        strided alike) become the tokens of sequence seqs[b] from start[b] on
+        (None: at its end); tokens held from there on are dropped first."""
+        n = cu.numel() - 1
+        kp, vp = self._rows(k, "k", self.K), self._rows(v, "v", self.K)
+        if v.shape[0] != k.shape[0] or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+            raise ValueError("k and v: as many rows, with the same stride, are needed")
+        N.check(N.lib().msi_kv_append(self.h, n, self._index(seqs, "seqs", n), self._index(cu, "cu"),
+                                      self._index(start, "start", n), kp, vp,
+                                      k.stride(0) if k.shape[0] > 1 else self.K * self.D, k.shape[0], _stream(stream)),
+                "msi_kv_append")
+
+    def attention(self, q, cu, max_rows, seqs=None, out=None, lse=None, scale=None, softcap=0.0, window=0,
+                  observe=False, stream=None):
+        """Attention of rows cu[b] .. cu[b+1] of q [n, heads, head_dim], the last
+        tokens of sequence seqs[b], over what it holds.  max_rows: at least the
+        rows of any one sequence.  scale None: head_dim ** -0.5.  observe: add up
+        each block's attention weight (decode form).  Returns (out, lse)."""
+        n, rows, heads = cu.numel() - 1, q.shape[0], q.shape[1]
+        qp = self._rows(q, "q", heads)
+        out = torch.empty((rows, heads, self.D), dtype=torch.bfloat16, device=q.device) if out is None else out
+        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if lse is None else lse
+        if out.shape != q.shape:
+            raise ValueError("out: the shape of q is needed")
+        op = self._rows(out, "out", heads)
+        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
+            raise ValueError("lse: a contiguous fp32 CUDA tensor [n, heads] is needed")
+        wide = heads * self.D
+        a = N.msi_kv_attention_args(n, self._index(seqs, "seqs", n), self._index(cu, "cu"), rows, max_rows, heads, qp,
+                                    q.stride(0) if rows > 1 else wide, op, out.stride(0) if rows > 1 else wide,
+                                    lse.data_ptr() if rows else None,
+                                    self.D ** -0.5 if scale is None else scale, softcap, window,
+                                    N.MSI_KV_OBSERVE if observe else 0)
+        key = (n, rows, max_rows, heads, observe)
+        need = self._need.get(key)
+        if need is None:  # a pure function of the cache's and the call's shape
+            b = ctypes.c_size_t()
+            N.check(N.lib().msi_kv_workspace_size(self.h, ctypes.byref(a), ctypes.byref(b), None), "msi_kv_workspace_size")
+            need = self._need[key] = b.value
+        ws = self._ws
+        if ws is None or ws.numel() < need:
+            ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+        self._used_on(stream, out, lse, ws)
+        N.check(N.lib().msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), _stream(stream)),
+                "msi_kv_attention")
+        return out, lse
+
+    def evict(self, seqs, keep, sinks=0, recent=1, stream=None):
+        """Sequences that hold more than `keep` blocks keep their first `sinks`,
+        their last `recent` and the heaviest others.  seqs: a tensor, or the
+        number of sequences 0, 1, ..."""
+        n = seqs if isinstance(seqs, int) else seqs.numel()
+        N.check(N.lib().msi_kv_evict(self.h, n, None if isinstance(seqs, int) else self._index(seqs, "seqs"), keep, sinks,
+                                     recent, _stream(stream)), "msi_kv_evict")
+
+    def release(self, seqs, stream=None):
+        """End sequences (a tensor, or the number of sequences 0, 1, ...)."""
+        n = seqs if isinstance(seqs, int) else seqs.numel()
+        N.check(N.lib().msi_kv_release(self.h, n, None if isinstance(seqs, int) else self._index(seqs, "seqs"),
+                                       _stream(stream)), "msi_kv_release")
+
+    def read(self, cu, rows, seqs=None, first=None, stream=None):
+        """The tokens from first[b] on (None: 0) of sequence seqs[b] as bf16 rows
+        cu[b] .. cu[b+1] of (k, v) [rows, kv_heads, head_dim]; rows = cu[-1]."""
+        n = cu.numel() - 1
+        kv = torch.empty((2, rows, self.K, self.D), dtype=torch.bfloat16, device="cuda")
+        k, v = kv[0], kv[1]
+        self._used_on(stream, kv)
+        N.check(N.lib().msi_kv_read(self.h, n, self._index(seqs, "seqs", n), self._index(first, "first", n),
+                                    self._index(cu, "cu"), rows, k.data_ptr() if rows else None,
+                                    v.data_ptr() if rows else None, _stream(stream)), "msi_kv_read")
+        return k, v
+
+    def status(self, stream=None) -> int:
+        """Wait for the stream; the cache's status word (MSI_OK: 0), which is cleared."""
+        s = ctypes.c_int()
+        N.check(N.lib().msi_kv_status(self.h, _stream(stream), ctypes.byref(s)), "msi_kv_status")
+        return s.value
+
+    def launches(self) -> int:
+        return int(N.lib().msi_kv_kernel_launches(self.h))
+
+    def close(self):
+        if getattr(self, "h", None) is not None and self.h.value:
+            N.check(N.lib().msi_kv_destroy(self.h), "msi_kv_destroy")
             self.h = None
 
     def __del__(self):

@@ -19,7 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmsi.so")
 SOURCES = ["plan.cu", "router.cu", "router_tc.cu", "permute.cu", "gemm.cu", "gemm_pair.cu", "gemm_fused.cu",
-           "gemm_fused_pair.cu", "gemm_cols.cu", "noalloc.cu", "source.cpp"]
+           "gemm_fused_pair.cu", "gemm_cols.cu", "noalloc.cu", "kv.cu", "kv_decode.cu", "source.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -42,6 +42,7 @@ def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
     deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "permute.cuh"),
+            os.path.join(CSRC, "kv.cuh"),
             os.path.join(CSRC, "source.h"),
             os.path.join(ROOT, "include", "msi.h")]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps)

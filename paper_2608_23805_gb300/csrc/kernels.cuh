@@ -15,6 +15,9 @@ constexpr int kScatterWarps = 4;   // scatter warps per block, one per router bl
 // The device that was current when the plan was created (plan.cu).
 int plan_device(const msi_plan* p);
 
+// Keep the text of a CUDA error for msi_last_cuda_error (plan.cu); MSI_ERR_CUDA.
+msi_status note_cuda_error(cudaError_t e, const char* what);
+
 struct RouterArgs {
   const __nv_bfloat16* x;  // [T, H]
   const float* wr;         // [E, H]

@@ -1,0 +1,165 @@
+// Key-value cache in 8 bits (include/msi.h, msi_kv_*): what its kernels share.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "kernels.cuh"
+
+namespace msi {
+
+constexpr int kKvMaxSeqs = 1024;
+constexpr int kKvMaxHeads = 64;
+constexpr float kKvTiny = 1e-20f;  // least absolute maximum of a block: its scale stays a normal number
+
+// The cache as the kernels see it (msi_kv_desc).
+struct KvCache {
+  int n_seqs, max_blocks, n_blocks, K, D, P, logP, fmt;
+  uint8_t* codes[2];
+  float* scale[2];
+  __nv_bfloat16* recent;
+  int* table;
+  int4* seq;     // {held, position, first position in `recent`, 0}
+  int* free_ids;
+  int* control;  // [0] free blocks, [1] status, [2] append ticket, [3] evict ticket
+  float* weight;
+};
+
+struct KvAppendArgs {
+  KvCache c;
+  int n, n_rows;
+  const int* seqs;
+  const int* cu;
+  const int* start;
+  const __nv_bfloat16* x[2];
+  long long stride;
+};
+
+struct KvEvictArgs {
+  KvCache c;
+  int n;
+  const int* seqs;
+  int keep, sinks, recent;
+  int release;
+};
+
+struct KvReadArgs {
+  KvCache c;
+  int n, n_rows;
+  const int* seqs;
+  const int* first;
+  const int* cu;
+  __nv_bfloat16* out[2];
+};
+
+struct KvAttnArgs {
+  KvCache c;
+  int n, n_rows, max_rows, H, G;
+  const int* seqs;
+  const int* cu;
+  const __nv_bfloat16* q;
+  long long q_stride;
+  __nv_bfloat16* out;
+  long long out_stride;
+  float* lse;
+  float scale, softcap;
+  int window, observe;
+  int ctas;            // CTAs that share the work
+  // workspace
+  float* part_o;       // [2 ctas][rows][D] unnormalised outputs of the parts of split items
+  float* part_ml;      // [2 ctas][2][rows] their reference exponents and sums
+  float* lse2;         // [n_rows, H] log2 of the sums (observe)
+  float* step_lse;     // [steps][rows] log2 of each 16-token step's sum (observe)
+  long long max_steps;
+  int* plan;           // chunk form: [items + 1] prefix of KV tiles over the items
+  int max_items;
+};
+
+cudaError_t launch_kv_append(const KvAppendArgs& a, cudaStream_t s);
+cudaError_t launch_kv_evict(const KvEvictArgs& a, cudaStream_t s);
+cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s);
+cudaError_t launch_kv_init(const KvCache& c, cudaStream_t s);
+// Decode form: rows of one sequence and key-value head (its part of the query
+// heads) in at most kv_decode_rows(D) columns of the MMA.
+int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4), 0: not in decode form
+cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s);
+
+#if defined(__CUDACC__)
+
+__device__ __forceinline__ void kv_raise(const KvCache& c, int status) { atomicCAS(c.control + 1, 0, status); }
+
+__device__ __forceinline__ float kv_nan() { return __int_as_float(0x7fc00000); }
+
+__device__ __forceinline__ int kv_seq(const int* seqs, int b) { return seqs == nullptr ? b : seqs[b]; }
+
+// Inclusive sums of `v` over the block's threads (a multiple of 32, at most
+// 1,024); `warp_sums` holds 32 ints.  Ends with the block in step.
+__device__ __forceinline__ int block_scan(int v, int* warp_sums) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[w] = v;
+  __syncthreads();
+  if (w == 0) {
+    int s = lane < nw ? warp_sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += u;
+    }
+    warp_sums[lane] = s;
+  }
+  __syncthreads();
+  return v + (w > 0 ? warp_sums[w - 1] : 0);
+}
+
+// Two e4m3 numbers (low byte first) as fp16: exact.
+__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t v) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// Codes to fp16, exactly: byte 0 and 1 (HI: 2 and 3) of z.
+//   Q8: byte q under the high byte 0x64 is the fp16 number 1024 + q; less 1152
+//   it is q - 128.
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t kv_f16x2(uint32_t z) {
+  if (FMT == MSI_KV_Q8) {
+    const uint32_t v = __byte_perm(z, 0x64646464u, HI ? 0x4342 : 0x4140);
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  return e4m3x2_f16x2(HI ? z >> 16 : z);
+}
+
+// What a query row is multiplied with to lie in fp16's range: the power of two
+// that takes its largest element to [1, 2) (bits of 2^-e; 2^e comes back into
+// the score's scale).  bf16 has 8 significant bits, fp16 11 and 14 exponents
+// below 1: products with codes stay exact but for elements under 2^-14 of the
+// row's largest, which are rounded to 2^-24 of it.  amax: bits of the row's
+// largest absolute value.
+__device__ __forceinline__ uint32_t kv_row_exp(uint32_t amax_bits) {
+  const uint32_t e = amax_bits >> 23;
+  return e < 1 ? 1 : e > 253 ? 253 : e;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// softcap * tanh(x / softcap) = softcap (1 - 2 / (e^(2 x / softcap) + 1)); the
+// quotient's limits are those of the formula.  two_log2e_cap = 2 log2(e) / cap.
+__device__ __forceinline__ float kv_softcap(float x, float cap, float two_log2e_cap) {
+  const float y = x * two_log2e_cap;
+  return cap * (1.0f - __fdividef(2.0f, ex2(y > 80.0f ? 80.0f : y) + 1.0f));  // a NaN stays one
+}
+
+#endif  // __CUDACC__
+
+}  // namespace msi

@@ -1,0 +1,686 @@
+// Attention over the 8-bit key-value cache in decode form: the rows of one
+// sequence and key-value head (its query heads times a few tokens, R <= 32)
+// against everything that the sequence holds.
+//
+// Mathematics.  With codes c and scales sk, sv of a token's block and head, a
+// row's score is s = scale * sk * (q . ck), its weight p = 2^(s log2 e - M), and
+//   out = sum p sv cv / sum p.
+// Codes are exact in fp16; q is brought to fp16's range by a power of two per
+// row (kv_row_exp), so the products are exact and the tensor core adds them up
+// in fp32.  sk multiplies the fp32 score.  sv goes into the exponent: the MMA's
+// operand is P = 2^(s log2 e + log2 sv - M) <= 2^8, rounded once to fp16 (the
+// choice that costs precision here: 2^-12 a weight, an eighth of bf16's), and
+// the sum takes P / sv in fp32.  M is a running reference, moved only when a P
+// would pass 2^8, so most steps rescale nothing.
+//
+// Layout.  A warp takes 16 tokens a step.  S^T = K Q^T and O^T = V^T P^T have
+// the tokens and the head's columns as the MMA's 16 rows and the query rows as
+// its 8 columns: with 8 rows no lane of the MMA is idle (queries as rows would
+// waste half of one).  The contraction's order is free, so a lane's operands
+// are 16 consecutive bytes of a code row, and V^T needs only byte interleaving
+// of two tokens' words.  Codes go to a ring of shared memory per warp by
+// 16-byte asynchronous copies, chunks XOR-swizzled by row.  The legacy MMA is
+// enough: 2 R flops a byte (110 TFLOP/s at 8 rows and 6.8 TB/s).
+//
+// Split.  The work is the list of all 16-token steps of all (sequence, head)
+// pairs; each CTA takes an equal run of it, whatever the lengths.  A pair that
+// lies in one CTA is finished there; parts of split ones are joined by
+// kv_join_kernel in the CTAs' order, so results do not depend on timing.
+#include "kv.cuh"
+
+namespace msi {
+namespace {
+
+constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLazy = 8.0f;  // P may reach 2^8
+
+__host__ __device__ constexpr int dec_stages(int D) { return D == 64 ? 8 : D == 128 ? 6 : 3; }
+__host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
+__host__ __device__ constexpr int dec_ring_bytes(int D) { return dec_stages(D) * dec_stage_bytes(D); }
+
+// One sequence of the call.
+struct KvWork {
+  int seq, row0, rows, held;
+  int step0, steps;  // 16-token steps that some row sees
+  bool ok;
+};
+
+__device__ __forceinline__ KvWork kv_work(const KvAttnArgs& a, int b) {
+  const KvCache& c = a.c;
+  KvWork w;
+  w.seq = kv_seq(a.seqs, b);
+  w.row0 = a.cu[b];
+  w.rows = a.cu[b + 1] - w.row0;
+  w.ok = w.seq >= 0 && w.seq < c.n_seqs && w.row0 >= 0 && w.rows >= 0 && w.rows <= a.max_rows &&
+         w.row0 <= a.n_rows - w.rows;
+  w.held = w.ok ? c.seq[w.seq].x : 0;
+  w.ok = w.ok && w.held >= 0 && w.held <= c.max_blocks << c.logP;
+  w.step0 = w.steps = 0;
+  if (!w.ok || w.rows == 0) return w;
+  const int lo = a.window > 0 ? max(0, w.held - w.rows - a.window + 1) : 0;
+  w.step0 = lo >> 4;
+  w.steps = ((w.held + 15) >> 4) - w.step0;
+  return w;
+}
+
+// The batch's steps: s_pre[b] = steps of the pairs before sequence b, over all
+// heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
+__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, long long* s_sum, int* s_bad) {
+  const int tid = threadIdx.x, T = blockDim.x, lane = tid & 31, wid = tid >> 5;
+  const int per = (a.n + T - 1) / T, b0 = min(a.n, tid * per), b1 = min(a.n, b0 + per);
+  if (tid == 0) *s_bad = 0;
+  __syncthreads();
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const KvWork w = kv_work(a, b);
+    if (!w.ok) *s_bad = 1;
+    mine += (long long)w.steps * a.c.K;
+  }
+  long long v = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  if (lane == 31) s_sum[wid] = v;
+  __syncthreads();
+  long long before = v - mine;
+  for (int i = 0; i < wid; ++i) before += s_sum[i];
+  for (int b = b0; b < b1; ++b) {
+    s_pre[b] = before;
+    before += (long long)kv_work(a, b).steps * a.c.K;
+  }
+  if (b0 < a.n && b1 == a.n) s_pre[a.n] = before;
+  __syncthreads();
+  return *s_bad == 0;
+}
+
+// CTAs that take part, and where CTA i's run of `total` steps begins.
+__device__ __forceinline__ int kv_ctas(long long total, int ctas) {
+  const long long most = (total + kDecWarps - 1) / kDecWarps;  // a step a warp at least
+  return (int)min((long long)ctas, max(most, 1LL));
+}
+__device__ __forceinline__ long long kv_begin(long long total, int ctas, int i) { return total * i / ctas; }
+// the CTA whose run holds step u
+__device__ __forceinline__ int kv_owner(long long total, int ctas, long long u) {
+  int i = (int)(u * ctas / total);
+  while (kv_begin(total, ctas, i + 1) <= u) ++i;
+  while (kv_begin(total, ctas, i) > u) --i;
+  return i;
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Byte offset of 16-byte chunk `ch` of token row r in a stage's [16][D] codes.
+template <int D>
+__device__ __forceinline__ int dec_chunk(int r, int ch) {
+  if (D == 64) return r * 64 + ((ch ^ ((r >> 1) & 3)) << 4);
+  return r * D + ((ch ^ (r & 7)) << 4);
+}
+// The chunk that lane t of a quad reads as its j-th: the contraction's order.
+template <int D>
+__device__ __forceinline__ int dec_kchunk(int t, int j) {
+  return D == 64 ? t : D == 128 ? 2 * t + j : 2 * t + (j & 1) + 8 * (j >> 1);
+}
+
+// A lane's view of the steps of a run: the block, scales of step base + lane.
+struct StepInfo {
+  int blk;
+  float ks, vs;
+};
+
+template <int D, int NT, int FMT>
+__global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a) {
+  constexpr int KS = D / 16;          // MMAs along a row, and column tiles of the output
+  constexpr int CH = D / 64;          // 16-byte chunks of a key row a lane takes
+  constexpr int R = 8 * NT;
+  constexpr int S = dec_stages(D), SB = dec_stage_bytes(D), RING = dec_ring_bytes(D);
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ long long s_sum[kDecWarps];
+  __shared__ int s_bad;
+  __shared__ float s_m[kDecWarps][R], s_l[kDecWarps][R];
+  long long* s_pre = reinterpret_cast<long long*>(smem + kDecWarps * RING);
+  const KvCache& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
+  grid_release();
+
+  const int status = c.control[1];
+  const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
+  const long long total = s_pre[a.n];
+  if (!ok || status != 0 || (a.observe && total > a.max_steps)) {
+    if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
+    // fail closed: no row of the call can be read as an answer
+    const long long vecs = (long long)a.n_rows * a.H * (D / 8);
+    for (long long i = (long long)blockIdx.x * kDecThreads + tid; i < vecs; i += (long long)gridDim.x * kDecThreads) {
+      const long long row = i / (a.H * (D / 8));
+      *reinterpret_cast<uint4*>(a.out + row * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
+          make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+    }
+    for (long long i = (long long)blockIdx.x * kDecThreads + tid; i < (long long)a.n_rows * a.H;
+         i += (long long)gridDim.x * kDecThreads)
+      if (a.lse != nullptr) a.lse[i] = kv_nan();
+    return;
+  }
+  const int ctas = kv_ctas(total, a.ctas);
+
+  // sequences that hold nothing
+  for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
+    if (s_pre[b + 1] != s_pre[b]) continue;
+    const KvWork w = kv_work(a, b);
+    for (int i = tid; i < w.rows * a.H * (D / 8); i += kDecThreads) {
+      const int row = i / (a.H * (D / 8));
+      *reinterpret_cast<uint4*>(a.out + (long long)(w.row0 + row) * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
+          make_uint4(0, 0, 0, 0);
+    }
+    for (int i = tid; i < w.rows * a.H; i += kDecThreads) {
+      if (a.lse != nullptr) a.lse[(long long)w.row0 * a.H + i] = -INFINITY;
+      if (a.observe) a.lse2[(long long)w.row0 * a.H + i] = -INFINITY;
+    }
+  }
+  if ((int)blockIdx.x >= ctas) return;
+
+  uint8_t* ring = smem + wid * RING;
+  const uint32_t ring_u = smem_u32(ring);
+  long long u = kv_begin(total, ctas, blockIdx.x);
+  const long long u_end = kv_begin(total, ctas, blockIdx.x + 1);
+  int b = 0;
+  {
+    int hi = a.n;
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (s_pre[mid] <= u) b = mid; else hi = mid;
+    }
+  }
+
+  while (u < u_end) {
+    while (s_pre[b + 1] <= u) ++b;
+    const KvWork w = kv_work(a, b);
+    const int h = (int)((u - s_pre[b]) / w.steps);
+    const long long item0 = s_pre[b] + (long long)h * w.steps;
+    const int first = (int)(u - item0);
+    const int last = (int)min((long long)w.steps, u_end - item0);  // steps [first, last) of the pair are this CTA's
+    const int n_rows = w.rows * a.G;
+    const int* table = c.table + (size_t)w.seq * c.max_blocks;
+
+    // the query rows as the MMA's columns
+    uint32_t qf[NT][KS][2];
+    float cs[NT][2];  // scale * 2^e of rows 2t and 2t + 1 of a tile
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = 8 * nt + g;
+      uint4 v[CH][2];
+      uint32_t amax = 0;
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
+        if (r < n_rows) {
+          const __nv_bfloat16* p = a.q + (long long)(w.row0 + r / a.G) * a.q_stride +
+                                   (size_t)(h * a.G + r % a.G) * D + dec_kchunk<D>(t, j) * 16;
+          v[j][0] = *reinterpret_cast<const uint4*>(p);
+          v[j][1] = *reinterpret_cast<const uint4*>(p + 8);
+        }
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(v[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, max((x[i] << 16) & 0x7fffffffu, x[i] & 0x7fff0000u));
+      }
+      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const uint32_t e = kv_row_exp(amax);
+      const float down = __uint_as_float((254 - e) << 23);
+      const float up = amax < 0x7f800000u ? __uint_as_float(e << 23) * a.scale : kv_nan();
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const uint32_t* x = reinterpret_cast<const uint32_t*>(v[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t f = amax < 0x7f800000u ? pack_f16x2(bf16_lo(x[i]) * down, bf16_hi(x[i]) * down) : 0u;
+          qf[nt][4 * j + (i >> 1)][i & 1] = f;
+        }
+      }
+      cs[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);
+      cs[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
+    }
+
+    float o[KS][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) o[k][nt][0] = o[k][nt][1] = o[k][nt][2] = o[k][nt][3] = 0.0f;
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.0f;
+    }
+    // the last token that rows 2t and 2t + 1 of a tile see
+    int see[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) see[nt][i] = w.held - w.rows + (8 * nt + 2 * t + i) / a.G;
+    const float two_cap = a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : 0.0f;
+
+    // this warp's steps: first + wid, + kDecWarps, ..
+    const int mine = last - first > wid ? (last - first - wid + kDecWarps - 1) / kDecWarps : 0;
+    auto info = [&](int i) {  // of the warp's step i
+      StepInfo s = {0, 0.0f, 1.0f};
+      if (i < mine) {
+        const int tok = (w.step0 + first + wid + i * kDecWarps) << 4;
+        s.blk = table[tok >> c.logP];
+        if (s.blk >= 0 && s.blk < c.n_blocks) {
+          s.ks = c.scale[0][(size_t)s.blk * c.K + h];
+          s.vs = c.scale[1][(size_t)s.blk * c.K + h];
+        } else {
+          kv_raise(c, MSI_ERR_INVALID_ARG);
+          s.blk = 0;
+          s.ks = s.vs = kv_nan();
+        }
+      }
+      return s;
+    };
+    StepInfo use = info(lane), ahead = use;  // steps 32 q + lane: those in use, those being fetched
+    auto fetch = [&](int i) {
+      if ((i & 31) == 0 && i > 0) ahead = info(i + lane);
+      const int blk = __shfl_sync(0xffffffffu, ahead.blk, i & 31);
+      if (i < mine) {
+        const int tok = (w.step0 + first + wid + i * kDecWarps) << 4;
+        const size_t at = (((size_t)blk * c.K + h) * c.P + (tok & (c.P - 1))) * D;
+        const uint8_t* kp = c.codes[0] + at;
+        const uint8_t* vp = c.codes[1] + at;
+        uint8_t* dst = ring + (i % S) * SB;
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) {  // 16 D / 512 copies of 16 bytes a lane
+          const int e = n * 32 + lane, r = e / (D / 16), ch = e % (D / 16);
+          cp_async16(dst + dec_chunk<D>(r, ch), kp + e * 16, 16);
+          cp_async16(dst + 16 * D + dec_chunk<D>(r, ch), vp + e * 16, 16);
+        }
+      }
+      cp_async_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < S - 1; ++i) fetch(i);
+
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+      if ((i & 31) == 0 && i > 0) use = ahead;
+      cp_async_wait<S - 2>();
+      __syncwarp();
+      fetch(i + S - 1);
+      const int idx = first + wid + i * kDecWarps;
+      const int tok0 = (w.step0 + idx) << 4;
+      const float ks = __shfl_sync(0xffffffffu, use.ks, i & 31);
+      const float vs = __shfl_sync(0xffffffffu, use.vs, i & 31);
+      const uint32_t kb = ring_u + (i % S) * SB, vb = kb + 16 * D;
+
+      float sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const uint4 x = ld_shared_v4(kb + dec_chunk<D>(g, dec_kchunk<D>(t, j)));
+        const uint4 y = ld_shared_v4(kb + dec_chunk<D>(g + 8, dec_kchunk<D>(t, j)));
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t a0 = kv_f16x2<FMT, false>(xs[q]), a2 = kv_f16x2<FMT, true>(xs[q]);
+          const uint32_t a1 = kv_f16x2<FMT, false>(ys[q]), a3 = kv_f16x2<FMT, true>(ys[q]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_f16(sc[nt], a0, a1, a2, a3, qf[nt][4 * j + q][0], qf[nt][4 * j + q][1]);
+        }
+      }
+
+      // exponents: [0], [1] token g, [2], [3] token g + 8; rows 2t, 2t + 1
+      const float lv = __log2f(vs);
+      const bool whole = tok0 + 16 <= w.held - w.rows + 1 &&
+                         (a.window == 0 || tok0 > w.held - 1 - a.window);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float ck = cs[nt][q & 1] * ks;
+          if (a.softcap > 0.0f) sc[nt][q] = fmaf(kv_softcap(sc[nt][q] * ck, a.softcap, two_cap), kLog2e, lv);
+          else sc[nt][q] = fmaf(sc[nt][q], ck * kLog2e, lv);
+          if (!whole) {
+            const int tok = tok0 + g + (q >> 1) * 8;
+            if (tok > see[nt][q & 1] || (a.window > 0 && tok <= see[nt][q & 1] - a.window)) sc[nt][q] = -INFINITY;
+          }
+        }
+      bool over = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) over |= sc[nt][q] > m[nt][q & 1] + kLazy;
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float v = fmaxf(sc[nt][q], sc[nt][q + 2]);
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            v = fmaxf(v, m[nt][q]);
+            const float f = v == -INFINITY ? 1.0f : ex2(m[nt][q] - v);
+            m[nt][q] = v;
+            l[nt][q] *= f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) o[k][nt][q] *= f, o[k][nt][q + 2] *= f;
+          }
+      }
+      const float iv = __fdividef(1.0f, vs);
+      uint32_t pf[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p[q] = sc[nt][q] == -INFINITY ? 0.0f : ex2(sc[nt][q] - m[nt][q & 1]);
+        // a row that sees none of a block's tokens takes nothing from its scale, a NaN least of all
+        const float s0 = p[0] + p[2] == 0.0f ? 0.0f : (p[0] + p[2]) * iv, s1 = p[1] + p[3] == 0.0f ? 0.0f : (p[1] + p[3]) * iv;
+        l[nt][0] += s0;
+        l[nt][1] += s1;
+        if (a.observe) {
+          float v0 = s0, v1 = s1;
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) {
+            v0 += __shfl_xor_sync(0xffffffffu, v0, x);
+            v1 += __shfl_xor_sync(0xffffffffu, v1, x);
+          }
+          if (g == 0)
+            *reinterpret_cast<float2*>(a.step_lse + (item0 + idx) * R + 8 * nt + 2 * t) =
+                make_float2(v0 > 0.0f ? m[nt][0] + __log2f(v0) : v0 == 0.0f ? -INFINITY : v0,
+                            v1 > 0.0f ? m[nt][1] + __log2f(v1) : v1 == 0.0f ? -INFINITY : v1);
+        }
+        pf[nt][0] = transpose8x8(pack_f16x2(p[0], p[1]));
+        pf[nt][1] = transpose8x8(pack_f16x2(p[2], p[3]));
+      }
+
+      // O^T += V^T P^T: rows d0 and d0 + 1 of a column tile, tokens 2t, 2t + 1, 2t + 8, 2t + 9
+      auto values = [&](const uint32_t* x, const uint32_t* y, const uint32_t* z, const uint32_t* v, int words, int k0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (q >= words) break;
+          const uint32_t lo0 = __byte_perm(x[q], y[q], 0x5140), lo1 = __byte_perm(x[q], y[q], 0x7362);
+          const uint32_t hi0 = __byte_perm(z[q], v[q], 0x5140), hi1 = __byte_perm(z[q], v[q], 0x7362);
+          const uint32_t a0 = kv_f16x2<FMT, false>(lo0), a1 = kv_f16x2<FMT, true>(lo0);
+          const uint32_t a2 = kv_f16x2<FMT, false>(hi0), a3 = kv_f16x2<FMT, true>(hi0);
+          const uint32_t b0 = kv_f16x2<FMT, false>(lo1), b1 = kv_f16x2<FMT, true>(lo1);
+          const uint32_t b2 = kv_f16x2<FMT, false>(hi1), b3 = kv_f16x2<FMT, true>(hi1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_f16(o[k0 + 2 * q][nt], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+            mma_f16(o[k0 + 2 * q + 1][nt], b0, b1, b2, b3, pf[nt][0], pf[nt][1]);
+          }
+        }
+      };
+      if constexpr (D == 64) {
+        const int ch = g >> 1, half = (g & 1) * 8;
+        const uint2 x = ld_shared_v2(vb + dec_chunk<D>(2 * t, ch) + half), y = ld_shared_v2(vb + dec_chunk<D>(2 * t + 1, ch) + half);
+        const uint2 z = ld_shared_v2(vb + dec_chunk<D>(2 * t + 8, ch) + half), v = ld_shared_v2(vb + dec_chunk<D>(2 * t + 9, ch) + half);
+        const uint32_t xs[4] = {x.x, x.y, 0, 0}, ys[4] = {y.x, y.y, 0, 0}, zs[4] = {z.x, z.y, 0, 0}, vs4[4] = {v.x, v.y, 0, 0};
+        values(xs, ys, zs, vs4, 2, 0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < D / 128; ++j) {
+          const uint4 x = ld_shared_v4(vb + dec_chunk<D>(2 * t, g + 8 * j)), y = ld_shared_v4(vb + dec_chunk<D>(2 * t + 1, g + 8 * j));
+          const uint4 z = ld_shared_v4(vb + dec_chunk<D>(2 * t + 8, g + 8 * j)), v = ld_shared_v4(vb + dec_chunk<D>(2 * t + 9, g + 8 * j));
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+          const uint32_t zs[4] = {z.x, z.y, z.z, z.w}, vs4[4] = {v.x, v.y, v.z, v.w};
+          values(xs, ys, zs, vs4, 4, 8 * j);
+        }
+      }
+      __syncwarp();  // the stage is read: the next turn's fetch writes it
+    }
+    cp_async_wait<0>();
+
+    // the warps' parts: reference and sum per row, then the outputs
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float v = l[nt][q];
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        if (g == 0) s_m[wid][8 * nt + 2 * t + q] = m[nt][q], s_l[wid][8 * nt + 2 * t + q] = v;
+      }
+    __syncthreads();  // also: every warp is done with its ring
+    float* part = reinterpret_cast<float*>(smem) + (size_t)wid * R * D;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int r = 8 * nt + 2 * t + q;
+        float top = s_m[0][r];
+#pragma unroll
+        for (int i = 1; i < kDecWarps; ++i) top = fmaxf(top, s_m[i][r]);
+        const float f = m[nt][q] == -INFINITY ? (l[nt][q] == 0.0f ? 0.0f : l[nt][q]) : ex2(m[nt][q] - top);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const int d = D == 64 ? 8 * g + 2 * k : 128 * (k >> 3) + 16 * g + 2 * (k & 7);
+          *reinterpret_cast<float2*>(part + r * D + d) = make_float2(o[k][nt][q] * f, o[k][nt][q + 2] * f);
+        }
+      }
+    __syncthreads();
+    const bool split = first > 0 || last < w.steps;
+    const int slot = 2 * blockIdx.x + (first > 0 ? 0 : 1);
+    for (int e = tid; e < n_rows * (D / 4); e += kDecThreads) {
+      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+      float top = s_m[0][r];
+#pragma unroll
+      for (int i = 1; i < kDecWarps; ++i) top = fmaxf(top, s_m[i][r]);
+      float sum = 0.0f;
+      float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kDecWarps; ++i) {
+        sum += s_m[i][r] == -INFINITY ? s_l[i][r] : s_l[i][r] * ex2(s_m[i][r] - top);
+        const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (size_t)i * R * D + r * D + d);
+        acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+      }
+      if (split) {
+        *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * R + r) * D + d) = acc;
+        if (d == 0) a.part_ml[(size_t)slot * 2 * R + r] = top, a.part_ml[(size_t)slot * 2 * R + R + r] = sum;
+      } else {
+        const long long row = w.row0 + r / a.G;
+        const int head = h * a.G + r % a.G;
+        const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (size_t)head * D + d) =
+            make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+        if (d == 0) {
+          const float l2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
+          if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
+          if (a.observe) a.lse2[row * a.H + head] = l2;
+        }
+      }
+    }
+    __syncthreads();  // the parts are read: the ring may be written
+    u = item0 + last;
+  }
+}
+
+// Joins the parts of a split pair, one row a CTA: weights 2^(M_i - M) over the
+// parts, in the CTAs' order within each warp and warp by warp.  Bound: latency.
+constexpr int kJoinThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int R) {
+  extern __shared__ long long s_pre[];
+  __shared__ long long s_sum[kJoinThreads / 32];
+  __shared__ int s_bad;
+  __shared__ float s_f[2 * 1024], s_part[kJoinThreads / 32][D], s_red[kJoinThreads / 32], s_top;
+  grid_wait();
+  grid_release();
+  const KvCache& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int status = c.control[1];
+  const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
+  if (!ok) return;  // every row is NaN already
+  const long long total = s_pre[a.n];
+  if (total == 0) return;
+  const int ctas = kv_ctas(total, a.ctas);
+  const int b = blockIdx.x / c.K, h = blockIdx.x % c.K, r = blockIdx.y;
+  const KvWork w = kv_work(a, b);
+  if (w.steps == 0 || r >= w.rows * a.G) return;
+  const long long u0 = s_pre[b] + (long long)h * w.steps;
+  const int c0 = kv_owner(total, ctas, u0), c1 = kv_owner(total, ctas, u0 + w.steps - 1);
+  if (c0 == c1) return;
+  const long long row = w.row0 + r / a.G;
+  const int head = h * a.G + r % a.G;
+  if (status != 0) {  // before the call (no parts were written) or within it
+    for (int d = tid; d < D; d += kJoinThreads)
+      a.out[row * a.out_stride + (size_t)head * D + d] = __ushort_as_bfloat16(0x7fc0);
+    if (tid == 0 && a.lse != nullptr) a.lse[row * a.H + head] = kv_nan();
+    return;
+  }
+  const int parts = c1 - c0 + 1;
+  auto slot_of = [&](int i) { return 2 * (c0 + i) + (kv_begin(total, ctas, c0 + i) > u0 ? 0 : 1); };
+  float top = -INFINITY;
+  for (int i = tid; i < parts; i += kJoinThreads) top = fmaxf(top, a.part_ml[(size_t)slot_of(i) * 2 * R + r]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) s_red[wid] = top;
+  __syncthreads();
+  top = s_red[0];
+#pragma unroll
+  for (int i = 1; i < kJoinThreads / 32; ++i) top = fmaxf(top, s_red[i]);
+  __syncthreads();
+  float sum = 0.0f;
+  for (int i = tid; i < parts; i += kJoinThreads) {
+    const float mi = a.part_ml[(size_t)slot_of(i) * 2 * R + r], li = a.part_ml[(size_t)slot_of(i) * 2 * R + R + r];
+    const float f = mi == -INFINITY ? (li == 0.0f ? 0.0f : li) : ex2(mi - top);
+    s_f[i] = f;
+    sum += mi == -INFINITY ? li : li * f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_red[wid] = sum;
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 32; ++i) sum += s_red[i];
+  // a lane's D / 32 columns
+  constexpr int V = D / 32;
+  float acc[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) acc[v] = 0.0f;
+#pragma unroll 4
+  for (int i = wid; i < parts; i += kJoinThreads / 32) {
+    const float* p = a.part_o + ((size_t)slot_of(i) * R + r) * D;
+    const float f = s_f[i];
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = fmaf(f, p[v * 32 + lane], acc[v]);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) s_part[wid][v * 32 + lane] = acc[v];
+  __syncthreads();
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  for (int d = tid; d < D; d += kJoinThreads) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kJoinThreads / 32; ++i) v += s_part[i][d];
+    a.out[row * a.out_stride + (size_t)head * D + d] = __float2bfloat16_rn(v * f);
+  }
+  if (tid == 0) {
+    const float l2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
+    if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
+    if (a.observe) a.lse2[row * a.H + head] = l2;
+  }
+}
+
+// Attention weight of each block: over its 16-token steps, the heads and the
+// rows, 2^(step's log2 sum - row's log2 sum), in that order; one warp a block.
+constexpr int kObsThreads = 256;
+
+__global__ void __launch_bounds__(kObsThreads) kv_observe_kernel(KvAttnArgs a, int R) {
+  extern __shared__ long long s_pre[];
+  __shared__ long long s_sum[kObsThreads / 32];
+  __shared__ int s_bad;
+  grid_wait();
+  grid_release();
+  const KvCache& c = a.c;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  if (c.control[1] != 0) return;
+  if (!kv_share(a, s_pre, s_sum, &s_bad)) return;
+  const int b = blockIdx.x;
+  const KvWork w = kv_work(a, b);
+  if (w.steps == 0) return;
+  const int n = w.rows * a.G, per = c.P / 16;
+  const int j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
+  for (int j = j0 + blockIdx.y * (kObsThreads / 32) + wid; j < j1; j += gridDim.y * (kObsThreads / 32)) {
+    const int s0 = max(w.step0, j * per) - w.step0, s1 = min(w.step0 + w.steps, (j + 1) * per) - w.step0;
+    float v = 0.0f;
+    for (int h = 0; h < c.K; ++h) {
+      const float* step = a.step_lse + (s_pre[b] + (long long)h * w.steps) * R;
+      for (int e = lane; e < (s1 - s0) * R; e += 32) {
+        const int r = e % R;
+        if (r < n) {
+          const float top = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
+          if (top != -INFINITY) v += ex2(step[(long long)s0 * R + e] - top);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0) {
+      const int id = c.table[(size_t)w.seq * c.max_blocks + j];
+      if (id >= 0 && id < c.n_blocks) c.weight[id] += v;
+    }
+  }
+}
+
+template <int D, int NT, int FMT>
+cudaError_t decode_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const size_t pre = (kKvMaxSeqs + 1) * sizeof(long long);
+  const int parts = kDecWarps * 8 * NT * D * 4, ring = kDecWarps * dec_ring_bytes(D);
+  static_assert(kDecWarps * 8 * NT * D * 4 <= kDecWarps * dec_ring_bytes(D), "the parts fit the rings");
+  (void)parts;
+  cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT>, (int)(ring + pre), done);
+  if (e != cudaSuccess) return e;
+  e = launch_after(false, kv_decode_kernel<D, NT, FMT>, dim3(a.ctas), dim3(kDecThreads),
+                   ring + (a.n + 1) * sizeof(long long), s, a);
+  if (e != cudaSuccess) return e;
+  e = launch_after(true, kv_join_kernel<D>, dim3(a.n * a.c.K, a.max_rows * a.G), dim3(kJoinThreads),
+                   (a.n + 1) * sizeof(long long), s, a, 8 * NT);
+  if (e != cudaSuccess) return e;
+  *launches = 2;
+  if (a.observe) {
+    const int per = kObsThreads / 32 * 4;  // four blocks a warp
+    const long long most = min((long long)a.c.max_blocks, (long long)a.c.n_blocks);
+    e = launch_after(true, kv_observe_kernel, dim3(a.n, (unsigned)min((most + per - 1) / per, 64LL)), dim3(kObsThreads),
+                     (a.n + 1) * sizeof(long long), s, a, 8 * NT);
+    *launches = 3;
+  }
+  return e;
+}
+
+template <int D, int NT>
+cudaError_t decode_fmt(const KvAttnArgs& a, int* launches, cudaStream_t s) {
+  return a.c.fmt == MSI_KV_Q8 ? decode_as<D, NT, MSI_KV_Q8>(a, launches, s) : decode_as<D, NT, MSI_KV_E4M3>(a, launches, s);
+}
+
+}  // namespace
+
+int kv_decode_tiles(int rows, int D) {
+  return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 && D < 256 ? 4 : 0;
+}
+
+cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s) {
+  const int nt = kv_decode_tiles(a.max_rows * a.G, a.c.D);
+  if (a.c.D == 64) return nt == 1 ? decode_fmt<64, 1>(a, launches, s) : nt == 2 ? decode_fmt<64, 2>(a, launches, s) : decode_fmt<64, 4>(a, launches, s);
+  if (a.c.D == 128) return nt == 1 ? decode_fmt<128, 1>(a, launches, s) : nt == 2 ? decode_fmt<128, 2>(a, launches, s) : decode_fmt<128, 4>(a, launches, s);
+  return nt == 1 ? decode_fmt<256, 1>(a, launches, s) : decode_fmt<256, 2>(a, launches, s);
+}
+
+}  // namespace msi

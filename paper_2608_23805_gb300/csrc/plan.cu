@@ -1469,6 +1469,8 @@ msi_status msi_plan_destroy(msi_plan* p) {
 
 int msi::plan_device(const msi_plan* p) { return p->dev; }
 
+msi_status msi::note_cuda_error(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+
 extern "C" {
 
 msi_status msi_workspace_size(const msi_plan* p, int T, size_t* bytes) {

@@ -31,6 +31,8 @@ MSI_W_BF16 = 0
 MSI_W_Q4G32 = 1
 MSI_TRACE_HIT, MSI_TRACE_STAGE, MSI_TRACE_EVICT, MSI_TRACE_PREFETCH = 0, 1, 2, 3
 MSI_SLOT_VACANT, MSI_SLOT_LOADING, MSI_SLOT_DEVICE_READY, MSI_SLOT_IN_USE, MSI_SLOT_RECYCLABLE = range(5)
+MSI_KV_Q8, MSI_KV_E4M3 = 0, 1
+MSI_KV_OBSERVE = 1
 MSI_FWD_RESIDUAL = 1
 MSI_FWD_SINGLE_CTA = 2
 MSI_FWD_SHARED_UNGATED = 4
@@ -66,6 +68,21 @@ class msi_counters(ctypes.Structure):
     _fields_ = [(n, ctypes.c_uint64) for n in
                 ("forwards", "streamed_forwards", "stages", "hits", "evicts", "h2d_bytes",
                  "rejections", "prefetches", "prefetch_hits")]
+
+
+class msi_kv_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("n_seqs", "max_blocks", "n_blocks", "n_kv_heads", "head_dim",
+                                             "block_tokens", "format")]
+                + [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale", "recent", "table",
+                                                  "seq_state", "free_ids", "control", "weight")])
+
+
+class msi_kv_attention_args(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("seqs", ctypes.c_void_p), ("cu", ctypes.c_void_p), ("n_rows", ctypes.c_int),
+                ("max_rows", ctypes.c_int), ("n_heads", ctypes.c_int), ("q", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("window", ctypes.c_int), ("flags", ctypes.c_uint)]
 
 
 class msi_source_desc(ctypes.Structure):
@@ -135,6 +152,18 @@ _SIGS = {
     "msi_kernel_launches": (ctypes.c_uint64, [_P]),
     "msi_timing_enable": (ctypes.c_int, [_P, ctypes.c_int]),
     "msi_timing_read": (ctypes.c_int, [_P, _P, _P, ctypes.c_int]),
+    "msi_kv_create": (ctypes.c_int, [ctypes.POINTER(msi_kv_desc), ctypes.POINTER(_P)]),
+    "msi_kv_destroy": (ctypes.c_int, [_P]),
+    "msi_kv_init": (ctypes.c_int, [_P, _P]),
+    "msi_kv_append": (ctypes.c_int, [_P, ctypes.c_int, _P, _P, _P, _P, _P, ctypes.c_int64, ctypes.c_int, _P]),
+    "msi_kv_workspace_size": (ctypes.c_int, [_P, ctypes.POINTER(msi_kv_attention_args),
+                                             ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_int)]),
+    "msi_kv_attention": (ctypes.c_int, [_P, ctypes.POINTER(msi_kv_attention_args), _P, ctypes.c_size_t, _P]),
+    "msi_kv_evict": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int, _P]),
+    "msi_kv_release": (ctypes.c_int, [_P, ctypes.c_int, _P, _P]),
+    "msi_kv_read": (ctypes.c_int, [_P, ctypes.c_int, _P, _P, _P, ctypes.c_int, _P, _P, _P]),
+    "msi_kv_status": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_int)]),
+    "msi_kv_kernel_launches": (ctypes.c_uint64, [_P]),
     "msi_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "msi_last_cuda_error": (ctypes.c_char_p, []),
 }
