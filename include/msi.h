@@ -550,7 +550,7 @@ enum { MSI_KV_Q8 = 0, MSI_KV_E4M3 = 1 };
  * block_tokens 16, 32, 64 or 128, max_blocks * block_tokens <= 2^28,
  * n_blocks < 2^21, at most 2^27 rows a call; other shapes return
  * MSI_ERR_UNSUPPORTED.  Device buffers (K = n_kv_heads, P = block_tokens,
- * D = head_dim), each 16-byte aligned: */
+ * D = head_dim), codes, recent and seq_state 16-byte aligned: */
 typedef struct {
   int n_seqs, max_blocks, n_blocks, n_kv_heads, head_dim, block_tokens, format;
   void* k_codes;       /* [n_blocks, K, P, D] bytes */

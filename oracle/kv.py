@@ -105,12 +105,13 @@ class KvModel:
     def attention(self, s, q, scale, softcap=0.0, window=0):
         """q fp64 [r, H, D], the last tokens of sequence s -> dict of out
         [r, H, D], lse [r, H], weights [H, r, held], and what error bounds need:
-        absolute weighted values [r, H, D] and largest sum of |scale q k| [r, H]."""
+        absolute weighted values [r, H, D], largest sum of |scale q k| [r, H] and
+        number of tokens seen times their largest absolute value [r, H]."""
         k, v = self.values(s)
         r, H, D = q.shape
         G, L = H // self.K, k.shape[0]
         out, mag = np.zeros((r, H, D)), np.zeros((r, H, D))
-        lse, size = np.full((r, H), -np.inf), np.zeros((r, H))
+        lse, size, bulk = np.full((r, H), -np.inf), np.zeros((r, H)), np.zeros((r, H))
         weights = np.zeros((H, r, L))
         for i in range(r):
             at = L - r + i
@@ -128,8 +129,9 @@ class KvModel:
                 lse[i, h] = top + math.log(e.sum())
                 out[i, h], mag[i, h] = p @ vv, p @ np.abs(vv)
                 size[i, h] = (np.abs(kk) @ np.abs(q[i, h])).max() * scale
+                bulk[i, h] = vv.shape[0] * np.abs(vv).max()
                 weights[h, i, lo:at + 1] = p
-        return {"out": out, "lse": lse, "weights": weights, "mag": mag, "size": size}
+        return {"out": out, "lse": lse, "weights": weights, "mag": mag, "size": size, "bulk": bulk}
 
     def observe(self, s, weights):
         """Add attention weights [H, r, held] up per block."""

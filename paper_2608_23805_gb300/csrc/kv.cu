@@ -569,7 +569,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
       g->n_heads % c.K != 0)
     return MSI_ERR_INVALID_ARG;
   if ((g->flags & ~(unsigned)MSI_KV_OBSERVE) != 0) return MSI_ERR_INVALID_ARG;
-  if (g->n_heads / c.K > 128 || (long long)g->max_rows * (g->n_heads / c.K) > (1 << 30)) return MSI_ERR_UNSUPPORTED;
+  if (g->n_heads / c.K > 128 || (long long)g->n_rows * (g->n_heads / c.K) > (1 << 30)) return MSI_ERR_UNSUPPORTED;
   KvAttnArgs a = {};
   a.c = c;
   a.n = g->n;
@@ -589,7 +589,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.window = g->window;
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;
   const int tiles = kv_decode_tiles(a.max_rows * a.G, c.D);
-  if (tiles == 0) return MSI_ERR_UNSUPPORTED;
+  if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
   a.ctas = kv->sms;
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -597,9 +597,16 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
     at = round256(at + n);
     return ws == nullptr ? nullptr : ws + here;
   };
-  const size_t rows = 8 * (size_t)tiles;
+  const size_t rows = tiles != 0 ? 8 * (size_t)tiles : kv_chunk_rows(c.D);
   a.part_o = reinterpret_cast<float*>(take(2 * (size_t)a.ctas * rows * c.D * 4));
   a.part_ml = reinterpret_cast<float*>(take(2 * (size_t)a.ctas * rows * 2 * 4));
+  if (tiles == 0) {
+    // each sequence has at most (rows - 1) / tile + 1 row tiles
+    a.max_items = (int)(((long long)a.n_rows * a.G / (long long)rows + a.n) * c.K);
+    a.items = reinterpret_cast<int4*>(take((size_t)a.max_items * sizeof(int4)));
+    a.item_pre = reinterpret_cast<long long*>(take(((size_t)a.max_items + 1) * sizeof(long long)));
+    a.plan = reinterpret_cast<int*>(take(2 * sizeof(int)));
+  }
   if (a.observe) {
     a.lse2 = reinterpret_cast<float*>(take((size_t)a.n_rows * a.H * 4));
     // no block belongs to two sequences: the pool bounds the steps
@@ -627,10 +634,11 @@ msi_status msi_kv_create(const msi_kv_desc* desc, msi_kv** out) {
       (P != 16 && P != 32 && P != 64 && P != 128) || (long long)d.max_blocks * P > (1LL << 28) ||
       d.n_blocks >= 1 << 21)
     return MSI_ERR_UNSUPPORTED;
-  const void* need[] = {d.k_codes, d.v_codes, d.k_scale, d.v_scale, d.recent,
-                        d.table,   d.seq_state, d.free_ids, d.control, d.weight};
-  for (const void* p : need)
+  for (const void* p : {(const void*)d.k_codes, (const void*)d.v_codes, (const void*)d.recent, (const void*)d.seq_state})
     if (!aligned16(p)) return MSI_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)d.k_scale, (const void*)d.v_scale, (const void*)d.table, (const void*)d.free_ids,
+                        (const void*)d.control, (const void*)d.weight})
+    if (p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3) != 0) return MSI_ERR_INVALID_ARG;
   msi_kv* kv = new (std::nothrow) msi_kv();
   if (kv == nullptr) return MSI_ERR_CUDA;
   cudaError_t e = cudaGetDevice(&kv->dev);
@@ -717,7 +725,8 @@ msi_status msi_kv_attention(msi_kv* kv, const msi_kv_attention_args* args, void*
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)
     return MSI_ERR_WORKSPACE;
   int kernels = 0;
-  const cudaError_t e = launch_kv_decode(a, &kernels, stream);
+  const cudaError_t e = kv_decode_tiles(a.max_rows * a.G, a.c.D) != 0 ? launch_kv_decode(a, &kernels, stream)
+                                                                      : launch_kv_chunk(a, &kernels, stream);
   return launched(kv, e, "msi_kv_attention", kernels);
 }
 

@@ -70,7 +70,10 @@ struct KvAttnArgs {
   float* lse2;         // [n_rows, H] log2 of the sums (observe)
   float* step_lse;     // [steps][rows] log2 of each 16-token step's sum (observe)
   long long max_steps;
-  int* plan;           // chunk form: [items + 1] prefix of KV tiles over the items
+  // chunk form: the items (sequence, key-value head, row tile) and the prefix of their token tiles
+  int4* items;            // [max_items] {sequence of the batch, head, row tile, first token tile}
+  long long* item_pre;    // [max_items + 1]
+  int* plan;              // [2] items, and whether every sequence is in range
   int max_items;
 };
 
@@ -79,9 +82,12 @@ cudaError_t launch_kv_evict(const KvEvictArgs& a, cudaStream_t s);
 cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s);
 cudaError_t launch_kv_init(const KvCache& c, cudaStream_t s);
 // Decode form: rows of one sequence and key-value head (its part of the query
-// heads) in at most kv_decode_rows(D) columns of the MMA.
+// heads) as columns of the MMA.
 int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4), 0: not in decode form
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s);
+// Chunk form: rows of one sequence and key-value head in tiles of the MMA's rows.
+int kv_chunk_rows(int D);  // rows of an item
+cudaError_t launch_kv_chunk(const KvAttnArgs& a, int* launches, cudaStream_t s);
 
 #if defined(__CUDACC__)
 
@@ -89,7 +95,49 @@ __device__ __forceinline__ void kv_raise(const KvCache& c, int status) { atomicC
 
 __device__ __forceinline__ float kv_nan() { return __int_as_float(0x7fc00000); }
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Equal runs of `total` units: where CTA i's begins, and the CTA whose run holds unit u.
+__device__ __forceinline__ long long kv_begin(long long total, int ctas, int i) { return total * i / ctas; }
+// the CTA whose run holds step u
+__device__ __forceinline__ int kv_owner(long long total, int ctas, long long u) {
+  int i = (int)(u * ctas / total);
+  while (kv_begin(total, ctas, i + 1) <= u) ++i;
+  while (kv_begin(total, ctas, i) > u) --i;
+  return i;
+}
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 __device__ __forceinline__ int kv_seq(const int* seqs, int b) { return seqs == nullptr ? b : seqs[b]; }
+
+// One sequence of the call.
+struct KvWork {
+  int seq, row0, rows, held;
+  int step0, steps;  // 16-token steps that some row sees
+  bool ok;
+};
+
+__device__ __forceinline__ KvWork kv_work(const KvAttnArgs& a, int b) {
+  const KvCache& c = a.c;
+  KvWork w;
+  w.seq = kv_seq(a.seqs, b);
+  w.row0 = a.cu[b];
+  w.rows = a.cu[b + 1] - w.row0;
+  w.ok = w.seq >= 0 && w.seq < c.n_seqs && w.row0 >= 0 && w.rows >= 0 && w.rows <= a.max_rows &&
+         w.row0 <= a.n_rows - w.rows;
+  w.held = w.ok ? c.seq[w.seq].x : 0;
+  w.ok = w.ok && w.held >= 0 && w.held <= c.max_blocks << c.logP;
+  w.step0 = w.steps = 0;
+  if (!w.ok || w.rows == 0) return w;
+  const int lo = a.window > 0 ? max(0, w.held - w.rows - a.window + 1) : 0;
+  w.step0 = lo >> 4;
+  w.steps = ((w.held + 15) >> 4) - w.step0;
+  return w;
+}
 
 // Inclusive sums of `v` over the block's threads (a multiple of 32, at most
 // 1,024); `warp_sums` holds 32 ints.  Ends with the block in step.

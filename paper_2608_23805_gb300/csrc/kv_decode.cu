@@ -32,37 +32,11 @@ namespace msi {
 namespace {
 
 constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;  // P may reach 2^8
 
 __host__ __device__ constexpr int dec_stages(int D) { return D == 64 ? 8 : D == 128 ? 6 : 3; }
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
 __host__ __device__ constexpr int dec_ring_bytes(int D) { return dec_stages(D) * dec_stage_bytes(D); }
-
-// One sequence of the call.
-struct KvWork {
-  int seq, row0, rows, held;
-  int step0, steps;  // 16-token steps that some row sees
-  bool ok;
-};
-
-__device__ __forceinline__ KvWork kv_work(const KvAttnArgs& a, int b) {
-  const KvCache& c = a.c;
-  KvWork w;
-  w.seq = kv_seq(a.seqs, b);
-  w.row0 = a.cu[b];
-  w.rows = a.cu[b + 1] - w.row0;
-  w.ok = w.seq >= 0 && w.seq < c.n_seqs && w.row0 >= 0 && w.rows >= 0 && w.rows <= a.max_rows &&
-         w.row0 <= a.n_rows - w.rows;
-  w.held = w.ok ? c.seq[w.seq].x : 0;
-  w.ok = w.ok && w.held >= 0 && w.held <= c.max_blocks << c.logP;
-  w.step0 = w.steps = 0;
-  if (!w.ok || w.rows == 0) return w;
-  const int lo = a.window > 0 ? max(0, w.held - w.rows - a.window + 1) : 0;
-  w.step0 = lo >> 4;
-  w.steps = ((w.held + 15) >> 4) - w.step0;
-  return w;
-}
 
 // The batch's steps: s_pre[b] = steps of the pairs before sequence b, over all
 // heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
@@ -96,20 +70,11 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
   return *s_bad == 0;
 }
 
-// CTAs that take part, and where CTA i's run of `total` steps begins.
+// CTAs that take part.
 __device__ __forceinline__ int kv_ctas(long long total, int ctas) {
   const long long most = (total + kDecWarps - 1) / kDecWarps;  // a step a warp at least
   return (int)min((long long)ctas, max(most, 1LL));
 }
-__device__ __forceinline__ long long kv_begin(long long total, int ctas, int i) { return total * i / ctas; }
-// the CTA whose run holds step u
-__device__ __forceinline__ int kv_owner(long long total, int ctas, long long u) {
-  int i = (int)(u * ctas / total);
-  while (kv_begin(total, ctas, i + 1) <= u) ++i;
-  while (kv_begin(total, ctas, i) > u) --i;
-  return i;
-}
-
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -121,11 +86,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // Byte offset of 16-byte chunk `ch` of token row r in a stage's [16][D] codes.
 template <int D>
 __device__ __forceinline__ int dec_chunk(int r, int ch) {
@@ -518,7 +478,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int
   extern __shared__ long long s_pre[];
   __shared__ long long s_sum[kJoinThreads / 32];
   __shared__ int s_bad;
-  __shared__ float s_f[2 * 1024], s_part[kJoinThreads / 32][D], s_red[kJoinThreads / 32], s_top;
+  __shared__ float s_f[2 * 1024], s_part[kJoinThreads / 32][D], s_red[kJoinThreads / 32];
   grid_wait();
   grid_release();
   const KvCache& c = a.c;

@@ -90,15 +90,16 @@ def check_rows(out, lse, ref, D, softcap):
     """Scores: fp32 sums of D exact products, ten more fp32 roundings of numbers
     no larger than the largest sum of absolute products (or the cap), and query
     elements under 2^-14 of a row's largest rounded to 2^-24 of it.  That error
-    ds moves every weight by a factor 1 + 2 ds.  Weights: fp16, 2^-11 at the
-    coarsest; the sum in fp32.  Output: bf16, 8 significant bits, so 2^-8 of it."""
+    ds moves every weight by a factor 1 + 2 ds.  Weights: fp16, 2^-11 of each,
+    and where fp16's exponents end (numbers under 2^-14 of the row's largest have
+    a spacing of 2^-24 of it) 2^-25 of the largest; the sum in fp32.  Output: bf16, 8 significant bits, so 2^-8 of it."""
     ds = (2 * D + 10) * 2.0 ** -24 * (ref["size"] + softcap + 1.0) + 2.0 ** -20
     empty = np.isinf(ref["lse"])
     assert (np.isneginf(lse) == empty).all()
     assert (out[empty] == 0).all()
     got, want = lse[~empty], ref["lse"][~empty]
     assert (np.abs(got - want) <= (ds + 2.0 ** -22 * np.abs(ref["lse"]))[~empty]).all(), np.abs(got - want).max()
-    own = (2.0 ** -11 + 2 * ds)[..., None] * ref["mag"] + 1e-30
+    own = (2.0 ** -11 + 2 * ds)[..., None] * ref["mag"] + 2.0 ** -25 * ref["bulk"][..., None] + 1e-30
     tol = 2.0 ** -8 * np.abs(ref["out"]) + 1.01 * own
     bad = np.abs(out - ref["out"]) > tol
     assert not bad.any(), (np.argwhere(bad)[:3], (np.abs(out - ref["out"]) / tol).max())

@@ -411,3 +411,107 @@ def test_graph_replay():
             check_rows(out[s:s + 1].double().cpu().numpy(), lse[s:s + 1].double().cpu().numpy(), ref, 64, 0.0)
     c.check_state()
     c.check_values()
+
+
+# -- chunk form: more rows a sequence and key-value head than decode form takes --
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("K,G,P", [(1, 1, 16), (2, 4, 64), (1, 7, 32), (1, 16, 128)])
+def test_chunk(D, K, G, P, fmt):
+    """Ragged chunks of ragged sequences: a sequence that holds nothing, one
+    whose chunk is all it holds, one without rows, one with a single row."""
+    c = KvCase(n_seqs=8, K=K, D=D, P=P, fmt=fmt)
+    seqs, held = [6, 0, 2, 1, 7], [300, 41, 129, 200, 70]
+    c.append(seqs, held)
+    c.attend([2, 5, 6, 0, 7, 1], [129, 3, 34, 41, 0, 1], K * G, q_scale=2.0)
+
+
+@pytest.mark.parametrize("D", [64, 256])
+@pytest.mark.parametrize("softcap,window", [(5.0, 0), (0.0, 1), (0.0, 100), (20.0, 33), (0.0, 5000)])
+def test_chunk_scores(D, softcap, window):
+    c = KvCase(n_seqs=2, K=2, D=D, P=16)
+    c.append([0, 1], [700, 90])
+    c.attend([1, 0], [60, 200], 4, softcap=softcap, window=window, q_scale=2.0)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_chunk_rows_that_see_nothing(D):
+    """More rows than tokens: the first of them give 0 and -inf."""
+    c = KvCase(n_seqs=2, K=1, D=D, P=16)
+    c.append([0, 1], [20, 333])
+    c.attend([0, 1], [300, 340], 2)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_chunk_rising_scores(D):
+    """Keys that grow along the sequence: the running reference moves in most
+    tiles, and scores reach thousands."""
+    c = KvCase(n_seqs=1, K=1, D=D, P=16)
+    k = bits(c.rng.standard_normal((1000, 1, D)) * np.linspace(0.1, 60, 1000)[:, None, None])
+    c.append([0], [1000], k=k)
+    c.attend([0], [70], 4, q_scale=8.0)
+
+
+def test_chunk_many_sequences():
+    """More items than a pass of the plan, and CTAs with parts of many of them."""
+    c = KvCase(n_seqs=300, K=4, D=64, P=16, n_blocks=2000, max_blocks=8)
+    order = c.rng.permutation(300).tolist()
+    c.append(order, [40] * 300)
+    c.attend(order, [33 + i % 2 for i in range(300)], 4)
+
+
+@pytest.mark.parametrize("D,fmt", [(128, N.MSI_KV_Q8), (256, N.MSI_KV_E4M3)])
+def test_chunk_not_finite(D, fmt):
+    """A block with a NaN: the rows before its tokens are as without it."""
+    c = KvCase(D=D, P=16, K=1, fmt=fmt, n_seqs=2)
+    k, v = c.rows(200), c.rows(200)
+    v[100, 0, 5] = bits([np.nan])[0]
+    c.append([0], [200], k=k, v=v)
+    c.append([1], [96], k=k[:96], v=v[:96])
+    q = c.rows(200, 2)
+    out, lse = c.cache.attention(tensor(q), ints([0, 200]), 200, seqs=ints([0]))
+    ref, ref_lse = c.cache.attention(tensor(q[:96]), ints([0, 96]), 96, seqs=ints([1]))
+    assert out[96:].isnan().all()
+    assert torch.equal(out[:96], ref) and torch.equal(lse[:96], ref_lse)
+
+
+def test_chunk_equals_decode_and_is_deterministic():
+    """A chunk's last row against the same row as a decode call, within both
+    forms' roundings; strided rows, another stream, the same bits every time."""
+    c = KvCase(n_seqs=3, K=2, D=128)
+    c.append([0, 1, 2], [900, 70, 512])
+    q = tensor(c.rows(180, 16))
+    cu, seqs = ints([0, 100, 140, 180]), ints([0, 1, 2])
+    out, lse = c.cache.attention(q, cu, 100, seqs=seqs)
+    one, one_lse = c.cache.attention(q[[99, 139, 179]].contiguous(), ints([0, 1, 2, 3]), 1, seqs=seqs)
+    last = out[[99, 139, 179]]
+    assert (last.float() - one.float()).abs().max() <= 2.0 ** -7 * one.float().abs().max()
+    assert (lse[[99, 139, 179]] - one_lse).abs().max() < 1e-5
+    wide = torch.full((180, 40, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, 8:24] = q
+    res = torch.zeros((180, 20, 128), dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        c.cache.attention(wide[:, 8:24], cu, 100, seqs=seqs, out=res[:, 2:18], stream=side)
+        side.synchronize()
+        assert torch.equal(res[:, 2:18], out)
+    assert (res[:, :2] == 0).all() and (res[:, 18:] == 0).all()
+
+
+def test_chunk_refusals():
+    c = KvCase(n_seqs=2, K=1, D=64, P=16)
+    c.append([0, 1], [50, 60])
+    q = tensor(c.rows(80, 2))
+    with pytest.raises(N.MsiError) as e:
+        c.cache.attention(q, ints([0, 40, 80]), 40, observe=True)
+    assert e.value.status == N.MSI_ERR_UNSUPPORTED
+    for seqs, cu in [([0, 2], [0, 40, 80]), ([0, 1], [0, 40, 81]), ([0, 1], [0, 41, 80])]:
+        out, lse = c.cache.attention(q, ints(cu), 40, seqs=ints(seqs))
+        assert out.isnan().all() and lse.isnan().all()
+        assert c.cache.status() == N.MSI_ERR_INVALID_ARG
+    c.cache.table[0, 1] = -5
+    out, _ = c.cache.attention(q, ints([0, 40, 80]), 40)
+    assert out[10:40].isnan().all()
+    assert c.cache.status() == N.MSI_ERR_INVALID_ARG
