@@ -406,48 +406,67 @@ class KvCache:
         h = ctypes.c_void_p()
         N.check(lib.msi_kv_create(ctypes.byref(d), ctypes.byref(h)), "msi_kv_create")
         self.h = h
+        self._lib = lib
+        self._device = self.table.device
         self._ws = None
         self._need = {}
         if buffers is None:
             self.init(stream)
 
+    # A decode step's calls are short: the checks read each attribute once.
+
     @staticmethod
     def _index(t, name, n=None):
         if t is None:
             return None
-        if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        shape = t.shape
+        if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 1 or (n is not None and shape[0] != n)
+                or not t.is_contiguous()):
             raise ValueError("%s: a contiguous int32 CUDA vector%s is needed" % (name, "" if n is None else " of %d" % n))
         return t.data_ptr()
 
     def _rows(self, t, name, heads):
-        if (t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 3 or t.shape[1:] != (heads, self.D)
-                or (t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D)))):
-            raise ValueError("%s: bf16 CUDA rows [n, %d, %d], each contiguous, are needed" % (name, heads, self.D))
-        return t.data_ptr() if t.shape[0] else None
+        """(pointer, elements between rows, rows) of bf16 rows [n, heads, D]."""
+        shape, D = t.shape, self.D
+        ok = t.dtype is torch.bfloat16 and t.is_cuda and len(shape) == 3 and shape[1] == heads and shape[2] == D
+        if ok:
+            n = shape[0]
+            if n == 0:
+                return None, heads * D, 0
+            row, head, one = t.stride()
+            if one == 1 and (head == D or heads == 1):
+                return t.data_ptr(), row if n > 1 else heads * D, n
+        raise ValueError("%s: bf16 CUDA rows [n, %d, %d], each contiguous, are needed" % (name, heads, D))
+
+    @staticmethod
+    def _on(stream):
+        if stream is None:  # the current stream, without making an object for it
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return stream.cuda_stream
 
     @staticmethod
     def _used_on(stream, *tensors):
         """Tensors made here on the current stream and used on another one."""
-        if stream is not None:
-            for t in tensors:
-                t.record_stream(stream)
+        for t in tensors:
+            t.record_stream(stream)
 
     def init(self, stream=None):
         """Empty the cache: every block free, no tokens, status 0."""
-        N.check(N.lib().msi_kv_init(self.h, _stream(stream)), "msi_kv_init")
+        N.check(N.lib().msi_kv_init(self.h, self._on(stream)), "msi_kv_init")
 
     def append(self, k, v, cu, seqs=None, start=None, stream=None):
         """Rows cu[b] .. cu[b+1] of k and v [n, kv_heads, head_dim] (rows may be
         strided alike) become the tokens of sequence seqs[b] from start[b] on
         (None: at its end); tokens held from there on are dropped first."""
         n = cu.numel() - 1
-        kp, vp = self._rows(k, "k", self.K), self._rows(v, "v", self.K)
-        if v.shape[0] != k.shape[0] or (k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+        kp, stride, rows = self._rows(k, "k", self.K)
+        vp, v_stride, v_rows = self._rows(v, "v", self.K)
+        if v_rows != rows or v_stride != stride:
             raise ValueError("k and v: as many rows, with the same stride, are needed")
-        N.check(N.lib().msi_kv_append(self.h, n, self._index(seqs, "seqs", n), self._index(cu, "cu"),
-                                      self._index(start, "start", n), kp, vp,
-                                      k.stride(0) if k.shape[0] > 1 else self.K * self.D, k.shape[0], _stream(stream)),
-                "msi_kv_append")
+        rc = self._lib.msi_kv_append(self.h, n, self._index(seqs, "seqs", n), self._index(cu, "cu"),
+                                     self._index(start, "start", n), kp, vp, stride, rows, self._on(stream))
+        if rc:
+            N.check(rc, "msi_kv_append")
 
     def attention(self, q, cu, max_rows, seqs=None, out=None, lse=None, scale=None, softcap=0.0, window=0,
                   observe=False, stream=None):
@@ -455,19 +474,19 @@ class KvCache:
         tokens of sequence seqs[b], over what it holds.  max_rows: at least the
         rows of any one sequence.  scale None: head_dim ** -0.5.  observe: add up
         each block's attention weight (decode form).  Returns (out, lse)."""
-        n, rows, heads = cu.numel() - 1, q.shape[0], q.shape[1]
-        qp = self._rows(q, "q", heads)
-        out = torch.empty((rows, heads, self.D), dtype=torch.bfloat16, device=q.device) if out is None else out
-        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if lse is None else lse
-        if out.shape != q.shape:
-            raise ValueError("out: the shape of q is needed")
-        op = self._rows(out, "out", heads)
-        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
+        n, heads = cu.numel() - 1, q.shape[1]
+        qp, q_stride, rows = self._rows(q, "q", heads)
+        if out is None:
+            out = torch.empty_like(q)
+        op, out_stride, out_rows = self._rows(out, "out", heads)
+        if lse is None:
+            lse = torch.empty((rows, heads), dtype=torch.float32, device=self._device)
+        elif tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
             raise ValueError("lse: a contiguous fp32 CUDA tensor [n, heads] is needed")
-        wide = heads * self.D
+        if out_rows != rows:
+            raise ValueError("out: the shape of q is needed")
         a = N.msi_kv_attention_args(n, self._index(seqs, "seqs", n), self._index(cu, "cu"), rows, max_rows, heads, qp,
-                                    q.stride(0) if rows > 1 else wide, op, out.stride(0) if rows > 1 else wide,
-                                    lse.data_ptr() if rows else None,
+                                    q_stride, op, out_stride, lse.data_ptr() if rows else None,
                                     self.D ** -0.5 if scale is None else scale, softcap, window,
                                     N.MSI_KV_OBSERVE if observe else 0)
         key = (n, rows, max_rows, heads, observe)
@@ -479,41 +498,49 @@ class KvCache:
         ws = self._ws
         if ws is None or ws.numel() < need:
             ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
-        self._used_on(stream, out, lse, ws)
-        N.check(N.lib().msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), _stream(stream)),
-                "msi_kv_attention")
+        if stream is not None:
+            self._used_on(stream, out, lse, ws)
+        rc = self._lib.msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), self._on(stream))
+        if rc:
+            N.check(rc, "msi_kv_attention")
         return out, lse
+
+    def _which(self, seqs):
+        return (seqs, None) if isinstance(seqs, int) else (seqs.numel(), self._index(seqs, "seqs"))
 
     def evict(self, seqs, keep, sinks=0, recent=1, stream=None):
         """Sequences that hold more than `keep` blocks keep their first `sinks`,
         their last `recent` and the heaviest others.  seqs: a tensor, or the
         number of sequences 0, 1, ..."""
-        n = seqs if isinstance(seqs, int) else seqs.numel()
-        N.check(N.lib().msi_kv_evict(self.h, n, None if isinstance(seqs, int) else self._index(seqs, "seqs"), keep, sinks,
-                                     recent, _stream(stream)), "msi_kv_evict")
+        n, ids = self._which(seqs)
+        rc = self._lib.msi_kv_evict(self.h, n, ids, keep, sinks, recent, self._on(stream))
+        if rc:
+            N.check(rc, "msi_kv_evict")
 
     def release(self, seqs, stream=None):
         """End sequences (a tensor, or the number of sequences 0, 1, ...)."""
-        n = seqs if isinstance(seqs, int) else seqs.numel()
-        N.check(N.lib().msi_kv_release(self.h, n, None if isinstance(seqs, int) else self._index(seqs, "seqs"),
-                                       _stream(stream)), "msi_kv_release")
+        n, ids = self._which(seqs)
+        N.check(self._lib.msi_kv_release(self.h, n, ids, self._on(stream)), "msi_kv_release")
 
     def read(self, cu, rows, seqs=None, first=None, stream=None):
         """The tokens from first[b] on (None: 0) of sequence seqs[b] as bf16 rows
         cu[b] .. cu[b+1] of (k, v) [rows, kv_heads, head_dim]; rows = cu[-1]."""
         n = cu.numel() - 1
-        kv = torch.empty((2, rows, self.K, self.D), dtype=torch.bfloat16, device="cuda")
-        k, v = kv[0], kv[1]
-        self._used_on(stream, kv)
-        N.check(N.lib().msi_kv_read(self.h, n, self._index(seqs, "seqs", n), self._index(first, "first", n),
-                                    self._index(cu, "cu"), rows, k.data_ptr() if rows else None,
-                                    v.data_ptr() if rows else None, _stream(stream)), "msi_kv_read")
+        k = torch.empty((rows, self.K, self.D), dtype=torch.bfloat16, device=self._device)
+        v = torch.empty_like(k)
+        if stream is not None:
+            self._used_on(stream, k, v)
+        rc = self._lib.msi_kv_read(self.h, n, self._index(seqs, "seqs", n), self._index(first, "first", n),
+                                   self._index(cu, "cu"), rows, k.data_ptr() if rows else None,
+                                   v.data_ptr() if rows else None, self._on(stream))
+        if rc:
+            N.check(rc, "msi_kv_read")
         return k, v
 
     def status(self, stream=None) -> int:
         """Wait for the stream; the cache's status word (MSI_OK: 0), which is cleared."""
         s = ctypes.c_int()
-        N.check(N.lib().msi_kv_status(self.h, _stream(stream), ctypes.byref(s)), "msi_kv_status")
+        N.check(N.lib().msi_kv_status(self.h, self._on(stream), ctypes.byref(s)), "msi_kv_status")
         return s.value
 
     def launches(self) -> int:

@@ -590,7 +590,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;
   const int tiles = kv_decode_tiles(a.max_rows * a.G, c.D);
   if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
-  a.ctas = kv->sms;
+  a.ctas = kv->sms < 1024 ? kv->sms : 1024;
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -603,11 +603,13 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   if (tiles == 0) {
     // each sequence has at most (rows - 1) / tile + 1 row tiles
     a.max_items = (int)(((long long)a.n_rows * a.G / (long long)rows + a.n) * c.K);
-    a.items = reinterpret_cast<int4*>(take((size_t)a.max_items * sizeof(int4)));
+    a.items = reinterpret_cast<int4*>(take(2 * (size_t)a.max_items * sizeof(int4)));
     a.item_pre = reinterpret_cast<long long*>(take(((size_t)a.max_items + 1) * sizeof(long long)));
-    a.plan = reinterpret_cast<int*>(take(2 * sizeof(int)));
+    a.plan = reinterpret_cast<int*>(take((4 + (size_t)a.ctas) * sizeof(int)));
   }
+  if (tiles != 0) a.split = reinterpret_cast<int4*>(take((size_t)a.ctas * sizeof(int4)));
   if (a.observe) {
+    a.item_pre = reinterpret_cast<long long*>(take(((size_t)a.n + 1) * sizeof(long long)));
     a.lse2 = reinterpret_cast<float*>(take((size_t)a.n_rows * a.H * 4));
     // no block belongs to two sequences: the pool bounds the steps
     a.max_steps = ((long long)c.n_blocks * (c.P / 16)) * c.K;

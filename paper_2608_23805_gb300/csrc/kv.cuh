@@ -67,13 +67,14 @@ struct KvAttnArgs {
   // workspace
   float* part_o;       // [2 ctas][rows][D] unnormalised outputs of the parts of split items
   float* part_ml;      // [2 ctas][2][rows] their reference exponents and sums
+  int4* split;         // decode form: [ctas] the pair that begins in a CTA's run and goes on past it
   float* lse2;         // [n_rows, H] log2 of the sums (observe)
   float* step_lse;     // [steps][rows] log2 of each 16-token step's sum (observe)
   long long max_steps;
   // chunk form: the items (sequence, key-value head, row tile) and the prefix of their token tiles
-  int4* items;            // [max_items] {sequence of the batch, head, row tile, first token tile}
-  long long* item_pre;    // [max_items + 1]
-  int* plan;              // [2] items, and whether every sequence is in range
+  int4* items;            // [2 max_items] {sequence, first row, rows, held}, {head, row tile, first token tile, 0}
+  long long* item_pre;    // [max_items + 1]; decode form: [n + 1] steps before each sequence's (observe)
+  int* plan;              // [4 + ctas] items, whether every sequence is in range, CTAs; then each CTA's first item
   int max_items;
 };
 

@@ -7,8 +7,9 @@
 // An item is one sequence, key-value head and tile of 128 or 256 rows (query
 // tokens times the head's query heads, so a tile reads the shared keys once).
 // A CTA works on one item at a time, in tiles of NT tokens:
-//   conversion warps: codes from global memory to registers a tile ahead, to
-//     fp16 (two instructions a pair), to swizzled shared memory;
+//   conversion warps: 16 tokens of keys or values at a time, from global memory
+//     to registers two turns ahead, to fp16 (two instructions a pair), to
+//     swizzled shared memory;
 //   MMA warp: S = Q K^T (both from shared memory), O += P V (P from TMEM, V with
 //     the columns contiguous);
 //   softmax warps, a row a thread: S from TMEM, P = 2^(c s + log2 sv - M) to
@@ -16,7 +17,8 @@
 //     the old M unless some sum of 16 weights passes 2^11 (a bound on each of
 //     them, so no maximum is taken); only then is M moved and O rescaled.
 // With two row tiles the tensor core works on one while softmax works on the
-// other; D = 256 leaves TMEM for one row tile, with two S buffers.
+// other; D = 256 leaves TMEM for one row tile, with two S buffers, and two
+// warps share each row's columns.
 //
 // The work is the list of all token tiles of all items; each CTA takes an equal
 // run, parts of split items are joined by kv_chunk_join_kernel in order.
@@ -32,18 +34,27 @@ constexpr float kChunkTop = 2048.0f;            // sums of 16 weights above it m
 
 template <int D>
 struct Chunk {
-  static constexpr int NQ = D == 256 ? 1 : 2;   // row tiles of 128
+  static constexpr int NQ = D == 256 ? 1 : 2;     // row tiles of 128
   static constexpr int NT = D == 256 ? 64 : 128;  // tokens of a tile
   static constexpr int ROWS = 128 * NQ;
-  static constexpr int NG = NT / 16;            // 16-token granules
-  static constexpr int QBYTES = 128 * D * 2;    // one row tile
+  static constexpr int NG = NT / 16;              // 16-token granules
+  static constexpr int COLS = NQ == 2 ? NT : NT / 2;  // S columns a softmax thread takes
+  static constexpr int QBYTES = 128 * D * 2;      // one row tile
   static constexpr int KBYTES = NT * D * 2;
   static constexpr int SMEM = NQ * QBYTES + 4 * KBYTES + 1024;
-  static constexpr int SW = 4 * NQ, CW = 4;     // softmax and conversion warps
-  static constexpr int THREADS = 32 * (SW + CW + 1);
-  static constexpr int IT = NT * D / 16 / 128;  // 16-code chunks of an operand a conversion thread takes
-  static constexpr int TO = 256;                // first column of O in TMEM
+  // a conversion task: 16 tokens, up to 128 columns; 8 of them an operand and tile
+  static constexpr int TC = D < 128 ? D : 128;
+  static constexpr int LOADS = TC / 32;           // 16-byte loads a lane
+  static constexpr int TO = 256;                  // first column of O in TMEM
 };
+// 8 softmax warps, 7 conversion warps, the MMA warp; the groups share 512 x 128
+// registers out: 2 x 168 + 2 x 88 a thread.
+constexpr int kSoftWarps = 8, kConvWarps = 7, kMmaWarp = kSoftWarps + kConvWarps;
+constexpr int kChunkThreads = 32 * (kMmaWarp + 1);
+constexpr int kSoftRegs = 168, kConvRegs = 88;
+static_assert(kChunkThreads == 512 && 2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
+// What an item costs beside its tiles (queries, first scores, output), in tiles.
+constexpr int kItemCost = 2;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
   uint64_t d;
@@ -75,7 +86,21 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
       "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "
+      "%13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int N, bool INC>
+__device__ __forceinline__ void set_regs() {
+  if (INC) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 
 // ---------------------------------------------------------------------------
 // The plan of a call: items and the prefix of their token tiles
@@ -84,7 +109,8 @@ constexpr int kPlanThreads = 1024;
 
 __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int rows_tile, int nt) {
   __shared__ int s_scan[32], s_base[kKvMaxSeqs + 1], s_bad;
-  __shared__ long long s_sum[32], s_total;
+  __shared__ int4 s_work[kKvMaxSeqs];  // seq, first row, rows, tokens held
+  __shared__ long long s_sum[32], s_pre[kPlanThreads + 1], s_total;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   grid_release();
@@ -93,6 +119,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
   int tiles = 0;
   if (tid < a.n) {
     const KvWork w = kv_work(a, tid);
+    s_work[tid] = make_int4(w.seq, w.row0, w.rows, w.held);
     if (!w.ok) s_bad = 1;
     else tiles = (w.rows * a.G + rows_tile - 1) / rows_tile * c.K;
   }
@@ -111,14 +138,15 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
         const int mid = (lo + hi) >> 1;
         if (s_base[mid] <= i) lo = mid; else hi = mid;
       }
-      const KvWork w = kv_work(a, lo);
-      const int per = (w.rows * a.G + rows_tile - 1) / rows_tile;
+      const int4 w = s_work[lo];
+      const int per = (w.z * a.G + rows_tile - 1) / rows_tile;
       const int h = (i - s_base[lo]) / per, rt = (i - s_base[lo]) % per;
-      const int r1 = min(w.rows * a.G, (rt + 1) * rows_tile) - 1;
-      const int see0 = w.held - w.rows + rt * rows_tile / a.G, see1 = w.held - w.rows + r1 / a.G;
+      const int r1 = min(w.z * a.G, (rt + 1) * rows_tile) - 1;
+      const int see0 = w.w - w.z + rt * rows_tile / a.G, see1 = w.w - w.z + r1 / a.G;
       const int t0 = a.window > 0 ? max(0, see0 - a.window + 1) / nt : 0;
-      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0);  // an item that sees nothing has a tile too
-      a.items[i] = make_int4(lo, h, rt, t0);
+      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0) + kItemCost;  // an item that sees nothing has a tile too
+      a.items[2 * i] = w;
+      a.items[2 * i + 1] = make_int4(h, rt, t0, 0);
     }
     long long v = n;
 #pragma unroll
@@ -131,14 +159,28 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
     long long before = s_total + v - n;
     for (int k = 0; k < wid; ++k) before += s_sum[k];
     if (i < items) a.item_pre[i] = before;
+    s_pre[tid] = before;  // read below where one pass has all items
     __syncthreads();
     if (tid == kPlanThreads - 1) s_total = before + n;
     __syncthreads();
   }
+  const long long total = s_total;
+  const int ctas = (int)min((long long)a.ctas, max(1LL, total / (kItemCost + 1)));
+  // where each CTA's run begins
+  for (int x = tid; x < ctas && items > 0; x += kPlanThreads) {
+    const long long u = kv_begin(total, ctas, x);
+    int lo = 0, hi = items;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((items <= kPlanThreads ? s_pre[mid] : a.item_pre[mid]) <= u) lo = mid; else hi = mid;
+    }
+    a.plan[4 + x] = lo;
+  }
   if (tid == 0) {
-    a.item_pre[items] = s_total;
+    a.item_pre[items] = total;
     a.plan[0] = items;
     a.plan[1] = ok;
+    a.plan[2] = ctas;
   }
 }
 
@@ -146,48 +188,44 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
 // A CTA's parts: runs of token tiles of successive items
 // ---------------------------------------------------------------------------
 struct Part {
-  int b, h, row_tile, tile0;   // of the item; tile0: its first token tile
+  int seq, row0, rows, held;   // of the sequence
+  int h, row_tile, tile0;      // of the item; tile0: its first token tile
   int first, last, tiles;      // token tiles [first, last) of the item's `tiles` are this CTA's
-  KvWork w;
 };
 
 struct PartWalk {
   long long u, end;
   int item;
 
-  __device__ __forceinline__ void init(const KvAttnArgs& a, int cta, int ctas) {
-    const int items = a.plan[0];
+  __device__ __forceinline__ void init(const KvAttnArgs& a, int cta) {
+    const int items = a.plan[0], ctas = a.plan[2];
+    item = a.plan[4 + cta];
     const long long total = a.item_pre[items];
     u = kv_begin(total, ctas, cta);
     end = kv_begin(total, ctas, cta + 1);
-    int hi = items;
-    item = 0;
-    while (hi - item > 1) {
-      const int mid = (item + hi) >> 1;
-      if (a.item_pre[mid] <= u) item = mid; else hi = mid;
-    }
   }
   __device__ __forceinline__ bool next(const KvAttnArgs& a, Part& p) {
-    if (u >= end) return false;
-    const int4 it = a.items[item];
-    const long long p0 = a.item_pre[item], p1 = a.item_pre[item + 1];
-    p.b = it.x;
-    p.h = it.y;
-    p.row_tile = it.z;
-    p.tile0 = it.w;
-    p.tiles = (int)(p1 - p0);
-    p.first = (int)(u - p0);
-    p.last = (int)(min(p1, end) - p0);
-    p.w = kv_work(a, it.x);
-    u = min(p1, end);
-    ++item;
-    return true;
+    while (u < end) {
+      const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
+      const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
+      p.first = (int)max(u - p0, 0LL);
+      p.last = (int)(min(p1, end) - p0);
+      p.tiles = (int)(p1 - p0);
+      u = min(p1, end);
+      ++item;
+      if (p.last <= p.first) continue;  // the run ends within the item's fixed cost
+      p.seq = w.x;
+      p.row0 = w.y;
+      p.rows = w.z;
+      p.held = w.w;
+      p.h = it.x;
+      p.row_tile = it.y;
+      p.tile0 = it.z;
+      return true;
+    }
+    return false;
   }
 };
-
-__device__ __forceinline__ int chunk_ctas(const KvAttnArgs& a) {
-  return (int)min((long long)a.ctas, max(1LL, a.item_pre[a.plan[0]]));
-}
 
 // log2 weights of 16 scores: c s + ad, or its capped form, masked beyond `lim`
 // and at or before `low` (columns of the granule)
@@ -206,7 +244,7 @@ template <int D, bool CAP, bool MASK>
 __device__ __forceinline__ float chunk_max(uint32_t ts, const Granule* info, float crow, float cap, float two_cap, int lim, int low) {
   float m = -INFINITY;
 #pragma unroll 1
-  for (int ch = 0; ch < Chunk<D>::NT / 32; ++ch) {
+  for (int ch = 0; ch < Chunk<D>::COLS / 32; ++ch) {
     uint32_t s[32];
     tmem_ld32(ts + 32 * ch, s);
     tmem_wait_regs(s);
@@ -222,47 +260,107 @@ __device__ __forceinline__ float chunk_max(uint32_t ts, const Granule* info, flo
   return m;
 }
 
+// two fp32 at once
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // P of a tile in registers (two a word) and the row's sum; over: some sum of 16
-// is above kChunkTop.
+// is above kChunkTop.  The next 32 scores are on their way while 32 are worked
+// on; products and sums go two at a time.
 template <int D, bool CAP, bool MASK>
 __device__ __forceinline__ float chunk_weights(uint32_t ts, const Granule* info, float crow, float m, float cap, float two_cap,
-                                               int lim, int low, uint32_t (&p)[Chunk<D>::NT / 2], bool& over) {
+                                               int lim, int low, uint32_t (&p)[Chunk<D>::COLS / 2], bool& over) {
+  constexpr int NCH = Chunk<D>::COLS / 32;
   float sum = 0.0f;
   over = m == -INFINITY;
   const float mu = over ? 0.0f : m;
+  uint32_t s[2][32];
+  tmem_ld32(ts, s[0]);
+  tmem_wait_regs(s[0]);
 #pragma unroll
-  for (int ch = 0; ch < Chunk<D>::NT / 32; ++ch) {
-    uint32_t s[32];
-    tmem_ld32(ts + 32 * ch, s);
-    tmem_wait_regs(s);
+  for (int ch = 0; ch < NCH; ++ch) {
+    if (ch + 1 < NCH) tmem_ld32(ts + 32 * (ch + 1), s[(ch + 1) & 1]);
+    const uint32_t (&x)[32] = s[ch & 1];
 #pragma unroll
     for (int gr = 0; gr < 2; ++gr) {
       const Granule g = info[2 * ch + gr];
       const float c = crow * g.ks, ad = g.lv - mu;
-      float part = 0.0f;
+      uint64_t part[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         const int col = 32 * ch + 16 * gr + i;
-        const float x = ex2(chunk_exp<CAP, MASK>(__uint_as_float(s[16 * gr + i]), c, ad, cap, two_cap, col, lim, low));
-        const float y = ex2(chunk_exp<CAP, MASK>(__uint_as_float(s[16 * gr + i + 1]), c, ad, cap, two_cap, col + 1, lim, low));
-        part += x;
-        part += y;
-        p[col / 2] = pack_f16x2(x, y);
+        const float s0 = __uint_as_float(x[16 * gr + i]), s1 = __uint_as_float(x[16 * gr + i + 1]);
+        float e0, e1;
+        if (CAP || MASK) {
+          e0 = chunk_exp<CAP, MASK>(s0, c, ad, cap, two_cap, col, lim, low);
+          e1 = chunk_exp<CAP, MASK>(s1, c, ad, cap, two_cap, col + 1, lim, low);
+        } else {
+          unpack2(fma2(pack2(s0, s1), pack2(c, c), pack2(ad, ad)), e0, e1);
+        }
+        e0 = ex2(e0);
+        e1 = ex2(e1);
+        part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(e0, e1));
+        p[col / 2] = pack_f16x2(e0, e1);
       }
-      over |= part > kChunkTop;
+      float lo, hi;
+      unpack2(add2(part[0], part[1]), lo, hi);
+      const float all = lo + hi;
+      over |= all > kChunkTop;
       // a row that sees none of a block's tokens takes nothing from its scale, a NaN least of all
-      sum += part == 0.0f ? 0.0f : part * g.iv;
+      sum += all == 0.0f ? 0.0f : all * g.iv;
     }
+    if (ch + 1 < NCH) tmem_wait_regs(s[(ch + 1) & 1]);
   }
   return sum;
 }
 
+// The two warps that share rows (D = 256): whether any lane of either says so.
+// A warp that gives up arrives once (pair_leave) after the abort flag is set;
+// its partner looks at the flag after each of these barriers.
+__device__ __forceinline__ bool pair_any(int id, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "barrier.cta.red.or.pred q, %1, 64, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(id), "r"((uint32_t)v)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void pair_leave(int id) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(id) : "memory"); }
+
+// 16 query elements a step to fp16, in the row's power of two, to swizzled shared memory
+__device__ __forceinline__ void store_query(uint32_t sq, int row, int c8, const uint4& v, float down) {
+  st_shared_v4(sq + (c8 >> 3) * 128 * 128 + (((c8 & 7) ^ (row & 7)) << 4),
+               make_uint4(pack_f16x2(bf16_lo(v.x) * down, bf16_hi(v.x) * down), pack_f16x2(bf16_lo(v.y) * down, bf16_hi(v.y) * down),
+                          pack_f16x2(bf16_lo(v.z) * down, bf16_hi(v.z) * down), pack_f16x2(bf16_lo(v.w) * down, bf16_hi(v.w) * down)));
+}
+
 template <int D, int FMT, bool CAP>
-__global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnArgs a) {
+__global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a) {
   using C = Chunk<D>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_bar[32];
   __shared__ __align__(16) Granule s_info[4][C::NG];
+  __shared__ float s_pair[C::NQ == 1 ? 3 : 1][2][128];  // of two warps that share rows: query maximum, reference, sum
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   uint8_t* sQ = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -276,22 +374,23 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
+    const int soft = C::NQ == 2 ? 128 : 256;  // threads of a row tile
     for (int i = 0; i < 2; ++i) {
-      mbar_init(kfull + i, C::CW);
+      mbar_init(kfull + i, 8);
       mbar_init(kempty + i, 1);
-      mbar_init(vfull + i, C::CW);
+      mbar_init(vfull + i, 8);
       mbar_init(vempty + i, 1);
-      mbar_init(qfull + i, 128);
+      mbar_init(qfull + i, soft);
       mbar_init(sfull + i, 1);
-      mbar_init(pfull + i, 128);
+      mbar_init(pfull + i, soft);
       mbar_init(ofull + i, 1);
-      mbar_init(ofree + i, 128);
+      mbar_init(ofree + i, soft);
     }
     mbar_init(drain, 1);
     mbar_fence_init();
     s_abort = 0;
   }
-  if (warp == C::SW + C::CW) {
+  if (warp == kMmaWarp) {
     tmem_alloc(&s_tmem, 512);
     tmem_relinquish();
   }
@@ -308,22 +407,214 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
     if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
     // fail closed: no row of the call can be read as an answer
     const long long vecs = (long long)a.n_rows * a.H * (D / 8);
-    for (long long i = (long long)blockIdx.x * C::THREADS + tid; i < vecs; i += (long long)gridDim.x * C::THREADS) {
+    for (long long i = (long long)blockIdx.x * kChunkThreads + tid; i < vecs; i += (long long)gridDim.x * kChunkThreads) {
       const long long row = i / (a.H * (D / 8));
       *reinterpret_cast<uint4*>(a.out + row * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
           make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
     }
-    for (long long i = (long long)blockIdx.x * C::THREADS + tid; i < (long long)a.n_rows * a.H;
-         i += (long long)gridDim.x * C::THREADS)
+    for (long long i = (long long)blockIdx.x * kChunkThreads + tid; i < (long long)a.n_rows * a.H;
+         i += (long long)gridDim.x * kChunkThreads)
       if (a.lse != nullptr) a.lse[i] = kv_nan();
   }
-  const int ctas = ok ? chunk_ctas(a) : 0;
   PartWalk walk;
   walk.u = walk.end = 0;
-  if (ok && a.plan[0] > 0 && (int)blockIdx.x < ctas) walk.init(a, blockIdx.x, ctas);
+  if (ok && a.plan[0] > 0 && (int)blockIdx.x < a.plan[2]) walk.init(a, blockIdx.x);
   Part part;
 
-  if (warp == C::SW + C::CW) {
+  if (warp < kSoftWarps) {
+    // ------------------------------------------------------------------ softmax
+    set_regs<kSoftRegs, true>();
+    // a row a thread; D = 256: two threads, each half of the columns
+    const int q = C::NQ == 2 ? warp >> 2 : 0, half = C::NQ == 2 ? 0 : warp >> 2;
+    const int tr = tid & 127;  // row in the row tile
+    const int pair = 1 + (warp & 3);
+    constexpr int kTopAt = C::NQ == 1 ? 1 : 0, kSumAt = C::NQ == 1 ? 2 : 0;
+    auto gone = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0) != 0; };
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float two_cap = CAP ? 2.0f * kLog2e / a.softcap : 0.0f;
+    uint32_t kv = 0, ns = 0, no = 0;  // token tiles before the part's; S tiles seen; PVs of this row tile
+    bool go = true;
+    while (go && walk.next(a, part)) {
+      const int n = part.last - part.first;
+      const int rows = part.rows * a.G;
+      if (q > 0 && rows - part.row_tile * C::ROWS <= 128) {  // no second row tile
+        kv += n;
+        continue;
+      }
+      const int r = part.row_tile * C::ROWS + q * 128 + tr;
+      const bool valid = r < rows;
+      const int qi = valid ? r / a.G : part.rows - 1, qh = part.h * a.G + (valid ? r - qi * a.G : 0);
+      const int see = part.held - part.rows + qi;
+      const long long row = part.row0 + qi;
+      // the query row (its half) in fp16's range; the scores of the part before
+      // have all been computed
+      constexpr int QV = D / 8 / (C::NQ == 2 ? 1 : 2);
+      float crow;
+      {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + row * a.q_stride + (size_t)qh * D) + half * QV;
+        uint4 v[QV];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < QV; ++i) v[i] = valid ? src[i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < QV; ++i) {
+          const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) amax = max(amax, max((x[k] << 16) & 0x7fffffffu, x[k] & 0x7fff0000u));
+        }
+        if (C::NQ == 1) {
+          s_pair[0][half][tr] = __uint_as_float(amax);
+          pair_any(pair, false);
+          if (gone()) break;
+          amax = max(amax, __float_as_uint(s_pair[0][half ^ 1][tr]));
+        }
+        const uint32_t e = kv_row_exp(amax);
+        const bool finite = amax < 0x7f800000u;
+        const float down = __uint_as_float((254 - e) << 23);
+        crow = (finite ? __uint_as_float(e << 23) * a.scale : kv_nan()) * (CAP ? 1.0f : kLog2e);
+        const uint32_t sq = smem_u32(sQ) + q * C::QBYTES + tr * 128;
+#pragma unroll
+        for (int i = 0; i < QV; ++i) store_query(sq, tr, half * QV + i, finite ? v[i] : make_uint4(0, 0, 0, 0), down);
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&qfull[q]);
+
+      const uint32_t to = tmem + C::TO + q * D + lanes;
+      float m = -INFINITY, l = 0.0f;
+      // tiles that every row of this row tile sees whole
+      const int r_end = min(rows, part.row_tile * C::ROWS + q * 128 + 128) - 1;
+      const int see_lo = part.held - part.rows + (part.row_tile * C::ROWS + q * 128) / a.G;
+      const int see_hi = part.held - part.rows + r_end / a.G;
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int buf = C::NQ == 2 ? q : (kv + j) & 1;
+        go = mbar_wait_warp(&sfull[buf], (C::NQ == 2 ? ns : (kv + j) >> 1) & 1, abort_flag, kChunkWait);
+        if (!go) break;
+        ++ns;
+        tc_fence_after();
+        const Granule* info = s_info[(kv + j) & 3] + half * (C::COLS / 16);
+        const int tok0 = (part.tile0 + part.first + j) * C::NT + half * C::COLS;
+        const uint32_t ts = tmem + buf * C::NT + lanes;
+        const bool mask = tok0 + C::COLS - 1 > see_lo || (a.window > 0 && tok0 <= see_hi - a.window);
+        const int lim = see - tok0, low = a.window > 0 ? lim - a.window : -1;
+        uint32_t p[C::COLS / 2];
+        float sum;
+#pragma unroll 1
+        for (int pass = j == 0;; ++pass) {
+          if (pass == 1) {  // move the reference
+            float top = fmaxf(m, chunk_max<D, CAP, true>(ts + half * C::COLS, info, crow, a.softcap, two_cap, lim, low));
+            if (C::NQ == 1) {
+              s_pair[kTopAt][half][tr] = top;
+              pair_any(pair, false);
+              go = !gone();
+              if (!go) break;
+              top = fmaxf(top, s_pair[kTopAt][half ^ 1][tr]);
+            }
+            if (j > 0) {
+              // the output so far, once the last product is in it (with two row
+              // tiles the scores of this tile came after it)
+              if (C::NQ == 1) {
+                go = mbar_wait_warp(&ofull[0], (no - 1) & 1, abort_flag, kChunkWait);
+                if (!go) break;
+                tc_fence_after();
+              }
+              const float f = top == -INFINITY ? 1.0f : ex2(m - top);
+              l *= f;
+              constexpr int W = C::NQ == 2 ? D : D / 2;
+#pragma unroll 1
+              for (int d = half * W; d < (half + 1) * W; d += 32) {
+                uint32_t o[32];
+                tmem_ld32(to + d, o);
+                tmem_wait_regs(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st32(to + d, o);
+              }
+              tmem_st_wait();
+            }
+            m = top;
+          }
+          bool over;
+          sum = mask ? chunk_weights<D, CAP, true>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over)
+                     : chunk_weights<D, CAP, false>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over);
+          over = over && pass == 0;
+          // both warps of a pair are through with S here: P goes over it
+          const bool again = C::NQ == 1 ? pair_any(pair, over) : __any_sync(0xffffffffu, over);
+          if (C::NQ == 1) go = !gone();
+          if (!again || !go) break;
+        }
+        if (!go) break;
+        l += sum;
+        if constexpr (C::NQ == 2) {
+          tmem_st32(ts, p);
+          tmem_st32(ts + 32, p + 32);
+        } else {
+          tmem_st16(ts + half * 16, p);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&pfull[buf]);
+        ++no;
+      }
+      kv += n;
+      if (!go) break;
+      // The last product.  A parity names a phase only where the one before is
+      // known to be over: with two row tiles the last scores came after the last
+      // but one product, else only after the one before that.
+      if (C::NQ == 1 && n > 1) go = mbar_wait_warp(&ofull[q], no & 1, abort_flag, kChunkWait);
+      go = go && mbar_wait_warp(&ofull[q], (no - 1) & 1, abort_flag, kChunkWait);
+      if (!go) break;
+      tc_fence_after();
+      if (C::NQ == 1) {
+        s_pair[kSumAt][half][tr] = l;
+        pair_any(pair, false);
+        go = !gone();
+        if (!go) break;
+        l = s_pair[kSumAt][0][tr] + s_pair[kSumAt][1][tr];
+      }
+      const bool split = part.first > 0 || part.last < part.tiles;
+      const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+      const int slot = 2 * blockIdx.x + (part.first > 0 ? 0 : 1);
+      __nv_bfloat16* dst = a.out + row * a.out_stride + (size_t)qh * D;
+      float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + q * 128 + tr;
+      constexpr int W = C::NQ == 2 ? D : D / 2;
+#pragma unroll 1
+      for (int d = half * W; d < (half + 1) * W; d += 32) {
+        uint32_t o[32];
+        tmem_ld32(to + d, o);
+        tmem_wait_regs(o);
+        if (!valid) continue;
+        if (split) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            po[(size_t)(d / 4 + i) * C::ROWS] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                            __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+        } else {
+          uint32_t v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(dst + d + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+      }
+      __syncwarp();
+      tc_fence_before();
+      mbar_arrive(&ofree[q]);
+      if (valid && half == 0) {
+        if (split) {
+          a.part_ml[(size_t)slot * 2 * C::ROWS + q * 128 + tr] = m;
+          a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + q * 128 + tr] = l;
+        } else if (a.lse != nullptr) {
+          a.lse[row * a.H + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+        }
+      }
+      __syncwarp();
+    }
+    if (C::NQ == 1 && gone()) pair_leave(pair);
+  } else {
+  set_regs<kConvRegs, false>();  // one instruction for the whole warpgroup
+  if (warp == kMmaWarp) {
     // --------------------------------------------------------------- MMA issuer
     const uint32_t desc_hi = (uint32_t)(sw128_desc(0) >> 32);
     const uint32_t q_lo = uniform((uint32_t)sw128_desc(smem_u32(sQ)));
@@ -333,12 +624,12 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
     const uint32_t tm = uniform(tmem);
     constexpr uint32_t id_s = idesc_f16(128, C::NT, 0), id_o = idesc_f16(128, D, 1);
     uint32_t kv = 0;                  // token tiles before the part's
-    uint32_t np[2] = {0, 0};          // P tiles waited for, per S buffer
-    uint32_t parts[2] = {0, 0};       // parts begun, per row tile
+    uint32_t np0 = 0, np1 = 0;        // P tiles waited for, per S buffer
+    uint32_t parts0 = 0, parts1 = 0;  // parts begun, per row tile
     bool go = true;
     while (go && __any_sync(0xffffffffu, walk.next(a, part))) {
       const int n = (int)uniform(part.last - part.first);
-      const int nq = C::NQ == 2 && (int)uniform(part.w.rows * a.G - part.row_tile * C::ROWS) > 128 ? 2 : 1;
+      const int nq = C::NQ == 2 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > 128 ? 2 : 1;
       auto scores = [&](int q, int buf, int j, bool first_q, bool last_q) {  // S[buf] = Q[q] K(tile j)^T
         const uint32_t t = kv + j, st = t & 1;
         if (first_q && !mbar_wait_warp(&kfull[st], (t >> 1) & 1, abort_flag, kChunkWait)) return false;
@@ -358,12 +649,12 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
       };
       auto outputs = [&](int q, int buf, int j, bool first_q, bool last_q) {  // O[q] += P[buf] V(tile j)
         const uint32_t t = kv + j, st = t & 1;
-        if (!mbar_wait_warp(&pfull[buf], np[buf] & 1, abort_flag, kChunkWait)) return false;
-        ++np[buf];
+        if (!mbar_wait_warp(&pfull[buf], (buf ? np1 : np0) & 1, abort_flag, kChunkWait)) return false;
+        if (buf) ++np1; else ++np0;
         if (first_q && !mbar_wait_warp(&vfull[st], (t >> 1) & 1, abort_flag, kChunkWait)) return false;
         if (j == 0) {
-          if (!mbar_wait_warp(&ofree[q], (parts[q] & 1) ^ 1, abort_flag, kChunkWait)) return false;
-          ++parts[q];
+          if (!mbar_wait_warp(&ofree[q], ((q ? parts1 : parts0) & 1) ^ 1, abort_flag, kChunkWait)) return false;
+          if (q) ++parts1; else ++parts0;
         }
         tc_fence_after();
         if (elect_one()) {
@@ -378,9 +669,8 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
         return true;
       };
       for (int q = 0; go && q < nq; ++q) {
-        go = mbar_wait_warp(&qfull[q], parts[q] & 1, abort_flag, kChunkWait);
-        if (C::NQ == 2) go = go && scores(q, q, 0, q == 0, q == nq - 1);
-        else go = go && scores(0, kv & 1, 0, true, true);
+        go = mbar_wait_warp(&qfull[q], (q ? parts1 : parts0) & 1, abort_flag, kChunkWait);
+        go = go && scores(q, C::NQ == 2 ? q : kv & 1, 0, q == 0, q == nq - 1);
       }
       for (int j = 0; go && j < n; ++j) {
         if (C::NQ == 2) {
@@ -403,259 +693,109 @@ __global__ void __launch_bounds__(Chunk<D>::THREADS, 1) kv_chunk_kernel(KvAttnAr
       while (!mbar_try_wait(drain, 0) && clock64() - t0 < kDrainCycles) {
       }
     }
-  } else if (warp >= C::SW) {
+  } else {
     // --------------------------------------------------------------- conversion
-    const int ct = tid - 32 * C::SW;
-    constexpr int CPR = D / 16;  // 16-code chunks of a row
-    const int col = ct % CPR, row0 = ct / CPR;
-    constexpr int RSTEP = 128 / CPR;
-    const uint32_t flip = (col >> 2) & 1;  // neighbouring panels start with different halves: no bank conflicts
-    uint4 kr[C::IT], vr[C::IT];
-    // lane g of a warp: block and scales of the tile's granule g
-    struct Tile {
-      int seq, h, tok0, held;
+    // The tasks of all token tiles in order, 8 of keys then 8 of values a tile;
+    // this warp takes every seventh.  A task's block is looked up three turns
+    // ahead, its scales and codes are loaded two turns ahead.
+    struct Task {
+      int t;         // token tile of the CTA; -1: none
+      int idx;       // of the tile's 16 tasks
+      int h, tok;    // the first of its tokens
+      int id;        // block; -1: past the tokens held, -2: out of range
     };
-    int n = 0, j = 0;
-    Tile next_tile = {0, 0, 0, 0};
-    auto advance = [&]() {  // to the next token tile; false at the end
-      if (j == n) {
-        if (!walk.next(a, part)) return false;
-        n = part.last - part.first;
-        j = 0;
-        next_tile.seq = part.w.seq;
-        next_tile.h = part.h;
-        next_tile.held = part.w.held;
-        next_tile.tok0 = (part.tile0 + part.first) * C::NT;
-      } else {
-        next_tile.tok0 += C::NT;
+    constexpr int SUB = D / C::TC;  // tasks of a granule's operand
+    constexpr int CPR = C::TC / 16; // 16-code chunks of a task's row
+    const int col = lane % CPR, row0 = lane / CPR;
+    constexpr int RSTEP = 32 / CPR;
+    const uint32_t flip = (col >> 2) & 1;  // neighbouring panels start with different halves: no bank conflicts
+    int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
+    int at = warp - kSoftWarps;            // the next task to look up
+    bool more = true;
+    auto look_up = [&]() {
+      Task k = {-1, 0, 0, 0, -1};
+      const int t = at >> 4;
+      while (more && t >= base + n) {
+        base += n;
+        n = 0;
+        more = walk.next(a, part);
+        if (more) n = part.last - part.first;
       }
-      ++j;
+      if (!more) return k;
+      k.t = t;
+      k.idx = at & 15;
+      k.h = part.h;
+      k.tok = (part.tile0 + part.first + t - base) * C::NT + ((at & 7) / SUB) * 16;
+      if (k.tok < part.held) {
+        k.id = c.table[(size_t)part.seq * c.max_blocks + (k.tok >> c.logP)];
+        if (k.id < 0 || k.id >= c.n_blocks) {
+          if (lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
+          k.id = -2;
+        }
+      }
+      at += kConvWarps;
+      return k;
+    };
+    auto load = [&](const Task& k, uint4 (&x)[C::LOADS], float& ks, float& vs) {
+      const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
+      ks = vs = k.id == -2 ? kv_nan() : 1.0f;
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) x[i] = make_uint4(z, z, z, z);
+      if (k.t < 0 || k.id < 0) return;
+      const uint8_t* src = c.codes[k.idx >> 3] + (((size_t)k.id * c.K + k.h) * c.P + (k.tok & (c.P - 1)) + row0) * D +
+                           (k.idx & (SUB - 1)) * C::TC + col * 16;
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * RSTEP * D);
+      if (k.idx < 8) {
+        ks = c.scale[0][(size_t)k.id * c.K + k.h];
+        vs = c.scale[1][(size_t)k.id * c.K + k.h];
+      }
+    };
+    Task k0 = look_up(), k1 = look_up(), k2 = look_up();
+    uint4 x0[C::LOADS], x1[C::LOADS];
+    float ks0, vs0, ks1, vs1;
+    load(k0, x0, ks0, vs0);
+    load(k1, x1, ks1, vs1);
+    auto turn = [&](const Task& k, uint4 (&x)[C::LOADS], float ks, float vs) {
+      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1;
+      const bool keys = k.idx < 8;
+      if (!mbar_wait_warp(keys ? &kempty[st] : &vempty[st], ph, abort_flag, kChunkWait)) return false;
+      const int g = (k.idx & 7) / SUB, panel0 = (k.idx & (SUB - 1)) * (C::TC / 64);
+      const uint32_t tile = smem_u32(keys ? sK : sV) + st * C::KBYTES + (panel0 + (col >> 2)) * C::NT * 128 + g * 16 * 128;
+      const uint32_t ch = (col & 3) * 2;
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) {
+        const uint32_t row = i * RSTEP + row0, to = tile + row * 128, x7 = row & 7;
+        const uint4 lo = make_uint4(kv_f16x2<FMT, false>(x[i].x), kv_f16x2<FMT, true>(x[i].x), kv_f16x2<FMT, false>(x[i].y), kv_f16x2<FMT, true>(x[i].y));
+        const uint4 hi = make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w));
+        st_shared_v4(to + (((ch + flip) ^ x7) << 4), flip ? hi : lo);
+        st_shared_v4(to + (((ch + (flip ^ 1)) ^ x7) << 4), flip ? lo : hi);
+      }
+      // the granule's scales: read by softmax after the scores, which follow kfull
+      if (keys && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, log2f(vs), 1.0f / vs, 0.0f};
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(keys ? &kfull[st] : &vfull[st]);
       return true;
     };
-    auto block_of = [&](const Tile& t) {
-      const int tok = t.tok0 + 16 * lane;
-      if (lane >= C::NG || tok >= t.held) return -1;
-      const int id = c.table[(size_t)t.seq * c.max_blocks + (tok >> c.logP)];
-      if (id >= 0 && id < c.n_blocks) return id;
-      kv_raise(c, MSI_ERR_INVALID_ARG);
-      return -2;
-    };
-    auto load = [&](const Tile& t, int id, int w, uint4 (&x)[C::IT]) {
-      const uint4 zero = FMT == MSI_KV_Q8 ? make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < C::IT; ++i) {
-        const int row = i * RSTEP + row0;
-        const int blk = __shfl_sync(0xffffffffu, id, row >> 4);
-        x[i] = zero;
-        if (blk >= 0)
-          x[i] = *reinterpret_cast<const uint4*>(c.codes[w] + (((size_t)blk * c.K + t.h) * c.P + ((t.tok0 + row) & (c.P - 1))) * D + col * 16);
-      }
-    };
-    auto store = [&](uint32_t base, const uint4 (&x)[C::IT]) {
-#pragma unroll
-      for (int i = 0; i < C::IT; ++i) {
-        const int row = i * RSTEP + row0;
-        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        uint4 o[2];
-        o[0] = make_uint4(kv_f16x2<FMT, false>(u[0]), kv_f16x2<FMT, true>(u[0]), kv_f16x2<FMT, false>(u[1]), kv_f16x2<FMT, true>(u[1]));
-        o[1] = make_uint4(kv_f16x2<FMT, false>(u[2]), kv_f16x2<FMT, true>(u[2]), kv_f16x2<FMT, false>(u[3]), kv_f16x2<FMT, true>(u[3]));
-        const uint32_t at = base + (col >> 2) * C::NT * 128 + row * 128;
-        const uint32_t ch = (col & 3) * 2, x7 = row & 7;
-        st_shared_v4(at + (((ch + flip) ^ x7) << 4), flip ? o[1] : o[0]);
-        st_shared_v4(at + (((ch + (flip ^ 1)) ^ x7) << 4), flip ? o[0] : o[1]);
-      }
-    };
-    auto scale_of = [&](const Tile& t, int id, int w) {
-      return id >= 0 ? c.scale[w][(size_t)id * c.K + t.h] : id == -1 ? 1.0f : kv_nan();
-    };
-    uint32_t t = 0;
-    bool more = advance();
-    Tile cur = next_tile;
-    int id = more ? block_of(cur) : -1;
-    float ks = 1.0f, vs = 1.0f;
-    if (more) {
-      ks = scale_of(cur, id, 0);
-      vs = scale_of(cur, id, 1);
-      load(cur, id, 0, kr);
-      load(cur, id, 1, vr);
+    while (k0.t >= 0) {
+      if (!turn(k0, x0, ks0, vs0)) break;
+      k0 = k2;
+      load(k0, x0, ks0, vs0);
+      k2 = look_up();
+      if (k1.t < 0 || !turn(k1, x1, ks1, vs1)) break;
+      k1 = k2;
+      load(k1, x1, ks1, vs1);
+      k2 = look_up();
     }
-    while (more) {
-      const uint32_t st = t & 1, ph = ((t >> 1) & 1) ^ 1;
-      const bool again = advance();
-      const Tile nxt = next_tile;
-      const int nid = again ? block_of(nxt) : -1;
-      if (!mbar_wait_warp(&kempty[st], ph, abort_flag, kChunkWait)) break;
-      store(smem_u32(sK) + st * C::KBYTES, kr);
-      if (ct < C::NG) s_info[t & 3][ct] = Granule{ks, log2f(vs), 1.0f / vs, 0.0f};
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&kfull[st]);
-      if (again) {
-        ks = scale_of(nxt, nid, 0);
-        vs = scale_of(nxt, nid, 1);
-        load(nxt, nid, 0, kr);
-      }
-      if (!mbar_wait_warp(&vempty[st], ph, abort_flag, kChunkWait)) break;
-      store(smem_u32(sV) + st * C::KBYTES, vr);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&vfull[st]);
-      if (again) load(nxt, nid, 1, vr);
-      more = again;
-      ++t;
-    }
-  } else {
-    // ------------------------------------------------------------------ softmax
-    const int q = warp >> 2, tr = tid & 127;  // row tile, row in it
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const float two_cap = CAP ? 2.0f * kLog2e / a.softcap : 0.0f;
-    uint32_t kv = 0, ns[2] = {0, 0}, no = 0;  // token tiles before the part's; S waited for; PVs of this row tile
-    bool go = true;
-    while (go && walk.next(a, part)) {
-      const int n = part.last - part.first;
-      const int rows = part.w.rows * a.G;
-      if (q > 0 && rows - part.row_tile * C::ROWS <= 128) {  // no second row tile
-        kv += n;
-        continue;
-      }
-      const int r = part.row_tile * C::ROWS + q * 128 + tr;
-      const bool valid = r < rows;
-      const int qi = valid ? r / a.G : part.w.rows - 1, qh = part.h * a.G + (valid ? r - qi * a.G : 0);
-      const int see = part.w.held - part.w.rows + qi;
-      const long long row = part.w.row0 + qi;
-      // the query row in fp16's range (the scores of the part before have all been computed)
-      const uint4* src = reinterpret_cast<const uint4*>(a.q + row * a.q_stride + (size_t)qh * D);
-      uint32_t amax = 0;
-#pragma unroll 4
-      for (int i = 0; i < D / 8; ++i) {
-        const uint4 v = valid ? src[i] : make_uint4(0, 0, 0, 0);
-        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) amax = max(amax, max((x[k] << 16) & 0x7fffffffu, x[k] & 0x7fff0000u));
-      }
-      const uint32_t e = kv_row_exp(amax);
-      const bool finite = amax < 0x7f800000u;
-      const float down = __uint_as_float((254 - e) << 23);
-      const float crow = (finite ? __uint_as_float(e << 23) * a.scale : kv_nan()) * (CAP ? 1.0f : kLog2e);
-      const uint32_t sq = smem_u32(sQ) + q * C::QBYTES + tr * 128;
-#pragma unroll 4
-      for (int i = 0; i < D / 8; ++i) {
-        const uint4 v = valid && finite ? src[i] : make_uint4(0, 0, 0, 0);
-        st_shared_v4(sq + (i >> 3) * 128 * 128 + (((i & 7) ^ (tr & 7)) << 4),
-                     make_uint4(pack_f16x2(bf16_lo(v.x) * down, bf16_hi(v.x) * down), pack_f16x2(bf16_lo(v.y) * down, bf16_hi(v.y) * down),
-                                pack_f16x2(bf16_lo(v.z) * down, bf16_hi(v.z) * down), pack_f16x2(bf16_lo(v.w) * down, bf16_hi(v.w) * down)));
-      }
-      fence_proxy_async_smem();
-      mbar_arrive(&qfull[q]);
-
-      const uint32_t to = tmem + C::TO + q * D + lanes;
-      float m = -INFINITY, l = 0.0f;
-      // tiles that every row of this row tile sees whole
-      const int r_end = min(rows, part.row_tile * C::ROWS + q * 128 + 128) - 1;
-      const int see_lo = part.w.held - part.w.rows + (part.row_tile * C::ROWS + q * 128) / a.G;
-      const int see_hi = part.w.held - part.w.rows + r_end / a.G;
-#pragma unroll 1
-      for (int j = 0; j < n; ++j) {
-        const int buf = C::NQ == 2 ? q : (kv + j) & 1;
-        go = mbar_wait_warp(&sfull[buf], ns[buf] & 1, abort_flag, kChunkWait);
-        if (!go) break;
-        ++ns[buf];
-        tc_fence_after();
-        const Granule* info = s_info[(kv + j) & 3];
-        const int tok0 = (part.tile0 + part.first + j) * C::NT;
-        const uint32_t ts = tmem + buf * C::NT + lanes;
-        const bool mask = tok0 + C::NT - 1 > see_lo || (a.window > 0 && tok0 <= see_hi - a.window);
-        const int lim = see - tok0, low = a.window > 0 ? lim - a.window : -1;
-        uint32_t p[C::NT / 2];
-        float sum = 0.0f;
-        bool over = true;
-        if (j > 0) {
-          sum = mask ? chunk_weights<D, CAP, true>(ts, info, crow, m, a.softcap, two_cap, lim, low, p, over)
-                     : chunk_weights<D, CAP, false>(ts, info, crow, m, a.softcap, two_cap, lim, low, p, over);
-        }
-        if (__any_sync(0xffffffffu, over)) {
-          const float top = fmaxf(m, chunk_max<D, CAP, true>(ts, info, crow, a.softcap, two_cap, lim, low));
-          if (j > 0) {
-            // the output so far, once the last product is in it (with two row
-            // tiles the scores of this tile came after it)
-            if (C::NQ == 1) {
-              go = mbar_wait_warp(&ofull[0], (no - 1) & 1, abort_flag, kChunkWait);
-              if (!go) break;
-              tc_fence_after();
-            }
-            const float f = top == -INFINITY ? 1.0f : ex2(m - top);
-            l *= f;
-#pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
-              uint32_t o[32];
-              tmem_ld32(to + d, o);
-              tmem_wait_regs(o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(to + d, o);
-            }
-            tmem_st_wait();
-          }
-          m = top;
-          sum = chunk_weights<D, CAP, true>(ts, info, crow, m, a.softcap, two_cap, lim, low, p, over);
-        }
-        l += sum;
-#pragma unroll
-        for (int i = 0; i < C::NT / 2; i += 32) tmem_st32(ts + i, p + i);
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(&pfull[buf]);
-        ++no;
-      }
-      kv += n;
-      if (!go) break;
-      go = mbar_wait_warp(&ofull[q], (no - 1) & 1, abort_flag, kChunkWait);
-      if (!go) break;
-      tc_fence_after();
-      const bool split = part.first > 0 || part.last < part.tiles;
-      const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-      const int slot = 2 * blockIdx.x + (part.first > 0 ? 0 : 1);
-      __nv_bfloat16* dst = a.out + row * a.out_stride + (size_t)qh * D;
-      float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + q * 128 + tr;
-#pragma unroll 1
-      for (int d = 0; d < D; d += 32) {
-        uint32_t o[32];
-        tmem_ld32(to + d, o);
-        tmem_wait_regs(o);
-        if (!valid) continue;
-        if (split) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            po[(size_t)(d / 4 + i) * C::ROWS] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
-                                                            __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
-        } else {
-          uint32_t v[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(dst + d + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        }
-      }
-      tc_fence_before();
-      mbar_arrive(&ofree[q]);
-      if (valid) {
-        if (split) {
-          a.part_ml[(size_t)slot * 2 * C::ROWS + q * 128 + tr] = m;
-          a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + q * 128 + tr] = l;
-        } else if (a.lse != nullptr) {
-          a.lse[row * a.H + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
-        }
-      }
-      __syncwarp();
-    }
+  }
   }
 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == C::SW + C::CW) tmem_dealloc(tmem, 512);
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
   if (tid == 0 && s_abort != 0) kv_raise(c, MSI_ERR_TIMEOUT);
 }
 
@@ -670,24 +810,20 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   grid_release();
   const KvCache& c = a.c;
   if (a.plan[1] == 0 || a.plan[0] == 0) return;  // every row is NaN already, or there is none
-  const int ctas = chunk_ctas(a);
-  if ((int)blockIdx.x >= ctas) return;
+  const int ctas = a.plan[2];
+  if ((int)blockIdx.x + 1 >= ctas) return;
   const long long total = a.item_pre[a.plan[0]];
   const long long begin = kv_begin(total, ctas, blockIdx.x), end = kv_begin(total, ctas, blockIdx.x + 1);
-  int item = 0, hi = a.plan[0];
-  while (hi - item > 1) {
-    const int mid = (item + hi) >> 1;
-    if (a.item_pre[mid] <= end - 1) item = mid; else hi = mid;
-  }
-  const long long p0 = a.item_pre[item], p1 = a.item_pre[item + 1];
-  if (p0 < begin || p1 <= end) return;
+  // the item that the next run begins with, if it has tiles in this one
+  const int item = a.plan[4 + blockIdx.x + 1];
+  const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
+  if (p0 < begin || p0 >= end) return;
   const int parts = kv_owner(total, ctas, p1 - 1) - blockIdx.x + 1;
-  const int4 it = a.items[item];
-  const KvWork w = kv_work(a, it.x);
-  const int tr = blockIdx.y * kChunkJoinRows + (threadIdx.x & 31), r = it.z * C::ROWS + tr;
-  if (r >= w.rows * a.G) return;
-  const int qi = r / a.G, qh = it.y * a.G + r % a.G;
-  const long long row = w.row0 + qi;
+  const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
+  const int tr = blockIdx.y * kChunkJoinRows + (threadIdx.x & 31), r = it.y * C::ROWS + tr;
+  if (r >= w.z * a.G) return;
+  const int qi = r / a.G, qh = it.x * a.G + r % a.G;
+  const long long row = w.y + qi;
   const int dw = threadIdx.x >> 5;  // this warp's columns: 4 dw, + 32, ..
   const bool failed = c.control[1] != 0;
   auto slot_of = [&](int i) { return (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)); };
@@ -726,7 +862,7 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT);
   if (e != cudaSuccess) return e;
-  e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(C::THREADS), C::SMEM, s, a);
+  e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(kChunkThreads), C::SMEM, s, a);
   if (e != cudaSuccess) return e;
   e = launch_after(true, kv_chunk_join_kernel<D>, dim3(a.ctas, C::ROWS / kChunkJoinRows), dim3(kChunkJoinThreads), 0, s, a);
   *launches = 3;

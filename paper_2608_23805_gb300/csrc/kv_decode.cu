@@ -31,12 +31,17 @@
 namespace msi {
 namespace {
 
-constexpr int kDecWarps = 8, kDecThreads = 32 * kDecWarps;
 constexpr float kLazy = 8.0f;  // P may reach 2^8
 
-__host__ __device__ constexpr int dec_stages(int D) { return D == 64 ? 8 : D == 128 ? 6 : 3; }
+// Warps of a CTA, by the registers that a warp's outputs and queries take
+// (D x 8 NT of each): the more the better hidden are a step's latencies.
+__host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 16 : 8; }
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
-__host__ __device__ constexpr int dec_ring_bytes(int D) { return dec_stages(D) * dec_stage_bytes(D); }
+// Stages of a warp's ring: 192 KB a CTA, at most 8.
+__host__ __device__ constexpr int dec_stages(int D, int NT) {
+  const int s = 192 * 1024 / dec_warps(D, NT) / dec_stage_bytes(D);
+  return s > 8 ? 8 : s;
+}
 
 // The batch's steps: s_pre[b] = steps of the pairs before sequence b, over all
 // heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
@@ -71,8 +76,8 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
 }
 
 // CTAs that take part.
-__device__ __forceinline__ int kv_ctas(long long total, int ctas) {
-  const long long most = (total + kDecWarps - 1) / kDecWarps;  // a step a warp at least
+__device__ __forceinline__ int kv_ctas(long long total, int ctas, int warps) {
+  const long long most = (total + warps - 1) / warps;  // a step a warp at least
   return (int)min((long long)ctas, max(most, 1LL));
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -105,11 +110,12 @@ struct StepInfo {
 };
 
 template <int D, int NT, int FMT>
-__global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a) {
+__global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvAttnArgs a) {
+  constexpr int kDecWarps = dec_warps(D, NT), kDecThreads = 32 * kDecWarps;
   constexpr int KS = D / 16;          // MMAs along a row, and column tiles of the output
   constexpr int CH = D / 64;          // 16-byte chunks of a key row a lane takes
   constexpr int R = 8 * NT;
-  constexpr int S = dec_stages(D), SB = dec_stage_bytes(D), RING = dec_ring_bytes(D);
+  constexpr int S = dec_stages(D, NT), SB = dec_stage_bytes(D), RING = S * SB;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long s_sum[kDecWarps];
   __shared__ int s_bad;
@@ -122,6 +128,9 @@ __global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a)
   const int status = c.control[1];
   const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
   const long long total = s_pre[a.n];
+  if (tid == 0) a.split[blockIdx.x] = make_int4(0, 0, 0, 0);
+  if (a.observe && blockIdx.x == 0)
+    for (int i = tid; i <= a.n; i += kDecThreads) a.item_pre[i] = s_pre[i];
   if (!ok || status != 0 || (a.observe && total > a.max_steps)) {
     if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
     // fail closed: no row of the call can be read as an answer
@@ -136,7 +145,7 @@ __global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a)
       if (a.lse != nullptr) a.lse[i] = kv_nan();
     return;
   }
-  const int ctas = kv_ctas(total, a.ctas);
+  const int ctas = kv_ctas(total, a.ctas, kDecWarps);
 
   // sequences that hold nothing
   for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
@@ -451,6 +460,8 @@ __global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a)
       if (split) {
         *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * R + r) * D + d) = acc;
         if (d == 0) a.part_ml[(size_t)slot * 2 * R + r] = top, a.part_ml[(size_t)slot * 2 * R + R + r] = sum;
+        if (e == 0 && first == 0)
+          a.split[blockIdx.x] = make_int4(w.row0, n_rows, h, kv_owner(total, ctas, item0 + w.steps - 1) - blockIdx.x + 1);
       } else {
         const long long row = w.row0 + r / a.G;
         const int head = h * a.G + r % a.G;
@@ -469,58 +480,55 @@ __global__ void __launch_bounds__(kDecThreads, 1) kv_decode_kernel(KvAttnArgs a)
   }
 }
 
-// Joins the parts of a split pair, one row a CTA: weights 2^(M_i - M) over the
-// parts, in the CTAs' order within each warp and warp by warp.  Bound: latency.
+// Joins the parts of the pair that begins in run x and goes on past it, row y:
+// weights 2^(M_i - M) over the parts, in the CTAs' order within each warp and
+// warp by warp.  Bound: latency.
 constexpr int kJoinThreads = 256;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int R) {
-  extern __shared__ long long s_pre[];
-  __shared__ long long s_sum[kJoinThreads / 32];
-  __shared__ int s_bad;
-  __shared__ float s_f[2 * 1024], s_part[kJoinThreads / 32][D], s_red[kJoinThreads / 32];
+  constexpr int W = kJoinThreads / 32;
+  __shared__ float s_f[1024], s_part[W][D], s_red[W];
   grid_wait();
   grid_release();
-  const KvCache& c = a.c;
+  const int4 at = a.split[blockIdx.x];  // first row, rows, head, parts
+  const int r = blockIdx.y, parts = at.w;
+  if (r >= at.y || parts == 0) return;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int status = c.control[1];
-  const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
-  if (!ok) return;  // every row is NaN already
-  const long long total = s_pre[a.n];
-  if (total == 0) return;
-  const int ctas = kv_ctas(total, a.ctas);
-  const int b = blockIdx.x / c.K, h = blockIdx.x % c.K, r = blockIdx.y;
-  const KvWork w = kv_work(a, b);
-  if (w.steps == 0 || r >= w.rows * a.G) return;
-  const long long u0 = s_pre[b] + (long long)h * w.steps;
-  const int c0 = kv_owner(total, ctas, u0), c1 = kv_owner(total, ctas, u0 + w.steps - 1);
-  if (c0 == c1) return;
-  const long long row = w.row0 + r / a.G;
-  const int head = h * a.G + r % a.G;
-  if (status != 0) {  // before the call (no parts were written) or within it
-    for (int d = tid; d < D; d += kJoinThreads)
-      a.out[row * a.out_stride + (size_t)head * D + d] = __ushort_as_bfloat16(0x7fc0);
-    if (tid == 0 && a.lse != nullptr) a.lse[row * a.H + head] = kv_nan();
-    return;
-  }
-  const int parts = c1 - c0 + 1;
-  auto slot_of = [&](int i) { return 2 * (c0 + i) + (kv_begin(total, ctas, c0 + i) > u0 ? 0 : 1); };
+  const long long row = at.x + r / a.G;
+  const int head = at.z * a.G + r % a.G;
+  const bool failed = a.c.control[1] != 0;  // within the call
+  auto slot_of = [&](int i) { return (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)); };
+  float mi[4], li[4];  // this thread's parts: W 128 / 32 = 1,024 CTAs at most
   float top = -INFINITY;
-  for (int i = tid; i < parts; i += kJoinThreads) top = fmaxf(top, a.part_ml[(size_t)slot_of(i) * 2 * R + r]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = k * kJoinThreads + tid;
+    mi[k] = -INFINITY;
+    li[k] = 0.0f;
+    if (i < parts) {
+      mi[k] = a.part_ml[slot_of(i) * 2 * R + r];
+      li[k] = a.part_ml[slot_of(i) * 2 * R + R + r];
+    }
+    top = fmaxf(top, mi[k]);
+  }
+  // a lane's D / 32 columns of the first parts, loaded before the weights are known
+  constexpr int V = D / 32;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (lane == 0) s_red[wid] = top;
   __syncthreads();
   top = s_red[0];
 #pragma unroll
-  for (int i = 1; i < kJoinThreads / 32; ++i) top = fmaxf(top, s_red[i]);
+  for (int i = 1; i < W; ++i) top = fmaxf(top, s_red[i]);
   __syncthreads();
   float sum = 0.0f;
-  for (int i = tid; i < parts; i += kJoinThreads) {
-    const float mi = a.part_ml[(size_t)slot_of(i) * 2 * R + r], li = a.part_ml[(size_t)slot_of(i) * 2 * R + R + r];
-    const float f = mi == -INFINITY ? (li == 0.0f ? 0.0f : li) : ex2(mi - top);
-    s_f[i] = f;
-    sum += mi == -INFINITY ? li : li * f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = k * kJoinThreads + tid;
+    const float f = mi[k] == -INFINITY ? (li[k] == 0.0f ? 0.0f : li[k]) : ex2(mi[k] - top);
+    if (i < parts) s_f[i] = f;
+    sum += mi[k] == -INFINITY ? li[k] : li[k] * f;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -528,15 +536,13 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int
   __syncthreads();
   sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kJoinThreads / 32; ++i) sum += s_red[i];
-  // a lane's D / 32 columns
-  constexpr int V = D / 32;
+  for (int i = 0; i < W; ++i) sum += s_red[i];
   float acc[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = 0.0f;
-#pragma unroll 4
-  for (int i = wid; i < parts; i += kJoinThreads / 32) {
-    const float* p = a.part_o + ((size_t)slot_of(i) * R + r) * D;
+#pragma unroll 8
+  for (int i = wid; i < parts; i += W) {
+    const float* p = a.part_o + (slot_of(i) * R + r) * D;
     const float f = s_f[i];
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = fmaf(f, p[v * 32 + lane], acc[v]);
@@ -544,57 +550,65 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int
 #pragma unroll
   for (int v = 0; v < V; ++v) s_part[wid][v * 32 + lane] = acc[v];
   __syncthreads();
-  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float f = failed ? kv_nan() : sum == 0.0f ? 0.0f : 1.0f / sum;
   for (int d = tid; d < D; d += kJoinThreads) {
     float v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kJoinThreads / 32; ++i) v += s_part[i][d];
+    for (int i = 0; i < W; ++i) v += s_part[i][d];
     a.out[row * a.out_stride + (size_t)head * D + d] = __float2bfloat16_rn(v * f);
   }
   if (tid == 0) {
-    const float l2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
+    const float l2 = failed ? kv_nan() : sum == 0.0f ? -INFINITY : top + log2f(sum);
     if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
     if (a.observe) a.lse2[row * a.H + head] = l2;
   }
 }
 
-// Attention weight of each block: over its 16-token steps, the heads and the
-// rows, 2^(step's log2 sum - row's log2 sum), in that order; one warp a block.
-constexpr int kObsThreads = 256;
+// Attention weight of each block: over the heads, its 16-token steps and the
+// rows, 2^(step's log2 sum - row's log2 sum), a lane a term, lanes added in one
+// order.  A warp takes 8 blocks in a row.  Bound: latency.
+constexpr int kObsThreads = 256, kObsBlocks = 8;
 
 __global__ void __launch_bounds__(kObsThreads) kv_observe_kernel(KvAttnArgs a, int R) {
-  extern __shared__ long long s_pre[];
-  __shared__ long long s_sum[kObsThreads / 32];
-  __shared__ int s_bad;
+  extern __shared__ float s_top[];  // [K][R] log2 of the rows' sums; -inf: a row that is none
+  const KvCache& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, b = blockIdx.x;
   grid_wait();
   grid_release();
-  const KvCache& c = a.c;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   if (c.control[1] != 0) return;
-  if (!kv_share(a, s_pre, s_sum, &s_bad)) return;
-  const int b = blockIdx.x;
   const KvWork w = kv_work(a, b);
   if (w.steps == 0) return;
-  const int n = w.rows * a.G, per = c.P / 16;
-  const int j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
-  for (int j = j0 + blockIdx.y * (kObsThreads / 32) + wid; j < j1; j += gridDim.y * (kObsThreads / 32)) {
-    const int s0 = max(w.step0, j * per) - w.step0, s1 = min(w.step0 + w.steps, (j + 1) * per) - w.step0;
-    float v = 0.0f;
-    for (int h = 0; h < c.K; ++h) {
-      const float* step = a.step_lse + (s_pre[b] + (long long)h * w.steps) * R;
-      for (int e = lane; e < (s1 - s0) * R; e += 32) {
-        const int r = e % R;
-        if (r < n) {
-          const float top = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
-          if (top != -INFINITY) v += ex2(step[(long long)s0 * R + e] - top);
-        }
-      }
-    }
+  const int per = c.P / 16, j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
+  if (j0 + (int)blockIdx.y * (kObsThreads / 32) * kObsBlocks >= j1) return;
+  const int n = w.rows * a.G;
+  const long long pre = a.item_pre[b];
+  for (int i = tid; i < c.K * R; i += kObsThreads) {
+    const int h = i / R, r = i - h * R;
+    s_top[i] = r < n ? a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G] : -INFINITY;
+  }
+  __syncthreads();
+  for (int j = j0 + (blockIdx.y * (kObsThreads / 32) + wid) * kObsBlocks; j < j1;
+       j += gridDim.y * (kObsThreads / 32) * kObsBlocks) {
+    float mine = 0.0f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (lane == 0) {
-      const int id = c.table[(size_t)w.seq * c.max_blocks + j];
-      if (id >= 0 && id < c.n_blocks) c.weight[id] += v;
+    for (int k = 0; k < kObsBlocks; ++k) {
+      // of block j + k: steps s0 .. s1 - 1 of the pair
+      const int s0 = max(w.step0, (j + k) * per) - w.step0, s1 = min(w.step0 + w.steps, (j + k + 1) * per) - w.step0;
+      const int one = (s1 - s0) * R;
+      float v = 0.0f;
+      for (int e = lane; e < c.K * one; e += 32) {
+        const int h = e / one, f = e - h * one;
+        const float top = s_top[h * R + (f & (R - 1))];  // R is a power of two
+        const float x = a.step_lse[(pre + (long long)h * w.steps + s0) * R + f];
+        if (top != -INFINITY) v += ex2(x - top);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane == k) mine = v;
+    }
+    if (lane < kObsBlocks && j + lane < j1) {
+      const int id = c.table[(size_t)w.seq * c.max_blocks + j + lane];
+      if (id >= 0 && id < c.n_blocks) c.weight[id] += mine;
     }
   }
 }
@@ -602,24 +616,20 @@ __global__ void __launch_bounds__(kObsThreads) kv_observe_kernel(KvAttnArgs a, i
 template <int D, int NT, int FMT>
 cudaError_t decode_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
-  const size_t pre = (kKvMaxSeqs + 1) * sizeof(long long);
-  const int parts = kDecWarps * 8 * NT * D * 4, ring = kDecWarps * dec_ring_bytes(D);
-  static_assert(kDecWarps * 8 * NT * D * 4 <= kDecWarps * dec_ring_bytes(D), "the parts fit the rings");
-  (void)parts;
-  cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT>, (int)(ring + pre), done);
+  constexpr int W = dec_warps(D, NT), ring = W * dec_stages(D, NT) * dec_stage_bytes(D);
+  static_assert(W * 8 * NT * D * 4 <= ring, "the parts fit the rings");
+  cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT>, ring + (kKvMaxSeqs + 1) * (int)sizeof(long long), done);
   if (e != cudaSuccess) return e;
-  e = launch_after(false, kv_decode_kernel<D, NT, FMT>, dim3(a.ctas), dim3(kDecThreads),
-                   ring + (a.n + 1) * sizeof(long long), s, a);
+  e = launch_after(false, kv_decode_kernel<D, NT, FMT>, dim3(a.ctas), dim3(32 * W), ring + (a.n + 1) * sizeof(long long), s, a);
   if (e != cudaSuccess) return e;
-  e = launch_after(true, kv_join_kernel<D>, dim3(a.n * a.c.K, a.max_rows * a.G), dim3(kJoinThreads),
-                   (a.n + 1) * sizeof(long long), s, a, 8 * NT);
+  e = launch_after(true, kv_join_kernel<D>, dim3(a.ctas, a.max_rows * a.G), dim3(kJoinThreads), 0, s, a, 8 * NT);
   if (e != cudaSuccess) return e;
   *launches = 2;
   if (a.observe) {
-    const int per = kObsThreads / 32 * 4;  // four blocks a warp
-    const long long most = min((long long)a.c.max_blocks, (long long)a.c.n_blocks);
-    e = launch_after(true, kv_observe_kernel, dim3(a.n, (unsigned)min((most + per - 1) / per, 64LL)), dim3(kObsThreads),
-                     (a.n + 1) * sizeof(long long), s, a, 8 * NT);
+    const int per = kObsThreads / 32 * kObsBlocks;
+    const int most = min(a.c.max_blocks, a.c.n_blocks);
+    e = launch_after(true, kv_observe_kernel, dim3(a.n, min((most + per - 1) / per, 64)), dim3(kObsThreads),
+                     a.c.K * 8 * NT * sizeof(float), s, a, 8 * NT);
     *launches = 3;
   }
   return e;
