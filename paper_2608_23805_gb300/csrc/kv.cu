@@ -61,24 +61,24 @@ __device__ __forceinline__ KvSpan kv_span(const KvAppendArgs& a, int b) {
   return s;
 }
 
-// A block of one head, keys or values, is rounded by one CTA in one pass over
-// its rows, which stay in registers between the maximum and the rounding.
-// Bound: memory (16-bit rows in, codes out).  32,768 tokens of 2 heads of 128:
-// see the figures at launch_kv_append.
+// A block of one head, keys or values, is a task: rounded in one pass over its
+// rows, which stay in registers between the maximum and the rounding.  A CTA
+// takes every gridDim-th task, so that the bookkeeping is paid for once in
+// several blocks.  Bound: memory (16-bit rows in, codes out) for prompts,
+// latency for single tokens.
 template <int THREADS, int VPT>
-__global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
+__global__ void __launch_bounds__(THREADS, (VPT <= 4 ? 1024 : 512) / THREADS) kv_append_kernel(KvAppendArgs a) {
   const KvCache& c = a.c;
   __shared__ int s_scan[32];
   __shared__ unsigned s_seen[kKvMaxSeqs / 32];
-  __shared__ int s_bad, s_item[4];  // s_item: batch entry, block, new blocks before the entry's, found
-  __shared__ int s_tot[3];
+  __shared__ int s_blocks[kKvMaxSeqs + 1], s_add[kKvMaxSeqs];  // changing and new blocks before each entry's
+  __shared__ int s_bad, s_tot[3];
   __shared__ unsigned s_max[THREADS / 32];
   __shared__ unsigned s_last;
   const int tid = threadIdx.x;
-  const int task = blockIdx.x, h = blockIdx.y >> 1, w = blockIdx.y & 1;
 
   for (int i = tid; i < kKvMaxSeqs / 32; i += THREADS) s_seen[i] = 0;
-  if (tid == 0) s_bad = 0, s_item[3] = 0;
+  if (tid == 0) s_bad = 0;
   const int n_free = c.control[0];
   const int status = c.control[1];
   __syncthreads();
@@ -105,20 +105,16 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
   const int add_in = block_scan(add, s_scan);
   const int drop_in = block_scan(drop, s_scan);
   if (tid == THREADS - 1) s_tot[0] = blocks_in, s_tot[1] = add_in, s_tot[2] = drop_in;
-  if (task >= blocks_in - blocks && task < blocks_in) {
+  {
     int p = blocks_in - blocks, q = add_in - add;
     for (int b = b0; b < b1; ++b) {
       const KvSpan s = kv_span(a, b);
-      if (task < p + s.blocks) {
-        s_item[0] = b;
-        s_item[1] = (s.start >> c.logP) + task - p;
-        s_item[2] = q;
-        s_item[3] = 1;
-        break;
-      }
+      s_blocks[b] = p;
+      s_add[b] = q;
       p += s.blocks;
       q += max(0, s.have - s.had);
     }
+    if (b0 < a.n && b1 == a.n) s_blocks[a.n] = p;
   }
   __syncthreads();
   const int bad = (s_bad & 1) != 0 || n_free < 0 || n_free > c.n_blocks || s_tot[2] > c.n_blocks - n_free
@@ -127,20 +123,27 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
                                                     : 0;
   const bool go = bad == 0 && status == 0;
 
-  if (go && s_item[3] != 0) {
-    const KvSpan s = kv_span(a, s_item[0]);
-    const int j = s_item[1];
-    const int id = j < s.had ? c.table[(size_t)s.seq * c.max_blocks + j] : c.free_ids[n_free - 1 - s_item[2] - (j - s.had)];
+  const int tasks = go ? s_tot[0] * 2 * c.K : 0;
+  for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int block = task / (2 * c.K), h = (task - block * 2 * c.K) >> 1, w = task & 1;
+    int b = 0, hi = a.n;  // the entry whose blocks hold it
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (s_blocks[mid] <= block) b = mid; else hi = mid;
+    }
+    const KvSpan s = kv_span(a, b);
+    const int j = (s.start >> c.logP) + block - s_blocks[b];
+    const int id = j < s.had ? c.table[(size_t)s.seq * c.max_blocks + j] : c.free_ids[n_free - 1 - s_add[b] - (j - s.had)];
     const bool id_ok = id >= 0 && id < c.n_blocks;
     const __nv_bfloat16* x = a.x[w] + (size_t)h * c.D;
     __nv_bfloat16* ring = c.recent + (((size_t)s.seq * 2 + w) * c.K + h) * (size_t)(2 * c.P) * c.D;
-    const int vpr = c.D >> 3;  // 16-byte vectors a row
+    const int log_vpr = c.D == 64 ? 3 : c.D == 128 ? 4 : 5, vpr = 1 << log_vpr;  // 16-byte vectors a row
     const int mask2 = 2 * c.P - 1;
     uint4 v[VPT];
     unsigned amax = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int e = i * THREADS + tid, o = e / vpr, dc = (e - o * vpr) * 8;
+      const int e = i * THREADS + tid, o = e >> log_vpr, dc = (e & (vpr - 1)) * 8;
       const int tok = (j << c.logP) + o;
       v[i] = make_uint4(0, 0, 0, 0);
       if (tok < s.start)
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
       }
       if (tid == 0) {
         c.scale[w][(size_t)id * c.K + h] = finite ? scale : kv_nan();
-        if (j >= s.had && blockIdx.y == 0) {
+        if (j >= s.had && h == 0 && w == 0) {
           c.table[(size_t)s.seq * c.max_blocks + j] = id;
           c.weight[id] = 0.0f;
         }
@@ -209,7 +212,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
       if (j >= jl - 1 && !(rides && j > j0 && ((j - j0) & 1) == 0)) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-          const int e = i * THREADS + tid, o = e / vpr, dc = (e - o * vpr) * 8;
+          const int e = i * THREADS + tid, o = e >> log_vpr, dc = (e & (vpr - 1)) * 8;
           const int tok = (j << c.logP) + o;
           if (tok >= s.start && tok < s.end)
             *reinterpret_cast<uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc) = v[i];
@@ -219,18 +222,19 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
       if (rides && j == j0 && jm > j0) {  // the barrier after the maximum is behind the reads of `recent`
         const int rows = min(c.P, s.end - (jm << c.logP));
         for (int e = tid; e < rows * vpr; e += THREADS) {
-          const int o = e / vpr, dc = (e - o * vpr) * 8, tok = (jm << c.logP) + o;
+          const int o = e >> log_vpr, dc = (e & (vpr - 1)) * 8, tok = (jm << c.logP) + o;
           *reinterpret_cast<uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc) =
               *reinterpret_cast<const uint4*>(x + (size_t)(s.row0 + tok - s.start) * a.stride + dc);
         }
       }
     }
+    __syncthreads();  // s_max is read: the next task may write it
   }
 
   __syncthreads();
   if (tid == 0) {
     __threadfence();
-    s_last = atomicAdd(reinterpret_cast<unsigned*>(c.control + 2), 1u) == gridDim.x * gridDim.y - 1;
+    s_last = atomicAdd(reinterpret_cast<unsigned*>(c.control + 2), 1u) == gridDim.x - 1;
   }
   __syncthreads();
   if (s_last == 0) return;
@@ -257,8 +261,9 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(KvAppendArgs a) {
 template <int THREADS, int VPT>
 cudaError_t append_as(const KvAppendArgs& a, cudaStream_t s) {
   // each sequence changes at most (rows - 1) / P + 2 blocks
-  const long long tasks = (long long)a.n_rows / a.c.P + 2LL * a.n;
-  kv_append_kernel<THREADS, VPT><<<dim3((unsigned)tasks, 2 * a.c.K), THREADS, 0, s>>>(a);
+  const long long tasks = ((long long)a.n_rows / a.c.P + 2LL * a.n) * 2 * a.c.K;
+  const long long most = (long long)a.sms * (1536 / THREADS);
+  kv_append_kernel<THREADS, VPT><<<(unsigned)(tasks < most ? tasks : most), THREADS, 0, s>>>(a);
   return cudaGetLastError();
 }
 
@@ -266,6 +271,7 @@ cudaError_t append_as(const KvAppendArgs& a, cudaStream_t s) {
 // Eviction and release
 // ---------------------------------------------------------------------------
 constexpr int kEvictThreads = 1024;
+constexpr int kEvictFew = 4, kEvictMine = 4;  // evictions found one by one, and candidates a thread then holds
 constexpr int kEvictKeys = 24576;  // candidates held in shared memory; longer tables are read again each pass
 
 // Ordering of fp32 weights as whole numbers (a NaN with a clear sign is above
@@ -275,13 +281,18 @@ __device__ __forceinline__ unsigned kv_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One CTA a sequence: the threshold weight by a radix selection (four passes
+// One CTA a sequence.  A cache that stays at its budget gives up a block or
+// two at a time: up to four are found one by one as the block-wide least (weight,
+// then the later block), which takes two barriers each, and the entries after
+// them move down.  More: the threshold weight by a radix selection (four passes
 // over 8 bits, whole-number histograms, so the result does not depend on any
 // order), then one pass over the table in order that keeps or frees.  Bound:
 // latency (dependent passes over a few KB).
 __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(KvEvictArgs a) {
   extern __shared__ unsigned s_key[];
   __shared__ int s_scan[32], s_hist[8][256], s_pick[2];
+  __shared__ unsigned s_least[32];
+  __shared__ int s_where[32], s_gone[kEvictFew + 1];
   __shared__ unsigned s_seen[kKvMaxSeqs / 32];
   __shared__ int s_bad, s_mine[3];  // s_mine: sequence, held, freed blocks before its own
   __shared__ int s_total;
@@ -319,7 +330,55 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(KvEvictArgs a) 
   const bool go = !bad && status == 0;
   const int n = go ? (s_mine[1] + c.P - 1) >> c.logP : 0;
 
-  if (go && n > keep) {
+  if (go && n > keep && !a.release && n - keep <= kEvictFew && n - a.sinks - a.recent <= kEvictMine * kEvictThreads) {
+    int* table = c.table + (size_t)s_mine[0] * c.max_blocks;
+    const int m = n - a.sinks - a.recent, out = n - keep;
+    const int lane = tid & 31, wid = tid >> 5;
+    unsigned key[kEvictMine];
+    int left[kEvictMine];  // table index; -1: none, or found already
+#pragma unroll
+    for (int k = 0; k < kEvictMine; ++k) {
+      const int i = k * kEvictThreads + tid;
+      left[k] = i < m ? a.sinks + i : -1;
+      key[k] = 0xffffffffu;
+      if (i < m) {
+        const int id = table[a.sinks + i];
+        key[k] = id >= 0 && id < c.n_blocks ? kv_key(c.weight[id]) : 0u;
+      }
+    }
+    for (int e = 0; e < out; ++e) {
+      unsigned low = 0xffffffffu;
+      int at = -1;
+#pragma unroll
+      for (int k = 0; k < kEvictMine; ++k)  // the later of equals
+        if (left[k] >= 0 && key[k] <= low) low = key[k], at = left[k];
+      const unsigned wl = __reduce_min_sync(0xffffffffu, at >= 0 ? low : 0xffffffffu);
+      const int wa = __reduce_max_sync(0xffffffffu, at >= 0 && low == wl ? at : -1);
+      if (lane == 0) s_least[wid] = wl, s_where[wid] = wa;
+      __syncthreads();
+      const unsigned bl = __reduce_min_sync(0xffffffffu, s_where[lane] >= 0 ? s_least[lane] : 0xffffffffu);
+      const int ba = __reduce_max_sync(0xffffffffu, s_where[lane] >= 0 && s_least[lane] == bl ? s_where[lane] : -1);
+#pragma unroll
+      for (int k = 0; k < kEvictMine; ++k)
+        if (left[k] == ba) left[k] = -1;
+      if (tid == 0) {  // in table order
+        int p = e;
+        for (; p > 0 && s_gone[p - 1] > ba; --p) s_gone[p] = s_gone[p - 1];
+        s_gone[p] = ba;
+      }
+      __syncthreads();
+    }
+    if (tid < out) c.free_ids[n_free + s_mine[2] + tid] = table[s_gone[tid]];
+    for (int t0 = s_gone[0] / kEvictThreads * kEvictThreads; t0 < n; t0 += kEvictThreads) {
+      const int j = t0 + tid;
+      const int id = j < n ? table[j] : -1;
+      int down = 0;
+      bool gone = false;
+      for (int e = 0; e < out; ++e) down += s_gone[e] < j, gone |= s_gone[e] == j;
+      __syncthreads();  // the tile is read; what it writes lies in it or before
+      if (j < n && !gone && down > 0) table[j - down] = id;
+    }
+  } else if (go && n > keep) {
     int* table = c.table + (size_t)s_mine[0] * c.max_blocks;
     const int sinks = a.release ? 0 : a.sinks;
     const int m = n - sinks - a.recent;        // candidates
@@ -416,17 +475,20 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(KvEvictArgs a) 
 // ---------------------------------------------------------------------------
 // Read back and init
 // ---------------------------------------------------------------------------
-constexpr int kReadThreads = 256, kReadRows = 16;
+constexpr int kReadThreads = 256, kReadRows = 64;
 
-// 16 rows a CTA: their blocks looked up by 16 threads, then 16 codes a thread
-// to two 16-byte stores.  Bound: memory (codes in, twice as many bytes out).
-__global__ void __launch_bounds__(kReadThreads) kv_read_kernel(KvReadArgs a) {
+// `per` (at most 64) rows a CTA: their blocks looked up by a thread each, then 16
+// codes a thread and step to two 16-byte stores.  16 rows where that leaves an
+// SM no more than four CTAs, so that short calls fill the GPU (65 rows of 64
+// sequences: 6 us against 10), 64 for the rest.  Bound: memory (codes in, twice
+// as many bytes out).
+__global__ void __launch_bounds__(kReadThreads) kv_read_kernel(KvReadArgs a, int per) {
   const KvCache& c = a.c;
   __shared__ long long s_at[kReadRows];  // element of the row in a head-0 block, or -1
   __shared__ int s_id[kReadRows];
   const int tid = threadIdx.x;
-  const int row0 = blockIdx.x * kReadRows;
-  if (tid < kReadRows) {
+  const int row0 = blockIdx.x * per;
+  if (tid < per) {
     const int row = row0 + tid;
     s_at[tid] = -1;
     s_id[tid] = 0;
@@ -454,7 +516,8 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(KvReadArgs a) {
   }
   __syncthreads();
   const int per_head = c.D >> 4, per_row = c.K * per_head;
-  const int rows = min(kReadRows, a.n_rows - row0);
+  const int rows = min(per, a.n_rows - row0);
+#pragma unroll 4
   for (int e = tid; e < 2 * rows * per_row; e += kReadThreads) {
     const int w = e >= rows * per_row;
     const int f = e - w * rows * per_row;
@@ -518,7 +581,8 @@ cudaError_t launch_kv_evict(const KvEvictArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s) {
-  kv_read_kernel<<<(a.n_rows + kReadRows - 1) / kReadRows, kReadThreads, 0, s>>>(a);
+  const int per = a.n_rows <= a.sms * 4 * 16 ? 16 : kReadRows;
+  kv_read_kernel<<<(a.n_rows + per - 1) / per, kReadThreads, 0, s>>>(a, per);
   return cudaGetLastError();
 }
 
@@ -694,7 +758,7 @@ msi_status msi_kv_append(msi_kv* kv, int n, const int32_t* seqs, const int32_t* 
   if (n == 0) return MSI_OK;
   if (n_rows > 0 && (!aligned16(k) || !aligned16(v) || row_stride < 0 || row_stride % 8 != 0)) return MSI_ERR_INVALID_ARG;
   KvAppendArgs a = {kv->c, n, n_rows, seqs, cu, start,
-                    {static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v)}, row_stride};
+                    {static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v)}, row_stride, kv->sms};
   return launched(kv, launch_kv_append(a, stream), "msi_kv_append");
 }
 
@@ -757,7 +821,7 @@ msi_status msi_kv_read(msi_kv* kv, int n, const int32_t* seqs, const int32_t* fi
     return MSI_ERR_INVALID_ARG;
   if (n_rows == 0) return MSI_OK;
   KvReadArgs a = {kv->c, n, n_rows, seqs, first, cu,
-                  {static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out)}};
+                  {static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out)}, kv->sms};
   return launched(kv, launch_kv_read(a, stream), "msi_kv_read");
 }
 

@@ -32,6 +32,7 @@ struct KvAppendArgs {
   const int* start;
   const __nv_bfloat16* x[2];
   long long stride;
+  int sms;
 };
 
 struct KvEvictArgs {
@@ -49,6 +50,7 @@ struct KvReadArgs {
   const int* first;
   const int* cu;
   __nv_bfloat16* out[2];
+  int sms;
 };
 
 struct KvAttnArgs {

@@ -48,10 +48,10 @@ struct Chunk {
   static constexpr int TO = 256;                  // first column of O in TMEM
 };
 // 8 softmax warps, 7 conversion warps, the MMA warp; the groups share 512 x 128
-// registers out: 2 x 168 + 2 x 88 a thread.
+// registers out: 2 x 144 + 2 x 112 a thread.
 constexpr int kSoftWarps = 8, kConvWarps = 7, kMmaWarp = kSoftWarps + kConvWarps;
 constexpr int kChunkThreads = 32 * (kMmaWarp + 1);
-constexpr int kSoftRegs = 168, kConvRegs = 88;
+constexpr int kSoftRegs = 144, kConvRegs = 112;
 static_assert(kChunkThreads == 512 && 2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
 // What an item costs beside its tiles (queries, first scores, output), in tiles.
 constexpr int kItemCost = 2;
@@ -237,7 +237,9 @@ __device__ __forceinline__ float chunk_exp(float s, float c, float ad, float cap
 }
 
 struct Granule {
-  float ks, lv, iv, pad;  // the key scale, log2 of the value scale and its inverse
+  // the key scale, log2 of the value scale and its inverse (1 for a NaN, which
+  // comes in through the exponents of the tokens that a row sees)
+  float ks, lv, iv, pad;
 };
 
 template <int D, bool CAP, bool MASK>
@@ -281,51 +283,46 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 
 // P of a tile in registers (two a word) and the row's sum; over: some sum of 16
-// is above kChunkTop.  The next 32 scores are on their way while 32 are worked
+// is above kChunkTop.  The next 16 scores are on their way while 16 are worked
 // on; products and sums go two at a time.
 template <int D, bool CAP, bool MASK>
 __device__ __forceinline__ float chunk_weights(uint32_t ts, const Granule* info, float crow, float m, float cap, float two_cap,
                                                int lim, int low, uint32_t (&p)[Chunk<D>::COLS / 2], bool& over) {
-  constexpr int NCH = Chunk<D>::COLS / 32;
+  constexpr int N = Chunk<D>::COLS / 16;
   float sum = 0.0f;
   over = m == -INFINITY;
   const float mu = over ? 0.0f : m;
-  uint32_t s[2][32];
-  tmem_ld32(ts, s[0]);
-  tmem_wait_regs(s[0]);
+  uint32_t s[2][16];
+  tmem_ld16(ts, s[0]);
 #pragma unroll
-  for (int ch = 0; ch < NCH; ++ch) {
-    if (ch + 1 < NCH) tmem_ld32(ts + 32 * (ch + 1), s[(ch + 1) & 1]);
-    const uint32_t (&x)[32] = s[ch & 1];
+  for (int gr = 0; gr < N; ++gr) {
+    tmem_ld_wait(s[gr & 1]);
+    if (gr + 1 < N) tmem_ld16(ts + 16 * (gr + 1), s[(gr + 1) & 1]);
+    const uint32_t (&x)[16] = s[gr & 1];
+    const Granule g = info[gr];
+    const float c = crow * g.ks, ad = g.lv - mu;
+    uint64_t part[2] = {0, 0};
 #pragma unroll
-    for (int gr = 0; gr < 2; ++gr) {
-      const Granule g = info[2 * ch + gr];
-      const float c = crow * g.ks, ad = g.lv - mu;
-      uint64_t part[2] = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const int col = 32 * ch + 16 * gr + i;
-        const float s0 = __uint_as_float(x[16 * gr + i]), s1 = __uint_as_float(x[16 * gr + i + 1]);
-        float e0, e1;
-        if (CAP || MASK) {
-          e0 = chunk_exp<CAP, MASK>(s0, c, ad, cap, two_cap, col, lim, low);
-          e1 = chunk_exp<CAP, MASK>(s1, c, ad, cap, two_cap, col + 1, lim, low);
-        } else {
-          unpack2(fma2(pack2(s0, s1), pack2(c, c), pack2(ad, ad)), e0, e1);
-        }
-        e0 = ex2(e0);
-        e1 = ex2(e1);
-        part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(e0, e1));
-        p[col / 2] = pack_f16x2(e0, e1);
+    for (int i = 0; i < 16; i += 2) {
+      const int col = 16 * gr + i;
+      const float s0 = __uint_as_float(x[i]), s1 = __uint_as_float(x[i + 1]);
+      float e0, e1;
+      if (CAP || MASK) {
+        e0 = chunk_exp<CAP, MASK>(s0, c, ad, cap, two_cap, col, lim, low);
+        e1 = chunk_exp<CAP, MASK>(s1, c, ad, cap, two_cap, col + 1, lim, low);
+      } else {
+        unpack2(fma2(pack2(s0, s1), pack2(c, c), pack2(ad, ad)), e0, e1);
       }
-      float lo, hi;
-      unpack2(add2(part[0], part[1]), lo, hi);
-      const float all = lo + hi;
-      over |= all > kChunkTop;
-      // a row that sees none of a block's tokens takes nothing from its scale, a NaN least of all
-      sum += all == 0.0f ? 0.0f : all * g.iv;
+      e0 = ex2(e0);
+      e1 = ex2(e1);
+      part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(e0, e1));
+      p[col / 2] = pack_f16x2(e0, e1);
     }
-    if (ch + 1 < NCH) tmem_wait_regs(s[(ch + 1) & 1]);
+    float lo, hi;
+    unpack2(add2(part[0], part[1]), lo, hi);
+    const float all = lo + hi;
+    over |= all > kChunkTop;
+    sum = fmaf(all, g.iv, sum);
   }
   return sum;
 }
@@ -416,6 +413,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
          i += (long long)gridDim.x * kChunkThreads)
       if (a.lse != nullptr) a.lse[i] = kv_nan();
   }
+  __syncthreads();  // every warp whole again before the register split
   PartWalk walk;
   walk.u = walk.end = 0;
   if (ok && a.plan[0] > 0 && (int)blockIdx.x < a.plan[2]) walk.init(a, blockIdx.x);
@@ -583,13 +581,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         uint32_t o[32];
         tmem_ld32(to + d, o);
         tmem_wait_regs(o);
-        if (!valid) continue;
-        if (split) {
+        if (valid && split) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             po[(size_t)(d / 4 + i) * C::ROWS] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
                                                             __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
-        } else {
+        } else if (valid) {
           uint32_t v[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f);
@@ -597,6 +594,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           for (int i = 0; i < 4; ++i)
             *reinterpret_cast<uint4*>(dst + d + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         }
+        __syncwarp();  // whole again before the next load from TMEM
       }
       __syncwarp();
       tc_fence_before();
@@ -702,18 +700,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       int t;         // token tile of the CTA; -1: none
       int idx;       // of the tile's 16 tasks
       int h, tok;    // the first of its tokens
-      int id;        // block; -1: past the tokens held, -2: out of range
+      int id;        // block
+      bool held;     // false: past the tokens held
     };
     constexpr int SUB = D / C::TC;  // tasks of a granule's operand
-    constexpr int CPR = C::TC / 16; // 16-code chunks of a task's row
-    const int col = lane % CPR, row0 = lane / CPR;
-    constexpr int RSTEP = 32 / CPR;
-    const uint32_t flip = (col >> 2) & 1;  // neighbouring panels start with different halves: no bank conflicts
+    constexpr int RSTEP = C::TC == 64 ? 8 : 4;  // rows a load of the warp covers
+    // eight lanes write two rows of one 64-column panel: no bank conflicts
+    const int col = (lane & 3) + (C::TC == 64 ? 0 : (lane >> 4) << 2);  // 16-code chunk of the row
+    const int row0 = (lane >> 2) & (RSTEP - 1);
+    const uint32_t to0 = (col >> 2) * C::NT * 128 + row0 * 128 + (((col & 3) * 2 ^ row0) << 4);  // rows 4 apart: chunk ^ 4
     int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
     int at = warp - kSoftWarps;            // the next task to look up
     bool more = true;
     auto look_up = [&]() {
-      Task k = {-1, 0, 0, 0, -1};
+      Task k = {-1, 0, 0, 0, 0, false};
       const int t = at >> 4;
       while (more && t >= base + n) {
         base += n;
@@ -727,21 +727,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       k.h = part.h;
       k.tok = (part.tile0 + part.first + t - base) * C::NT + ((at & 7) / SUB) * 16;
       if (k.tok < part.held) {
+        // looked at when the codes are loaded: a wait for it here would cost a latency a task
         k.id = c.table[(size_t)part.seq * c.max_blocks + (k.tok >> c.logP)];
-        if (k.id < 0 || k.id >= c.n_blocks) {
-          if (lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
-          k.id = -2;
-        }
+        k.held = true;
       }
       at += kConvWarps;
       return k;
     };
     auto load = [&](const Task& k, uint4 (&x)[C::LOADS], float& ks, float& vs) {
       const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
-      ks = vs = k.id == -2 ? kv_nan() : 1.0f;
+      const bool there = k.id >= 0 && k.id < c.n_blocks;
+      ks = vs = k.held && !there ? kv_nan() : 1.0f;
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) x[i] = make_uint4(z, z, z, z);
-      if (k.t < 0 || k.id < 0) return;
+      if (k.held && !there && lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
+      if (!k.held || !there) return;
       const uint8_t* src = c.codes[k.idx >> 3] + (((size_t)k.id * c.K + k.h) * c.P + (k.tok & (c.P - 1)) + row0) * D +
                            (k.idx & (SUB - 1)) * C::TC + col * 16;
 #pragma unroll
@@ -761,18 +761,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const bool keys = k.idx < 8;
       if (!mbar_wait_warp(keys ? &kempty[st] : &vempty[st], ph, abort_flag, kChunkWait)) return false;
       const int g = (k.idx & 7) / SUB, panel0 = (k.idx & (SUB - 1)) * (C::TC / 64);
-      const uint32_t tile = smem_u32(keys ? sK : sV) + st * C::KBYTES + (panel0 + (col >> 2)) * C::NT * 128 + g * 16 * 128;
-      const uint32_t ch = (col & 3) * 2;
+      const uint32_t tile = smem_u32(keys ? sK : sV) + st * C::KBYTES + panel0 * C::NT * 128 + g * 16 * 128 + to0;
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
-        const uint32_t row = i * RSTEP + row0, to = tile + row * 128, x7 = row & 7;
-        const uint4 lo = make_uint4(kv_f16x2<FMT, false>(x[i].x), kv_f16x2<FMT, true>(x[i].x), kv_f16x2<FMT, false>(x[i].y), kv_f16x2<FMT, true>(x[i].y));
-        const uint4 hi = make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w));
-        st_shared_v4(to + (((ch + flip) ^ x7) << 4), flip ? hi : lo);
-        st_shared_v4(to + (((ch + (flip ^ 1)) ^ x7) << 4), flip ? lo : hi);
+        // the swizzle: chunk ^ (row & 7), the row being row0 + i RSTEP
+        const uint32_t to = RSTEP == 4 && (i & 1) ? (tile ^ 64) + i * RSTEP * 128 : tile + i * RSTEP * 128;
+        st_shared_v4(to, make_uint4(kv_f16x2<FMT, false>(x[i].x), kv_f16x2<FMT, true>(x[i].x), kv_f16x2<FMT, false>(x[i].y), kv_f16x2<FMT, true>(x[i].y)));
+        st_shared_v4(to ^ 16, make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w)));
       }
       // the granule's scales: read by softmax after the scores, which follow kfull
-      if (keys && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, log2f(vs), 1.0f / vs, 0.0f};
+      if (keys && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, log2f(vs), vs > 0.0f ? 1.0f / vs : 1.0f, 0.0f};
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(keys ? &kfull[st] : &vfull[st]);

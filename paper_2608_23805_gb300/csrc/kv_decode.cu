@@ -25,7 +25,7 @@
 // Split.  The work is the list of all 16-token steps of all (sequence, head)
 // pairs; each CTA takes an equal run of it, whatever the lengths.  A pair that
 // lies in one CTA is finished there; parts of split ones are joined by
-// kv_join_kernel in the CTAs' order, so results do not depend on timing.
+// kv_finish_kernel in the CTAs' order, so results do not depend on timing.
 #include "kv.cuh"
 
 namespace msi {
@@ -86,6 +86,9 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -103,13 +106,13 @@ __device__ __forceinline__ int dec_kchunk(int t, int j) {
   return D == 64 ? t : D == 128 ? 2 * t + j : 2 * t + (j & 1) + 8 * (j >> 1);
 }
 
-// A lane's view of the steps of a run: the block, scales of step base + lane.
+// A lane's view of the steps of a run: block and scales of step base + lane.
 struct StepInfo {
   int blk;
-  float ks, vs;
+  float ks, lv, iv;  // key scale, log2 of the value scale and its inverse
 };
 
-template <int D, int NT, int FMT>
+template <int D, int NT, int FMT, bool OBS>
 __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvAttnArgs a) {
   constexpr int kDecWarps = dec_warps(D, NT), kDecThreads = 32 * kDecWarps;
   constexpr int KS = D / 16;          // MMAs along a row, and column tiles of the output
@@ -129,9 +132,9 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
   const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
   const long long total = s_pre[a.n];
   if (tid == 0) a.split[blockIdx.x] = make_int4(0, 0, 0, 0);
-  if (a.observe && blockIdx.x == 0)
+  if (OBS && blockIdx.x == 0)
     for (int i = tid; i <= a.n; i += kDecThreads) a.item_pre[i] = s_pre[i];
-  if (!ok || status != 0 || (a.observe && total > a.max_steps)) {
+  if (!ok || status != 0 || (OBS && total > a.max_steps)) {
     if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
     // fail closed: no row of the call can be read as an answer
     const long long vecs = (long long)a.n_rows * a.H * (D / 8);
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
     }
     for (int i = tid; i < w.rows * a.H; i += kDecThreads) {
       if (a.lse != nullptr) a.lse[(long long)w.row0 * a.H + i] = -INFINITY;
-      if (a.observe) a.lse2[(long long)w.row0 * a.H + i] = -INFINITY;
+      if (OBS) a.lse2[(long long)w.row0 * a.H + i] = -INFINITY;
     }
   }
   if ((int)blockIdx.x >= ctas) return;
@@ -184,11 +187,12 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
     const int first = (int)(u - item0);
     const int last = (int)min((long long)w.steps, u_end - item0);  // steps [first, last) of the pair are this CTA's
     const int n_rows = w.rows * a.G;
+    const bool cap = a.softcap > 0.0f;
     const int* table = c.table + (size_t)w.seq * c.max_blocks;
 
     // the query rows as the MMA's columns
     uint32_t qf[NT][KS][2];
-    float cs[NT][2];  // scale * 2^e of rows 2t and 2t + 1 of a tile
+    float cs[NT][2];  // scale * 2^e (log2 e) of rows 2t and 2t + 1 of a tile
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = 8 * nt + g;
@@ -211,7 +215,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       const uint32_t e = kv_row_exp(amax);
       const float down = __uint_as_float((254 - e) << 23);
-      const float up = amax < 0x7f800000u ? __uint_as_float(e << 23) * a.scale : kv_nan();
+      const float up = amax < 0x7f800000u ? __uint_as_float(e << 23) * (cap ? a.scale : a.scale * kLog2e) : kv_nan();
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
         const uint32_t* x = reinterpret_cast<const uint32_t*>(v[j]);
@@ -226,58 +230,69 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
     }
 
     float o[KS][NT][4], m[NT][2], l[NT][2];
+    float mu[NT][2];  // m, or 0 where no token has been seen: masked exponents are -inf either way
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) o[k][nt][0] = o[k][nt][1] = o[k][nt][2] = o[k][nt][3] = 0.0f;
       m[nt][0] = m[nt][1] = -INFINITY;
+      mu[nt][0] = mu[nt][1] = 0.0f;
       l[nt][0] = l[nt][1] = 0.0f;
     }
-    // the last token that rows 2t and 2t + 1 of a tile see
-    int see[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) see[nt][i] = w.held - w.rows + (8 * nt + 2 * t + i) / a.G;
-    const float two_cap = a.softcap > 0.0f ? 2.0f * kLog2e / a.softcap : 0.0f;
+    const float two_cap = cap ? 2.0f * kLog2e / a.softcap : 0.0f;
 
     // this warp's steps: first + wid, + kDecWarps, ..
     const int mine = last - first > wid ? (last - first - wid + kDecWarps - 1) / kDecWarps : 0;
     auto info = [&](int i) {  // of the warp's step i
-      StepInfo s = {0, 0.0f, 1.0f};
+      StepInfo s = {0, 0.0f, 0.0f, 1.0f};
       if (i < mine) {
         const int tok = (w.step0 + first + wid + i * kDecWarps) << 4;
         s.blk = table[tok >> c.logP];
         if (s.blk >= 0 && s.blk < c.n_blocks) {
           s.ks = c.scale[0][(size_t)s.blk * c.K + h];
-          s.vs = c.scale[1][(size_t)s.blk * c.K + h];
+          const float vs = c.scale[1][(size_t)s.blk * c.K + h];
+          s.lv = log2f(vs);
+          // a NaN comes in through the exponents of the tokens that a row sees;
+          // rows that see none have weights 0 and must not meet it here
+          s.iv = vs > 0.0f ? 1.0f / vs : 1.0f;
         } else {
           kv_raise(c, MSI_ERR_INVALID_ARG);
           s.blk = 0;
-          s.ks = s.vs = kv_nan();
+          s.ks = s.lv = kv_nan();
         }
       }
       return s;
     };
     StepInfo use = info(lane), ahead = use;  // steps 32 q + lane: those in use, those being fetched
+    // a lane's copies: 16 bytes of row r0 + 512 / D per copy
+    constexpr int CPR = D / 16, RPC = 32 / CPR;
+    uint32_t in_dst[2];
+    in_dst[0] = ring_u + dec_chunk<D>(lane / CPR, lane % CPR);
+    in_dst[1] = ring_u + dec_chunk<D>(lane / CPR + RPC, lane % CPR);
+    int st_in = 0;  // the stage that the next fetch fills
     auto fetch = [&](int i) {
       if ((i & 31) == 0 && i > 0) ahead = info(i + lane);
       const int blk = __shfl_sync(0xffffffffu, ahead.blk, i & 31);
       if (i < mine) {
         const int tok = (w.step0 + first + wid + i * kDecWarps) << 4;
-        const size_t at = (((size_t)blk * c.K + h) * c.P + (tok & (c.P - 1))) * D;
+        const size_t at = (((size_t)blk * c.K + h) * c.P + (tok & (c.P - 1))) * D + lane * 16;
         const uint8_t* kp = c.codes[0] + at;
         const uint8_t* vp = c.codes[1] + at;
-        uint8_t* dst = ring + (i % S) * SB;
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n) {  // 16 D / 512 copies of 16 bytes a lane
-          const int e = n * 32 + lane, r = e / (D / 16), ch = e % (D / 16);
-          cp_async16(dst + dec_chunk<D>(r, ch), kp + e * 16, 16);
-          cp_async16(dst + 16 * D + dec_chunk<D>(r, ch), vp + e * 16, 16);
+        for (int n = 0; n < D / 32; ++n) {  // rows n RPC on: every second copy has the first one's swizzle
+          constexpr int P2 = D == 64 ? 1 : D == 128 ? 2 : 4;  // copies after which the swizzle repeats
+          uint32_t dst;
+          if (P2 == 4) dst = ring_u + dec_chunk<D>(lane / CPR + (n & 3) * RPC, lane % CPR) + (n >> 2) * 4 * RPC * D;
+          else dst = in_dst[n & (P2 - 1)] + (n / P2) * P2 * RPC * D;
+          dst += st_in * SB;
+          copy16(dst, kp + n * 512);
+          copy16(dst + 16 * D, vp + n * 512);
         }
       }
       cp_async_commit();
+      st_in = st_in + 1 == S ? 0 : st_in + 1;
     };
+    int st = 0;  // the stage in use
 #pragma unroll 1
     for (int i = 0; i < S - 1; ++i) fetch(i);
 
@@ -290,8 +305,10 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       const int idx = first + wid + i * kDecWarps;
       const int tok0 = (w.step0 + idx) << 4;
       const float ks = __shfl_sync(0xffffffffu, use.ks, i & 31);
-      const float vs = __shfl_sync(0xffffffffu, use.vs, i & 31);
-      const uint32_t kb = ring_u + (i % S) * SB, vb = kb + 16 * D;
+      const float lv = __shfl_sync(0xffffffffu, use.lv, i & 31);
+      const float iv = __shfl_sync(0xffffffffu, use.iv, i & 31);
+      const uint32_t kb = ring_u + st * SB, vb = kb + 16 * D;
+      st = st + 1 == S ? 0 : st + 1;
 
       float sc[NT][4];
 #pragma unroll
@@ -311,21 +328,31 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       }
 
       // exponents: [0], [1] token g, [2], [3] token g + 8; rows 2t, 2t + 1
-      const float lv = __log2f(vs);
       const bool whole = tok0 + 16 <= w.held - w.rows + 1 &&
                          (a.window == 0 || tok0 > w.held - 1 - a.window);
+      if (cap) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float ck = cs[nt][q & 1] * ks;
-          if (a.softcap > 0.0f) sc[nt][q] = fmaf(kv_softcap(sc[nt][q] * ck, a.softcap, two_cap), kLog2e, lv);
-          else sc[nt][q] = fmaf(sc[nt][q], ck * kLog2e, lv);
-          if (!whole) {
+          for (int q = 0; q < 4; ++q)
+            sc[nt][q] = fmaf(kv_softcap(sc[nt][q] * (cs[nt][q & 1] * ks), a.softcap, two_cap), kLog2e, lv);
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sc[nt][q] = fmaf(sc[nt][q], cs[nt][q & 1] * ks, lv);
+      }
+      if (!whole) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
             const int tok = tok0 + g + (q >> 1) * 8;
-            if (tok > see[nt][q & 1] || (a.window > 0 && tok <= see[nt][q & 1] - a.window)) sc[nt][q] = -INFINITY;
+            // the last token that the row sees
+            const int see = w.held - w.rows + (8 * nt + 2 * t + (q & 1)) / a.G;
+            if (tok > see || (a.window > 0 && tok <= see - a.window)) sc[nt][q] = -INFINITY;
           }
-        }
+      }
       bool over = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -343,23 +370,22 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
             v = fmaxf(v, m[nt][q]);
             const float f = v == -INFINITY ? 1.0f : ex2(m[nt][q] - v);
             m[nt][q] = v;
+            mu[nt][q] = v == -INFINITY ? 0.0f : v;
             l[nt][q] *= f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) o[k][nt][q] *= f, o[k][nt][q + 2] *= f;
           }
       }
-      const float iv = __fdividef(1.0f, vs);
       uint32_t pf[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float p[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) p[q] = sc[nt][q] == -INFINITY ? 0.0f : ex2(sc[nt][q] - m[nt][q & 1]);
-        // a row that sees none of a block's tokens takes nothing from its scale, a NaN least of all
-        const float s0 = p[0] + p[2] == 0.0f ? 0.0f : (p[0] + p[2]) * iv, s1 = p[1] + p[3] == 0.0f ? 0.0f : (p[1] + p[3]) * iv;
+        for (int q = 0; q < 4; ++q) p[q] = ex2(sc[nt][q] - mu[nt][q & 1]);
+        const float s0 = (p[0] + p[2]) * iv, s1 = (p[1] + p[3]) * iv;
         l[nt][0] += s0;
         l[nt][1] += s1;
-        if (a.observe) {
+        if (OBS) {
           float v0 = s0, v1 = s1;
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) {
@@ -471,7 +497,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         if (d == 0) {
           const float l2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
           if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
-          if (a.observe) a.lse2[row * a.H + head] = l2;
+          if (OBS) a.lse2[row * a.H + head] = l2;
         }
       }
     }
@@ -480,25 +506,23 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
   }
 }
 
-// Joins the parts of the pair that begins in run x and goes on past it, row y:
+// Joins the parts of the pair that begins in run x and goes on past it, row r:
 // weights 2^(M_i - M) over the parts, in the CTAs' order within each warp and
 // warp by warp.  Bound: latency.
 constexpr int kJoinThreads = 256;
 
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int R) {
+__device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r) {
   constexpr int W = kJoinThreads / 32;
   __shared__ float s_f[1024], s_part[W][D], s_red[W];
-  grid_wait();
-  grid_release();
-  const int4 at = a.split[blockIdx.x];  // first row, rows, head, parts
-  const int r = blockIdx.y, parts = at.w;
+  const int4 at = a.split[x];  // first row, rows, head, parts
+  const int parts = at.w;
   if (r >= at.y || parts == 0) return;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const long long row = at.x + r / a.G;
   const int head = at.z * a.G + r % a.G;
   const bool failed = a.c.control[1] != 0;  // within the call
-  auto slot_of = [&](int i) { return (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)); };
+  auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
   float mi[4], li[4];  // this thread's parts: W 128 / 32 = 1,024 CTAs at most
   float top = -INFINITY;
 #pragma unroll
@@ -560,35 +584,50 @@ __global__ void __launch_bounds__(kJoinThreads) kv_join_kernel(KvAttnArgs a, int
   if (tid == 0) {
     const float l2 = failed ? kv_nan() : sum == 0.0f ? -INFINITY : top + log2f(sum);
     if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
-    if (a.observe) a.lse2[row * a.H + head] = l2;
   }
 }
 
 // Attention weight of each block: over the heads, its 16-token steps and the
 // rows, 2^(step's log2 sum - row's log2 sum), a lane a term, lanes added in one
-// order.  A warp takes 8 blocks in a row.  Bound: latency.
-constexpr int kObsThreads = 256, kObsBlocks = 8;
+// order.  A warp takes 8 blocks in a row.  Does not wait for the joins: the
+// sums of a split pair's rows are put together here from its parts as well.
+// Bound: latency.
+constexpr int kObsBlocks = 8;
 
-__global__ void __launch_bounds__(kObsThreads) kv_observe_kernel(KvAttnArgs a, int R) {
-  extern __shared__ float s_top[];  // [K][R] log2 of the rows' sums; -inf: a row that is none
+__device__ __forceinline__ void kv_observe(const KvAttnArgs& a, int R, int warps, int b, int y, int ny, float* s_top) {
+  // s_top: [K][R] log2 of the rows' sums; -inf: a row that is none
   const KvCache& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, b = blockIdx.x;
-  grid_wait();
-  grid_release();
-  if (c.control[1] != 0) return;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const KvWork w = kv_work(a, b);
-  if (w.steps == 0) return;
+  const long long pre = a.item_pre[b], total = a.item_pre[a.n];
+  if (c.control[1] != 0 || w.steps == 0) return;
   const int per = c.P / 16, j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
-  if (j0 + (int)blockIdx.y * (kObsThreads / 32) * kObsBlocks >= j1) return;
+  if (j0 + y * (kJoinThreads / 32) * kObsBlocks >= j1) return;
   const int n = w.rows * a.G;
-  const long long pre = a.item_pre[b];
-  for (int i = tid; i < c.K * R; i += kObsThreads) {
+  const int ctas = kv_ctas(total, a.ctas, warps);
+  for (int i = tid; i < c.K * R; i += kJoinThreads) {
     const int h = i / R, r = i - h * R;
-    s_top[i] = r < n ? a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G] : -INFINITY;
+    float top = -INFINITY;
+    if (r < n) {
+      const long long u0 = pre + (long long)h * w.steps;
+      const int c0 = kv_owner(total, ctas, u0), c1 = kv_owner(total, ctas, u0 + w.steps - 1);
+      if (c0 == c1) {
+        top = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
+      } else {
+        float sum = 0.0f;
+        for (int x = c0; x <= c1; ++x) {
+          const float* ml = a.part_ml + (size_t)(2 * x + (x == c0 ? 1 : 0)) * 2 * R + r;
+          const float m = ml[0], l = ml[R];
+          if (m > top) sum = top == -INFINITY ? 0.0f : sum * ex2(top - m), top = m;
+          sum += m == -INFINITY ? l : l * ex2(m - top);
+        }
+        top = sum == 0.0f ? -INFINITY : top + log2f(sum);
+      }
+    }
+    s_top[i] = top;
   }
   __syncthreads();
-  for (int j = j0 + (blockIdx.y * (kObsThreads / 32) + wid) * kObsBlocks; j < j1;
-       j += gridDim.y * (kObsThreads / 32) * kObsBlocks) {
+  for (int j = j0 + (y * (kJoinThreads / 32) + wid) * kObsBlocks; j < j1; j += ny * (kJoinThreads / 32) * kObsBlocks) {
     float mine = 0.0f;
 #pragma unroll
     for (int k = 0; k < kObsBlocks; ++k) {
@@ -613,31 +652,43 @@ __global__ void __launch_bounds__(kObsThreads) kv_observe_kernel(KvAttnArgs a, i
   }
 }
 
-template <int D, int NT, int FMT>
-cudaError_t decode_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
+// The joins (`joins` CTAs: runs by rows), then the block weights (`ny` CTAs a
+// sequence).
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, int R, int warps, int joins, int ny) {
+  extern __shared__ float s_top[];
+  grid_wait();
+  grid_release();
+  const int x = blockIdx.x;
+  if (x < joins) kv_join<D>(a, R, x % a.ctas, x / a.ctas);
+  else kv_observe(a, R, warps, (x - joins) / ny, (x - joins) % ny, ny, s_top);
+}
+
+template <int D, int NT, int FMT, bool OBS>
+cudaError_t decode_as(const KvAttnArgs& a, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   constexpr int W = dec_warps(D, NT), ring = W * dec_stages(D, NT) * dec_stage_bytes(D);
   static_assert(W * 8 * NT * D * 4 <= ring, "the parts fit the rings");
-  cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT>, ring + (kKvMaxSeqs + 1) * (int)sizeof(long long), done);
+  cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT, OBS>, ring + (kKvMaxSeqs + 1) * (int)sizeof(long long), done);
   if (e != cudaSuccess) return e;
-  e = launch_after(false, kv_decode_kernel<D, NT, FMT>, dim3(a.ctas), dim3(32 * W), ring + (a.n + 1) * sizeof(long long), s, a);
+  e = launch_after(false, kv_decode_kernel<D, NT, FMT, OBS>, dim3(a.ctas), dim3(32 * W),
+                   ring + (a.n + 1) * sizeof(long long), s, a);
   if (e != cudaSuccess) return e;
-  e = launch_after(true, kv_join_kernel<D>, dim3(a.ctas, a.max_rows * a.G), dim3(kJoinThreads), 0, s, a, 8 * NT);
-  if (e != cudaSuccess) return e;
-  *launches = 2;
-  if (a.observe) {
-    const int per = kObsThreads / 32 * kObsBlocks;
-    const int most = min(a.c.max_blocks, a.c.n_blocks);
-    e = launch_after(true, kv_observe_kernel, dim3(a.n, min((most + per - 1) / per, 64)), dim3(kObsThreads),
-                     a.c.K * 8 * NT * sizeof(float), s, a, 8 * NT);
-    *launches = 3;
-  }
-  return e;
+  const int joins = a.ctas * a.max_rows * a.G;
+  const int per = kJoinThreads / 32 * kObsBlocks;
+  const int ny = min((min(a.c.max_blocks, a.c.n_blocks) + per - 1) / per, 64);
+  return launch_after(true, kv_finish_kernel<D>, dim3(joins + (OBS ? a.n * ny : 0)), dim3(kJoinThreads),
+                      OBS ? a.c.K * 8 * NT * sizeof(float) : 0, s, a, 8 * NT, W, joins, ny);
+}
+
+template <int D, int NT, int FMT>
+cudaError_t decode_opt(const KvAttnArgs& a, cudaStream_t s) {
+  return a.observe ? decode_as<D, NT, FMT, true>(a, s) : decode_as<D, NT, FMT, false>(a, s);
 }
 
 template <int D, int NT>
-cudaError_t decode_fmt(const KvAttnArgs& a, int* launches, cudaStream_t s) {
-  return a.c.fmt == MSI_KV_Q8 ? decode_as<D, NT, MSI_KV_Q8>(a, launches, s) : decode_as<D, NT, MSI_KV_E4M3>(a, launches, s);
+cudaError_t decode_fmt(const KvAttnArgs& a, cudaStream_t s) {
+  return a.c.fmt == MSI_KV_Q8 ? decode_opt<D, NT, MSI_KV_Q8>(a, s) : decode_opt<D, NT, MSI_KV_E4M3>(a, s);
 }
 
 }  // namespace
@@ -648,9 +699,10 @@ int kv_decode_tiles(int rows, int D) {
 
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   const int nt = kv_decode_tiles(a.max_rows * a.G, a.c.D);
-  if (a.c.D == 64) return nt == 1 ? decode_fmt<64, 1>(a, launches, s) : nt == 2 ? decode_fmt<64, 2>(a, launches, s) : decode_fmt<64, 4>(a, launches, s);
-  if (a.c.D == 128) return nt == 1 ? decode_fmt<128, 1>(a, launches, s) : nt == 2 ? decode_fmt<128, 2>(a, launches, s) : decode_fmt<128, 4>(a, launches, s);
-  return nt == 1 ? decode_fmt<256, 1>(a, launches, s) : decode_fmt<256, 2>(a, launches, s);
+  *launches = 2;
+  if (a.c.D == 64) return nt == 1 ? decode_fmt<64, 1>(a, s) : nt == 2 ? decode_fmt<64, 2>(a, s) : decode_fmt<64, 4>(a, s);
+  if (a.c.D == 128) return nt == 1 ? decode_fmt<128, 1>(a, s) : nt == 2 ? decode_fmt<128, 2>(a, s) : decode_fmt<128, 4>(a, s);
+  return nt == 1 ? decode_fmt<256, 1>(a, s) : decode_fmt<256, 2>(a, s);
 }
 
 }  // namespace msi
