@@ -100,16 +100,16 @@ __device__ __forceinline__ float kv_nan() { return __int_as_float(0x7fc00000); }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Equal runs of `total` units: where CTA i's begins, and the CTA whose run holds unit u.
-__device__ __forceinline__ long long kv_begin(long long total, int ctas, int i) { return total * i / ctas; }
-// the CTA whose run holds step u
-__device__ __forceinline__ int kv_owner(long long total, int ctas, long long u) {
-  int i = (int)(u * ctas / total);
-  while (kv_begin(total, ctas, i + 1) <= u) ++i;
-  while (kv_begin(total, ctas, i) > u) --i;
-  return i;
-}
-
+// `total` units in `ctas` runs of nearly equal length, the longer ones spread
+// evenly (so that equal items, cut by a multiple of their number, are cut alike).
+struct KvRuns {
+  long long total;
+  int ctas;
+  // where run i begins
+  __device__ __forceinline__ long long begin(int i) const { return total * i / ctas; }
+  // the run that holds unit u: the last i with total i < (u + 1) ctas
+  __device__ __forceinline__ int owner(long long u) const { return (int)(((u + 1) * ctas - 1) / total); }
+};
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);

@@ -167,8 +167,9 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
   const long long total = s_total;
   const int ctas = (int)min((long long)a.ctas, max(1LL, total / (kItemCost + 1)));
   // where each CTA's run begins
+  const KvRuns runs = {total, ctas};
   for (int x = tid; x < ctas && items > 0; x += kPlanThreads) {
-    const long long u = kv_begin(total, ctas, x);
+    const long long u = runs.begin(x);
     int lo = 0, hi = items;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -201,8 +202,9 @@ struct PartWalk {
     const int items = a.plan[0], ctas = a.plan[2];
     item = a.plan[4 + cta];
     const long long total = a.item_pre[items];
-    u = kv_begin(total, ctas, cta);
-    end = kv_begin(total, ctas, cta + 1);
+    const KvRuns runs = {total, ctas};
+    u = runs.begin(cta);
+    end = runs.begin(cta + 1);
   }
   __device__ __forceinline__ bool next(const KvAttnArgs& a, Part& p) {
     while (u < end) {
@@ -811,12 +813,13 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   const int ctas = a.plan[2];
   if ((int)blockIdx.x + 1 >= ctas) return;
   const long long total = a.item_pre[a.plan[0]];
-  const long long begin = kv_begin(total, ctas, blockIdx.x), end = kv_begin(total, ctas, blockIdx.x + 1);
+  const KvRuns runs = {total, ctas};
+  const long long begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
   // the item that the next run begins with, if it has tiles in this one
   const int item = a.plan[4 + blockIdx.x + 1];
   const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
   if (p0 < begin || p0 >= end) return;
-  const int parts = kv_owner(total, ctas, p1 - 1) - blockIdx.x + 1;
+  const int parts = runs.owner(p1 - 1) - blockIdx.x + 1;
   const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
   const int tr = blockIdx.y * kChunkJoinRows + (threadIdx.x & 31), r = it.y * C::ROWS + tr;
   if (r >= w.z * a.G) return;

@@ -77,8 +77,8 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
 
 // CTAs that take part.
 __device__ __forceinline__ int kv_ctas(long long total, int ctas, int warps) {
-  const long long most = (total + warps - 1) / warps;  // a step a warp at least
-  return (int)min((long long)ctas, max(most, 1LL));
+  // a step a warp at least
+  return total >= (long long)ctas * warps ? ctas : max(1, ((int)total + warps - 1) / warps);
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
     return;
   }
   const int ctas = kv_ctas(total, a.ctas, kDecWarps);
+  const KvRuns runs = {total, ctas};
 
   // sequences that hold nothing
   for (int b = blockIdx.x; b < a.n; b += gridDim.x) {
@@ -168,8 +169,8 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
 
   uint8_t* ring = smem + wid * RING;
   const uint32_t ring_u = smem_u32(ring);
-  long long u = kv_begin(total, ctas, blockIdx.x);
-  const long long u_end = kv_begin(total, ctas, blockIdx.x + 1);
+  long long u = runs.begin(blockIdx.x);
+  const long long u_end = runs.begin(blockIdx.x + 1);
   int b = 0;
   {
     int hi = a.n;
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * R + r) * D + d) = acc;
         if (d == 0) a.part_ml[(size_t)slot * 2 * R + r] = top, a.part_ml[(size_t)slot * 2 * R + R + r] = sum;
         if (e == 0 && first == 0)
-          a.split[blockIdx.x] = make_int4(w.row0, n_rows, h, kv_owner(total, ctas, item0 + w.steps - 1) - blockIdx.x + 1);
+          a.split[blockIdx.x] = make_int4(w.row0, n_rows, h, runs.owner(item0 + w.steps - 1) - blockIdx.x + 1);
       } else {
         const long long row = w.row0 + r / a.G;
         const int head = h * a.G + r % a.G;
@@ -587,81 +588,98 @@ __device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r
   }
 }
 
-// Attention weight of each block: over the heads, its 16-token steps and the
-// rows, 2^(step's log2 sum - row's log2 sum), a lane a term, lanes added in one
-// order.  A warp takes 8 blocks in a row.  Does not wait for the joins: the
-// sums of a split pair's rows are put together here from its parts as well.
-// Bound: latency.
-constexpr int kObsBlocks = 8;
-
-__device__ __forceinline__ void kv_observe(const KvAttnArgs& a, int R, int warps, int b, int y, int ny, float* s_top) {
-  // s_top: [K][R] log2 of the rows' sums; -inf: a row that is none
+// Attention weight of each block: over the heads, its 16-token granules and the
+// rows, 2^(granule's log2 sum - row's log2 sum).  The granules of neighbouring
+// blocks lie together, so a lane takes four rows of one granule for every head,
+// and a warp the blocks that 128 of these sums hold (or one block, in passes).
+// Lanes are added in one order.  `warps` warps, of which this is the wid-th.
+// s_top: [K][R] log2 of the rows' sums; -inf: a row that is none.
+__device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w, long long pre, int R, const float* s_top, int wid,
+                                           int warps) {
   const KvCache& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const KvWork w = kv_work(a, b);
-  const long long pre = a.item_pre[b], total = a.item_pre[a.n];
-  if (c.control[1] != 0 || w.steps == 0) return;
-  const int per = c.P / 16, j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
-  if (j0 + y * (kJoinThreads / 32) * kObsBlocks >= j1) return;
-  const int n = w.rows * a.G;
-  const int ctas = kv_ctas(total, a.ctas, warps);
-  for (int i = tid; i < c.K * R; i += kJoinThreads) {
-    const int h = i / R, r = i - h * R;
-    float top = -INFINITY;
-    if (r < n) {
-      const long long u0 = pre + (long long)h * w.steps;
-      const int c0 = kv_owner(total, ctas, u0), c1 = kv_owner(total, ctas, u0 + w.steps - 1);
-      if (c0 == c1) {
-        top = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
-      } else {
-        float sum = 0.0f;
-        for (int x = c0; x <= c1; ++x) {
-          const float* ml = a.part_ml + (size_t)(2 * x + (x == c0 ? 1 : 0)) * 2 * R + r;
-          const float m = ml[0], l = ml[R];
-          if (m > top) sum = top == -INFINITY ? 0.0f : sum * ex2(top - m), top = m;
-          sum += m == -INFINITY ? l : l * ex2(m - top);
-        }
-        top = sum == 0.0f ? -INFINITY : top + log2f(sum);
+  const int lane = threadIdx.x & 31;
+  const int per = c.P / 16, sums = per * R;                // of a block and head: 8 .. 256, a power of two
+  const int nb = sums >= 128 ? 1 : 128 / sums;             // blocks of a warp's turn
+  const int lanes = sums >= 128 ? 32 : sums / 4;           // lanes of a block
+  const int j0 = w.step0 / per, j1 = (w.held + c.P - 1) >> c.logP;
+  for (int j = j0 + wid * nb; j < j1; j += warps * nb) {
+    const int mine = j + lane / lanes;
+    const bool writes = (lane & (lanes - 1)) == 0 && mine < j1;
+    const int id = writes ? c.table[(size_t)w.seq * c.max_blocks + mine] : -1;
+    const bool there = id >= 0 && id < c.n_blocks;
+    const float had = there ? c.weight[id] : 0.0f;
+    float v = 0.0f;
+    for (int f = lane * 4; f < nb * sums; f += 128) {
+      const int step = j * per + f / R - w.step0, r = f & (R - 1);  // R is a power of two
+      if (step < 0 || step >= w.steps) continue;
+      const float* p = a.step_lse + (pre + step) * R + r;
+#pragma unroll 4
+      for (int h = 0; h < c.K; ++h) {
+        const float4 x = *reinterpret_cast<const float4*>(p + (long long)h * w.steps * R);
+        const float4 t = *reinterpret_cast<const float4*>(s_top + h * R + r);
+        if (t.x != -INFINITY) v += ex2(x.x - t.x);
+        if (t.y != -INFINITY) v += ex2(x.y - t.y);
+        if (t.z != -INFINITY) v += ex2(x.z - t.z);
+        if (t.w != -INFINITY) v += ex2(x.w - t.w);
       }
     }
-    s_top[i] = top;
-  }
-  __syncthreads();
-  for (int j = j0 + (y * (kJoinThreads / 32) + wid) * kObsBlocks; j < j1; j += ny * (kJoinThreads / 32) * kObsBlocks) {
-    float mine = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kObsBlocks; ++k) {
-      // of block j + k: steps s0 .. s1 - 1 of the pair
-      const int s0 = max(w.step0, (j + k) * per) - w.step0, s1 = min(w.step0 + w.steps, (j + k + 1) * per) - w.step0;
-      const int one = (s1 - s0) * R;
-      float v = 0.0f;
-      for (int e = lane; e < c.K * one; e += 32) {
-        const int h = e / one, f = e - h * one;
-        const float top = s_top[h * R + (f & (R - 1))];  // R is a power of two
-        const float x = a.step_lse[(pre + (long long)h * w.steps + s0) * R + f];
-        if (top != -INFINITY) v += ex2(x - top);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane == k) mine = v;
-    }
-    if (lane < kObsBlocks && j + lane < j1) {
-      const int id = c.table[(size_t)w.seq * c.max_blocks + j + lane];
-      if (id >= 0 && id < c.n_blocks) c.weight[id] += mine;
-    }
+    __syncwarp();
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (there) c.weight[id] = had + v;
   }
 }
 
-// The joins (`joins` CTAs: runs by rows), then the block weights (`ny` CTAs a
-// sequence).
+// The joins as `joins` CTAs (runs by
+// rows), then the block weights (`ny` CTAs a sequence), which put the sums of a
+// split pair's rows together from its parts as well and so need not wait for the
+// joins.
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, int R, int warps, int joins, int ny) {
-  extern __shared__ float s_top[];
+  extern __shared__ __align__(16) float s_top[];
   grid_wait();
   grid_release();
   const int x = blockIdx.x;
-  if (x < joins) kv_join<D>(a, R, x % a.ctas, x / a.ctas);
-  else kv_observe(a, R, warps, (x - joins) / ny, (x - joins) % ny, ny, s_top);
+  if (x < joins) {
+    kv_join<D>(a, R, x % a.ctas, x / a.ctas);
+    return;
+  }
+  const KvCache& c = a.c;
+  const int b = (x - joins) / ny, y = (x - joins) % ny;
+  const KvWork w = kv_work(a, b);
+  const long long pre = a.item_pre[b], total = a.item_pre[a.n];
+  if (c.control[1] != 0 || w.steps == 0) return;
+  const int n = w.rows * a.G;
+  const KvRuns runs = {total, kv_ctas(total, a.ctas, warps)};
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  for (int i = wid; i < c.K * R; i += kJoinThreads / 32) {  // a warp a row
+    const int h = i / R, r = i - h * R;
+    float l2 = -INFINITY;
+    if (r < n) {
+      const long long u0 = pre + (long long)h * w.steps;
+      const int c0 = runs.owner(u0), c1 = runs.owner(u0 + w.steps - 1);
+      if (c0 == c1) {
+        l2 = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
+      } else {
+        float top = -INFINITY, sum = 0.0f;
+        for (int x = c0 + lane; x <= c1; x += 32) {
+          const float* ml = a.part_ml + (size_t)(2 * x + (x == c0 ? 1 : 0)) * 2 * R + r;
+          const float m = ml[0], l = ml[R];
+          if (m > top) sum = top == -INFINITY ? sum : sum * ex2(top - m), top = m;
+          sum += m == -INFINITY ? l : l * ex2(m - top);
+        }
+        float all = top;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+        if (top != -INFINITY) sum *= ex2(top - all);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        l2 = sum == 0.0f ? -INFINITY : all + log2f(sum);
+      }
+    }
+    if (lane == 0) s_top[i] = l2;
+  }
+  __syncthreads();
+  kv_weights(a, w, pre, R, s_top, y * (kJoinThreads / 32) + wid, ny * (kJoinThreads / 32));
 }
 
 template <int D, int NT, int FMT, bool OBS>
@@ -675,7 +693,8 @@ cudaError_t decode_as(const KvAttnArgs& a, cudaStream_t s) {
                    ring + (a.n + 1) * sizeof(long long), s, a);
   if (e != cudaSuccess) return e;
   const int joins = a.ctas * a.max_rows * a.G;
-  const int per = kJoinThreads / 32 * kObsBlocks;
+  // a turn of every warp of a CTA; longer tables take several
+  const int sums = a.c.P / 16 * 8 * NT, per = kJoinThreads / 32 * (sums >= 128 ? 1 : 128 / sums);
   const int ny = min((min(a.c.max_blocks, a.c.n_blocks) + per - 1) / per, 64);
   return launch_after(true, kv_finish_kernel<D>, dim3(joins + (OBS ? a.n * ny : 0)), dim3(kJoinThreads),
                       OBS ? a.c.K * 8 * NT * sizeof(float) : 0, s, a, 8 * NT, W, joins, ny);
