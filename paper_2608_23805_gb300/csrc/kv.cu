@@ -61,18 +61,46 @@ __device__ __forceinline__ KvSpan kv_span(const KvAppendArgs& a, int b) {
   return s;
 }
 
+__device__ __forceinline__ unsigned max_u16x2(unsigned x, unsigned y) {
+  unsigned r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+
+// Four bf16 times inv, rounded to whole numbers (ties to even) plus 128, as
+// bytes: the sum with 1.5 2^23 + 128 has a spacing of 1, its low byte is the code.
+__device__ __forceinline__ uint32_t round_q8(uint32_t a, uint32_t b, float inv) {
+  constexpr float kMagic = 12583040.0f;
+  const uint32_t r0 = __float_as_uint(__fadd_rn(__fmul_rn(bf16_lo(a), inv), kMagic));
+  const uint32_t r1 = __float_as_uint(__fadd_rn(__fmul_rn(bf16_hi(a), inv), kMagic));
+  const uint32_t r2 = __float_as_uint(__fadd_rn(__fmul_rn(bf16_lo(b), inv), kMagic));
+  const uint32_t r3 = __float_as_uint(__fadd_rn(__fmul_rn(bf16_hi(b), inv), kMagic));
+  return __byte_perm(__byte_perm(r0, r1, 0x0040), __byte_perm(r2, r3, 0x0040), 0x5410);
+}
+
+// Four bf16 times inv as e4m3 bytes.
+__device__ __forceinline__ uint32_t round_e4m3(uint32_t a, uint32_t b, float inv) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fmul_rn(bf16_hi(a), inv)), "f"(__fmul_rn(bf16_lo(a), inv)));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fmul_rn(bf16_hi(b), inv)), "f"(__fmul_rn(bf16_lo(b), inv)));
+  return (uint32_t)lo | (uint32_t)hi << 16;
+}
+
 // A block of one head, keys or values, is a task: rounded in one pass over its
 // rows, which stay in registers between the maximum and the rounding.  A CTA
 // takes every gridDim-th task, so that the bookkeeping is paid for once in
 // several blocks.  Bound: memory (16-bit rows in, codes out) for prompts,
 // latency for single tokens.
+constexpr int append_threads(int vpt) { return vpt <= 4 ? 1024 : 512; }  // of an SM, by the registers a thread takes
+
 template <int THREADS, int VPT>
-__global__ void __launch_bounds__(THREADS, (VPT <= 4 ? 1024 : 512) / THREADS) kv_append_kernel(KvAppendArgs a) {
+__global__ void __launch_bounds__(THREADS, append_threads(VPT) / THREADS) kv_append_kernel(KvAppendArgs a) {
   const KvCache& c = a.c;
   __shared__ int s_scan[32];
   __shared__ unsigned s_seen[kKvMaxSeqs / 32];
   __shared__ int s_blocks[kKvMaxSeqs + 1], s_add[kKvMaxSeqs];  // changing and new blocks before each entry's
-  __shared__ int s_bad, s_tot[3];
+  __shared__ int s_bad, s_tot[3], s_at[2];  // s_at: the task's block in the table and in the pool
+  __shared__ KvSpan s_span;
   __shared__ unsigned s_max[THREADS / 32];
   __shared__ unsigned s_last;
   const int tid = threadIdx.x;
@@ -126,39 +154,44 @@ __global__ void __launch_bounds__(THREADS, (VPT <= 4 ? 1024 : 512) / THREADS) kv
   const int tasks = go ? s_tot[0] * 2 * c.K : 0;
   for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
     const int block = task / (2 * c.K), h = (task - block * 2 * c.K) >> 1, w = task & 1;
-    int b = 0, hi = a.n;  // the entry whose blocks hold it
-    while (hi - b > 1) {
-      const int mid = (b + hi) >> 1;
-      if (s_blocks[mid] <= block) b = mid; else hi = mid;
+    if (tid == 0) {
+      int b = 0, hi = a.n;  // the entry whose blocks hold it
+      while (hi - b > 1) {
+        const int mid = (b + hi) >> 1;
+        if (s_blocks[mid] <= block) b = mid; else hi = mid;
+      }
+      s_span = kv_span(a, b);
+      const int j = (s_span.start >> c.logP) + block - s_blocks[b];
+      s_at[0] = j;
+      s_at[1] = j < s_span.had ? c.table[(size_t)s_span.seq * c.max_blocks + j]
+                               : c.free_ids[n_free - 1 - s_add[b] - (j - s_span.had)];
     }
-    const KvSpan s = kv_span(a, b);
-    const int j = (s.start >> c.logP) + block - s_blocks[b];
-    const int id = j < s.had ? c.table[(size_t)s.seq * c.max_blocks + j] : c.free_ids[n_free - 1 - s_add[b] - (j - s.had)];
+    __syncthreads();
+    const KvSpan s = s_span;
+    const int j = s_at[0], id = s_at[1];
     const bool id_ok = id >= 0 && id < c.n_blocks;
     const __nv_bfloat16* x = a.x[w] + (size_t)h * c.D;
     __nv_bfloat16* ring = c.recent + (((size_t)s.seq * 2 + w) * c.K + h) * (size_t)(2 * c.P) * c.D;
     const int log_vpr = c.D == 64 ? 3 : c.D == 128 ? 4 : 5, vpr = 1 << log_vpr;  // 16-byte vectors a row
     const int mask2 = 2 * c.P - 1;
     uint4 v[VPT];
-    unsigned amax = 0;
+    const int dc0 = (tid & (vpr - 1)) * 8, o0 = tid >> log_vpr, ostep = THREADS >> log_vpr;  // a thread keeps its columns
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int e = i * THREADS + tid, o = e >> log_vpr, dc = (e & (vpr - 1)) * 8;
-      const int tok = (j << c.logP) + o;
+      const int tok = (j << c.logP) + o0 + i * ostep;
       v[i] = make_uint4(0, 0, 0, 0);
       if (tok < s.start)
-        v[i] = *reinterpret_cast<const uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc);
+        v[i] = *reinterpret_cast<const uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc0);
       else if (tok < s.end)
-        v[i] = *reinterpret_cast<const uint4*>(x + (size_t)(s.row0 + tok - s.start) * a.stride + dc);
+        v[i] = *reinterpret_cast<const uint4*>(x + (size_t)(s.row0 + tok - s.start) * a.stride + dc0);
     }
+    unsigned both = 0;  // as whole numbers, two at a time: an infinity or NaN is above every number
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const uint32_t* u = reinterpret_cast<const uint32_t*>(&v[i]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)  // as whole numbers: an infinity or NaN is above every number
-        amax = max(amax, max((u[q] << 16) & 0x7fffffffu, u[q] & 0x7fff0000u));
+      both = max_u16x2(both, max_u16x2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu));
+      both = max_u16x2(both, max_u16x2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
     }
-    amax = __reduce_max_sync(0xffffffffu, amax);
+    unsigned amax = __reduce_max_sync(0xffffffffu, max(both << 16, both & 0xffff0000u));
     if ((tid & 31) == 0) s_max[tid >> 5] = amax;
     __syncthreads();
 #pragma unroll
@@ -169,28 +202,13 @@ __global__ void __launch_bounds__(THREADS, (VPT <= 4 ? 1024 : 512) / THREADS) kv
     const float inv = __fdiv_rn(top, am);
     const float scale = __fmul_rn(am, c.fmt == MSI_KV_Q8 ? 1.0f / 127.0f : 1.0f / 448.0f);
     if (id_ok) {
-      uint8_t* dst = c.codes[w] + ((size_t)id * c.K + h) * (size_t)c.P * c.D;
+      uint8_t* dst = c.codes[w] + ((size_t)id * c.K + h) * (size_t)c.P * c.D + o0 * c.D + dc0;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
-        const uint32_t* u = reinterpret_cast<const uint32_t*>(&v[i]);
-        uint32_t r[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          float f[4] = {bf16_lo(u[2 * q]), bf16_hi(u[2 * q]), bf16_lo(u[2 * q + 1]), bf16_hi(u[2 * q + 1])};
-#pragma unroll
-          for (int m = 0; m < 4; ++m) f[m] = finite ? __fmul_rn(f[m], inv) : 0.0f;
-          if (c.fmt == MSI_KV_Q8) {
-            r[q] = 0;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) r[q] |= (uint32_t)(__float2int_rn(f[m]) + 128) << (8 * m);
-          } else {
-            uint16_t lo, hi;
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(f[1]), "f"(f[0]));
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(f[3]), "f"(f[2]));
-            r[q] = (uint32_t)lo | (uint32_t)hi << 16;
-          }
-        }
-        *reinterpret_cast<uint2*>(dst + (size_t)(i * THREADS + tid) * 8) = make_uint2(r[0], r[1]);
+        const uint4 q = finite ? v[i] : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint2*>(dst + (size_t)i * ostep * c.D) =
+            c.fmt == MSI_KV_Q8 ? make_uint2(round_q8(q.x, q.y, inv), round_q8(q.z, q.w, inv))
+                               : make_uint2(round_e4m3(q.x, q.y, inv), round_e4m3(q.z, q.w, inv));
       }
       if (tid == 0) {
         c.scale[w][(size_t)id * c.K + h] = finite ? scale : kv_nan();
@@ -212,10 +230,9 @@ __global__ void __launch_bounds__(THREADS, (VPT <= 4 ? 1024 : 512) / THREADS) kv
       if (j >= jl - 1 && !(rides && j > j0 && ((j - j0) & 1) == 0)) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-          const int e = i * THREADS + tid, o = e >> log_vpr, dc = (e & (vpr - 1)) * 8;
-          const int tok = (j << c.logP) + o;
+          const int tok = (j << c.logP) + o0 + i * ostep;
           if (tok >= s.start && tok < s.end)
-            *reinterpret_cast<uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc) = v[i];
+            *reinterpret_cast<uint4*>(ring + (size_t)((tok + s.shift) & mask2) * c.D + dc0) = v[i];
         }
       }
       const int jm = ((jl - j0) & 1) == 0 ? jl : jl - 1;
@@ -262,7 +279,7 @@ template <int THREADS, int VPT>
 cudaError_t append_as(const KvAppendArgs& a, cudaStream_t s) {
   // each sequence changes at most (rows - 1) / P + 2 blocks
   const long long tasks = ((long long)a.n_rows / a.c.P + 2LL * a.n) * 2 * a.c.K;
-  const long long most = (long long)a.sms * (1536 / THREADS);
+  const long long most = (long long)a.sms * (append_threads(VPT) / THREADS);  // all resident
   kv_append_kernel<THREADS, VPT><<<(unsigned)(tasks < most ? tasks : most), THREADS, 0, s>>>(a);
   return cudaGetLastError();
 }
@@ -515,36 +532,39 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(KvReadArgs a, int
     }
   }
   __syncthreads();
-  const int per_head = c.D >> 4, per_row = c.K * per_head;
+  // `group` lanes a row (a power of two), 16 codes a lane and turn
+  const int log_ph = c.D == 64 ? 2 : c.D == 128 ? 3 : 4, per_row = c.K << log_ph, both = 2 * per_row;
   const int rows = min(per, a.n_rows - row0);
+  const int group = both >= 32 ? 32 : 1 << (31 - __clz(both));
+  const int lane = tid & (group - 1);
 #pragma unroll 4
-  for (int e = tid; e < 2 * rows * per_row; e += kReadThreads) {
-    const int w = e >= rows * per_row;
-    const int f = e - w * rows * per_row;
-    const int r = f / per_row, g = f - r * per_row, h = g / per_head, dc = (g - h * per_head) * 16;
+  for (int r = tid / group; r < rows; r += kReadThreads / group) {
     const long long at = s_at[r];
-    uint32_t o[8];
-    if (at < 0) {
+    for (int e = lane; e < both; e += group) {
+      const int w = e >= per_row, f = e - w * per_row, h = f >> log_ph, dc = (f - (h << log_ph)) * 16;
+      uint32_t o[8];
+      if (at < 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = 0x7fc07fc0u;
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(c.codes[w] + at + (size_t)h * c.P * c.D + dc);
-      const float s = c.scale[w][(size_t)s_id[r] * c.K + h];
-      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < 8; ++i) o[i] = 0x7fc07fc0u;
+      } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(c.codes[w] + at + (size_t)h * c.P * c.D + dc);
+        const float s = c.scale[w][(size_t)s_id[r] * c.K + h];
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t p, q;
-        if (c.fmt == MSI_KV_Q8) p = kv_f16x2<MSI_KV_Q8, false>(u[i]), q = kv_f16x2<MSI_KV_Q8, true>(u[i]);
-        else p = kv_f16x2<MSI_KV_E4M3, false>(u[i]), q = kv_f16x2<MSI_KV_E4M3, true>(u[i]);
-        const float2 x = __half22float2(*reinterpret_cast<__half2*>(&p));
-        const float2 y = __half22float2(*reinterpret_cast<__half2*>(&q));
-        o[2 * i] = pack_bf16x2(x.x * s, x.y * s);
-        o[2 * i + 1] = pack_bf16x2(y.x * s, y.y * s);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p, q;
+          if (c.fmt == MSI_KV_Q8) p = kv_f16x2<MSI_KV_Q8, false>(u[i]), q = kv_f16x2<MSI_KV_Q8, true>(u[i]);
+          else p = kv_f16x2<MSI_KV_E4M3, false>(u[i]), q = kv_f16x2<MSI_KV_E4M3, true>(u[i]);
+          const float2 x = __half22float2(*reinterpret_cast<__half2*>(&p));
+          const float2 y = __half22float2(*reinterpret_cast<__half2*>(&q));
+          o[2 * i] = pack_bf16x2(x.x * s, x.y * s);
+          o[2 * i + 1] = pack_bf16x2(y.x * s, y.y * s);
+        }
       }
+      uint4* dst = reinterpret_cast<uint4*>(a.out[w] + ((size_t)(row0 + r) * c.K + h) * c.D + dc);
+      dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
     }
-    uint4* dst = reinterpret_cast<uint4*>(a.out[w] + ((size_t)(row0 + r) * c.K + h) * c.D + dc);
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
