@@ -696,7 +696,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
     a.item_pre = reinterpret_cast<long long*>(take(((size_t)a.n + 1) * sizeof(long long)));
     a.lse2 = reinterpret_cast<float*>(take((size_t)a.n_rows * a.H * 4));
     // no block belongs to two sequences: the pool bounds the steps
-    a.max_steps = ((long long)c.n_blocks * (c.P / 16)) * c.K;
+    a.max_steps = ((long long)c.n_blocks * (c.P / 16) + (long long)a.n * kv_decode_pair_cost()) * c.K;
     a.step_lse = reinterpret_cast<float*>(take((size_t)a.max_steps * rows * 4));
   }
   *bytes = at;

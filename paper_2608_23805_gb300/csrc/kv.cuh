@@ -86,6 +86,7 @@ cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s);
 cudaError_t launch_kv_init(const KvCache& c, cudaStream_t s);
 // Decode form: rows of one sequence and key-value head (its part of the query
 // heads) as columns of the MMA.
+int kv_decode_pair_cost();               // units of work that a pair is counted beside its steps
 int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4), 0: not in decode form
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s);
 // Chunk form: rows of one sequence and key-value head in tiles of the MMA's rows.

@@ -36,6 +36,9 @@ constexpr float kLazy = 8.0f;  // P may reach 2^8
 // Warps of a CTA, by the registers that a warp's outputs and queries take
 // (D x 8 NT of each): the more the better hidden are a step's latencies.
 __host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 16 : 8; }
+// What a pair costs a CTA beside its steps (queries, first loads, the warps'
+// sums), in steps.
+constexpr int kPairCost = 8;
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
 // Stages of a warp's ring: 192 KB a CTA, at most 8.
 __host__ __device__ constexpr int dec_stages(int D, int NT) {
@@ -43,7 +46,10 @@ __host__ __device__ constexpr int dec_stages(int D, int NT) {
   return s > 8 ? 8 : s;
 }
 
-// The batch's steps: s_pre[b] = steps of the pairs before sequence b, over all
+// A pair's units of work: its fixed cost, then its steps.
+__device__ __forceinline__ int kv_units(const KvWork& w) { return w.steps > 0 ? w.steps + kPairCost : 0; }
+
+// The batch's work: s_pre[b] = units of the pairs before sequence b, over all
 // heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
 __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, long long* s_sum, int* s_bad) {
   const int tid = threadIdx.x, T = blockDim.x, lane = tid & 31, wid = tid >> 5;
@@ -54,7 +60,7 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
   for (int b = b0; b < b1; ++b) {
     const KvWork w = kv_work(a, b);
     if (!w.ok) *s_bad = 1;
-    mine += (long long)w.steps * a.c.K;
+    mine += (long long)kv_units(w) * a.c.K;
   }
   long long v = mine;
 #pragma unroll
@@ -68,7 +74,7 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
   for (int i = 0; i < wid; ++i) before += s_sum[i];
   for (int b = b0; b < b1; ++b) {
     s_pre[b] = before;
-    before += (long long)kv_work(a, b).steps * a.c.K;
+    before += (long long)kv_units(kv_work(a, b)) * a.c.K;
   }
   if (b0 < a.n && b1 == a.n) s_pre[a.n] = before;
   __syncthreads();
@@ -183,10 +189,15 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
   while (u < u_end) {
     while (s_pre[b + 1] <= u) ++b;
     const KvWork w = kv_work(a, b);
-    const int h = (int)((u - s_pre[b]) / w.steps);
-    const long long item0 = s_pre[b] + (long long)h * w.steps;
-    const int first = (int)(u - item0);
-    const int last = (int)min((long long)w.steps, u_end - item0);  // steps [first, last) of the pair are this CTA's
+    const int units = kv_units(w), h = (int)((u - s_pre[b]) / units);
+    const long long item0 = s_pre[b] + (long long)h * units + kPairCost;  // the first step
+    const int first = (int)max(u - item0, 0LL);
+    const int last = (int)(min(item0 + w.steps, u_end) - item0);  // steps [first, last) of the pair are this CTA's
+    u = item0 + last;
+    if (last <= first) {  // the run ends within the pair's fixed cost
+      u = u_end;
+      break;
+    }
     const int n_rows = w.rows * a.G;
     const bool cap = a.softcap > 0.0f;
     const int* table = c.table + (size_t)w.seq * c.max_blocks;
@@ -452,7 +463,10 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         if (g == 0) s_m[wid][8 * nt + 2 * t + q] = m[nt][q], s_l[wid][8 * nt + 2 * t + q] = v;
       }
     __syncthreads();  // also: every warp is done with its ring
-    float* part = reinterpret_cast<float*>(smem) + (size_t)wid * R * D;
+    // [row][column tile][g]: the lanes' pairs of columns side by side, rows two
+    // pairs further apart than their length, so that no two lanes share a bank
+    constexpr int RS = D / 2 + 2;
+    float2* part = reinterpret_cast<float2*>(smem) + (size_t)wid * R * RS;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -463,29 +477,27 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         for (int i = 1; i < kDecWarps; ++i) top = fmaxf(top, s_m[i][r]);
         const float f = m[nt][q] == -INFINITY ? (l[nt][q] == 0.0f ? 0.0f : l[nt][q]) : ex2(m[nt][q] - top);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const int d = D == 64 ? 8 * g + 2 * k : 128 * (k >> 3) + 16 * g + 2 * (k & 7);
-          *reinterpret_cast<float2*>(part + r * D + d) = make_float2(o[k][nt][q] * f, o[k][nt][q + 2] * f);
-        }
+        for (int k = 0; k < KS; ++k) part[r * RS + 8 * k + g] = make_float2(o[k][nt][q] * f, o[k][nt][q + 2] * f);
       }
     __syncthreads();
     const bool split = first > 0 || last < w.steps;
     const int slot = 2 * blockIdx.x + (first > 0 ? 0 : 1);
-    for (int e = tid; e < n_rows * (D / 4); e += kDecThreads) {
-      const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+    for (int e = tid; e < n_rows * (D / 2); e += kDecThreads) {
+      const int r = e / (D / 2), p = e % (D / 2), k = p >> 3, pg = p & 7;
+      const int d = D == 64 ? 8 * pg + 2 * k : 128 * (k >> 3) + 16 * pg + 2 * (k & 7);
       float top = s_m[0][r];
 #pragma unroll
       for (int i = 1; i < kDecWarps; ++i) top = fmaxf(top, s_m[i][r]);
-      float sum = 0.0f;
-      float4 acc = make_float4(0, 0, 0, 0);
+      float sum = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
       for (int i = 0; i < kDecWarps; ++i) {
         sum += s_m[i][r] == -INFINITY ? s_l[i][r] : s_l[i][r] * ex2(s_m[i][r] - top);
-        const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (size_t)i * R * D + r * D + d);
-        acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+        const float2 v = reinterpret_cast<const float2*>(smem)[((size_t)i * R + r) * RS + p];
+        x += v.x;
+        y += v.y;
       }
       if (split) {
-        *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * R + r) * D + d) = acc;
+        *reinterpret_cast<float2*>(a.part_o + ((size_t)slot * R + r) * D + d) = make_float2(x, y);
         if (d == 0) a.part_ml[(size_t)slot * 2 * R + r] = top, a.part_ml[(size_t)slot * 2 * R + R + r] = sum;
         if (e == 0 && first == 0)
           a.split[blockIdx.x] = make_int4(w.row0, n_rows, h, runs.owner(item0 + w.steps - 1) - blockIdx.x + 1);
@@ -493,8 +505,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         const long long row = w.row0 + r / a.G;
         const int head = h * a.G + r % a.G;
         const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-        *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (size_t)head * D + d) =
-            make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+        *reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + (size_t)head * D + d) = pack_bf16x2(x * f, y * f);
         if (d == 0) {
           const float l2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
           if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
@@ -503,7 +514,6 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       }
     }
     __syncthreads();  // the parts are read: the ring may be written
-    u = item0 + last;
   }
 }
 
@@ -524,6 +534,41 @@ __device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r
   const int head = at.z * a.G + r % a.G;
   const bool failed = a.c.control[1] != 0;  // within the call
   auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
+  constexpr int V = D / 32;  // a lane's columns
+  if (parts <= 8) {  // one warp, no barriers
+    if (wid > 0) return;
+    const float pm = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + r] : -INFINITY;
+    const float pl = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + R + r] : 0.0f;
+    float acc[V], part[8][V];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int v = 0; v < V; ++v) part[i][v] = i < parts ? a.part_o[(slot_of(i) * R + r) * D + v * 32 + lane] : 0.0f;
+    float top = pm;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float f = pm == -INFINITY ? (pl == 0.0f ? 0.0f : pl) : ex2(pm - top);
+    float sum = pm == -INFINITY ? pl : pl * f;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    sum = __shfl_sync(0xffffffffu, sum, 0);
+    top = __shfl_sync(0xffffffffu, top, 0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __shfl_sync(0xffffffffu, f, i);
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] = fmaf(w, part[i][v], acc[v]);
+    }
+    const float inv = failed ? kv_nan() : sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      a.out[row * a.out_stride + (size_t)head * D + v * 32 + lane] = __float2bfloat16_rn(acc[v] * inv);
+    if (lane == 0 && a.lse != nullptr)
+      a.lse[row * a.H + head] = failed ? kv_nan() : sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    return;
+  }
   float mi[4], li[4];  // this thread's parts: W 128 / 32 = 1,024 CTAs at most
   float top = -INFINITY;
 #pragma unroll
@@ -537,8 +582,6 @@ __device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r
     }
     top = fmaxf(top, mi[k]);
   }
-  // a lane's D / 32 columns of the first parts, loaded before the weights are known
-  constexpr int V = D / 32;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (lane == 0) s_red[wid] = top;
@@ -612,10 +655,10 @@ __device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w,
     for (int f = lane * 4; f < nb * sums; f += 128) {
       const int step = j * per + f / R - w.step0, r = f & (R - 1);  // R is a power of two
       if (step < 0 || step >= w.steps) continue;
-      const float* p = a.step_lse + (pre + step) * R + r;
+      const float* p = a.step_lse + (pre + kPairCost + step) * R + r;
 #pragma unroll 4
       for (int h = 0; h < c.K; ++h) {
-        const float4 x = *reinterpret_cast<const float4*>(p + (long long)h * w.steps * R);
+        const float4 x = *reinterpret_cast<const float4*>(p + (long long)h * kv_units(w) * R);
         const float4 t = *reinterpret_cast<const float4*>(s_top + h * R + r);
         if (t.x != -INFINITY) v += ex2(x.x - t.x);
         if (t.y != -INFINITY) v += ex2(x.y - t.y);
@@ -629,22 +672,20 @@ __device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w,
   }
 }
 
-// The joins as `joins` CTAs (runs by
-// rows), then the block weights (`ny` CTAs a sequence), which put the sums of a
-// split pair's rows together from its parts as well and so need not wait for the
-// joins.
+// The block weights (`ny` CTAs a sequence), which put the sums of a split pair's
+// rows together from its parts, and the joins (`joins` CTAs: runs by rows).
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, int R, int warps, int joins, int ny) {
   extern __shared__ __align__(16) float s_top[];
   grid_wait();
   grid_release();
-  const int x = blockIdx.x;
-  if (x < joins) {
-    kv_join<D>(a, R, x % a.ctas, x / a.ctas);
+  const int obs = gridDim.x - joins;  // first: they take longer
+  if ((int)blockIdx.x >= obs) {
+    kv_join<D>(a, R, (blockIdx.x - obs) % a.ctas, (blockIdx.x - obs) / a.ctas);
     return;
   }
   const KvCache& c = a.c;
-  const int b = (x - joins) / ny, y = (x - joins) % ny;
+  const int b = blockIdx.x / ny, y = blockIdx.x % ny;
   const KvWork w = kv_work(a, b);
   const long long pre = a.item_pre[b], total = a.item_pre[a.n];
   if (c.control[1] != 0 || w.steps == 0) return;
@@ -655,7 +696,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, i
     const int h = i / R, r = i - h * R;
     float l2 = -INFINITY;
     if (r < n) {
-      const long long u0 = pre + (long long)h * w.steps;
+      const long long u0 = pre + (long long)h * kv_units(w) + kPairCost;
       const int c0 = runs.owner(u0), c1 = runs.owner(u0 + w.steps - 1);
       if (c0 == c1) {
         l2 = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
@@ -686,7 +727,7 @@ template <int D, int NT, int FMT, bool OBS>
 cudaError_t decode_as(const KvAttnArgs& a, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   constexpr int W = dec_warps(D, NT), ring = W * dec_stages(D, NT) * dec_stage_bytes(D);
-  static_assert(W * 8 * NT * D * 4 <= ring, "the parts fit the rings");
+  static_assert(W * 8 * NT * (D + 4) * 4 <= ring, "the parts fit the rings");
   cudaError_t e = smem_attr_once(kv_decode_kernel<D, NT, FMT, OBS>, ring + (kKvMaxSeqs + 1) * (int)sizeof(long long), done);
   if (e != cudaSuccess) return e;
   e = launch_after(false, kv_decode_kernel<D, NT, FMT, OBS>, dim3(a.ctas), dim3(32 * W),
@@ -711,6 +752,8 @@ cudaError_t decode_fmt(const KvAttnArgs& a, cudaStream_t s) {
 }
 
 }  // namespace
+
+int kv_decode_pair_cost() { return kPairCost; }
 
 int kv_decode_tiles(int rows, int D) {
   return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 && D < 256 ? 4 : 0;
