@@ -205,6 +205,12 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 
+__device__ __forceinline__ float lg2(float x) {
+  float r;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // softcap * tanh(x / softcap) = softcap (1 - 2 / (e^(2 x / softcap) + 1)); the
 // quotient's limits are those of the formula.  two_log2e_cap = 2 log2(e) / cap.
 __device__ __forceinline__ float kv_softcap(float x, float cap, float two_log2e_cap) {

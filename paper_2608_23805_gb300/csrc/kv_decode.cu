@@ -243,12 +243,14 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
 
     float o[KS][NT][4], m[NT][2], l[NT][2];
     float mu[NT][2];  // m, or 0 where no token has been seen: masked exponents are -inf either way
+    float lim[NT][2];  // exponents above it move m
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) o[k][nt][0] = o[k][nt][1] = o[k][nt][2] = o[k][nt][3] = 0.0f;
       m[nt][0] = m[nt][1] = -INFINITY;
       mu[nt][0] = mu[nt][1] = 0.0f;
+      lim[nt][0] = lim[nt][1] = -INFINITY;
       l[nt][0] = l[nt][1] = 0.0f;
     }
     const float two_cap = cap ? 2.0f * kLog2e / a.softcap : 0.0f;
@@ -278,9 +280,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
     StepInfo use = info(lane), ahead = use;  // steps 32 q + lane: those in use, those being fetched
     // a lane's copies: 16 bytes of row r0 + 512 / D per copy
     constexpr int CPR = D / 16, RPC = 32 / CPR;
-    uint32_t in_dst[2];
-    in_dst[0] = ring_u + dec_chunk<D>(lane / CPR, lane % CPR);
-    in_dst[1] = ring_u + dec_chunk<D>(lane / CPR + RPC, lane % CPR);
+    const uint32_t in_dst = ring_u + dec_chunk<D>(lane / CPR, lane % CPR);
     int st_in = 0;  // the stage that the next fetch fills
     auto fetch = [&](int i) {
       if ((i & 31) == 0 && i > 0) ahead = info(i + lane);
@@ -291,12 +291,9 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
         const uint8_t* kp = c.codes[0] + at;
         const uint8_t* vp = c.codes[1] + at;
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n) {  // rows n RPC on: every second copy has the first one's swizzle
-          constexpr int P2 = D == 64 ? 1 : D == 128 ? 2 : 4;  // copies after which the swizzle repeats
-          uint32_t dst;
-          if (P2 == 4) dst = ring_u + dec_chunk<D>(lane / CPR + (n & 3) * RPC, lane % CPR) + (n >> 2) * 4 * RPC * D;
-          else dst = in_dst[n & (P2 - 1)] + (n / P2) * P2 * RPC * D;
-          dst += st_in * SB;
+        for (int n = 0; n < D / 32; ++n) {
+          // rows n RPC on: the swizzle, row & 7, changes by n RPC & 7 (D = 64: by nothing)
+          const uint32_t dst = ((in_dst + st_in * SB) ^ (D == 64 ? 0 : (n * RPC & 7) << 4)) + n * RPC * D;
           copy16(dst, kp + n * 512);
           copy16(dst + 16 * D, vp + n * 512);
         }
@@ -305,6 +302,8 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       st_in = st_in + 1 == S ? 0 : st_in + 1;
     };
     int st = 0;  // the stage in use
+    const uint32_t k_at = dec_chunk<D>(g, dec_kchunk<D>(t, 0));
+    const uint32_t v_at = D == 64 ? dec_chunk<D>(2 * t, g >> 1) + (g & 1) * 8 : dec_chunk<D>(2 * t, g);
 #pragma unroll 1
     for (int i = 0; i < S - 1; ++i) fetch(i);
 
@@ -327,8 +326,10 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
       for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        const uint4 x = ld_shared_v4(kb + dec_chunk<D>(g, dec_kchunk<D>(t, j)));
-        const uint4 y = ld_shared_v4(kb + dec_chunk<D>(g + 8, dec_kchunk<D>(t, j)));
+        // chunk dec_kchunk(t, j): one more flips the lowest bit, eight more are the next 128 bytes
+        const uint32_t kj = ((kb + k_at) ^ ((j & 1) << 4)) + (j >> 1) * 128;
+        const uint4 x = ld_shared_v4(kj);
+        const uint4 y = ld_shared_v4(kj + 8 * D);  // row g + 8: the same swizzle
         const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) over |= sc[nt][q] > m[nt][q & 1] + kLazy;
+        for (int q = 0; q < 4; ++q) over |= sc[nt][q] > lim[nt][q & 1];
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -383,6 +384,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
             const float f = v == -INFINITY ? 1.0f : ex2(m[nt][q] - v);
             m[nt][q] = v;
             mu[nt][q] = v == -INFINITY ? 0.0f : v;
+            lim[nt][q] = v + kLazy;
             l[nt][q] *= f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) o[k][nt][q] *= f, o[k][nt][q + 2] *= f;
@@ -406,8 +408,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
           }
           if (g == 0)
             *reinterpret_cast<float2*>(a.step_lse + (item0 + idx) * R + 8 * nt + 2 * t) =
-                make_float2(v0 > 0.0f ? m[nt][0] + __log2f(v0) : v0 == 0.0f ? -INFINITY : v0,
-                            v1 > 0.0f ? m[nt][1] + __log2f(v1) : v1 == 0.0f ? -INFINITY : v1);
+                make_float2(mu[nt][0] + lg2(v0), mu[nt][1] + lg2(v1));
         }
         pf[nt][0] = transpose8x8(pack_f16x2(p[0], p[1]));
         pf[nt][1] = transpose8x8(pack_f16x2(p[2], p[3]));
@@ -431,17 +432,17 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
           }
         }
       };
+      // tokens 2t, 2t + 1 (the next row: D = 64 has its swizzle in pairs of rows), 2t + 8, 2t + 9
       if constexpr (D == 64) {
-        const int ch = g >> 1, half = (g & 1) * 8;
-        const uint2 x = ld_shared_v2(vb + dec_chunk<D>(2 * t, ch) + half), y = ld_shared_v2(vb + dec_chunk<D>(2 * t + 1, ch) + half);
-        const uint2 z = ld_shared_v2(vb + dec_chunk<D>(2 * t + 8, ch) + half), v = ld_shared_v2(vb + dec_chunk<D>(2 * t + 9, ch) + half);
+        const uint32_t va = vb + v_at;
+        const uint2 x = ld_shared_v2(va), y = ld_shared_v2(va + D), z = ld_shared_v2(va + 8 * D), v = ld_shared_v2(va + 9 * D);
         const uint32_t xs[4] = {x.x, x.y, 0, 0}, ys[4] = {y.x, y.y, 0, 0}, zs[4] = {z.x, z.y, 0, 0}, vs4[4] = {v.x, v.y, 0, 0};
         values(xs, ys, zs, vs4, 2, 0);
       } else {
 #pragma unroll
         for (int j = 0; j < D / 128; ++j) {
-          const uint4 x = ld_shared_v4(vb + dec_chunk<D>(2 * t, g + 8 * j)), y = ld_shared_v4(vb + dec_chunk<D>(2 * t + 1, g + 8 * j));
-          const uint4 z = ld_shared_v4(vb + dec_chunk<D>(2 * t + 8, g + 8 * j)), v = ld_shared_v4(vb + dec_chunk<D>(2 * t + 9, g + 8 * j));
+          const uint32_t va = vb + v_at + j * 128, vo = ((vb + v_at) ^ 16) + j * 128 + D;
+          const uint4 x = ld_shared_v4(va), y = ld_shared_v4(vo), z = ld_shared_v4(va + 8 * D), v = ld_shared_v4(vo + 8 * D);
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
           const uint32_t zs[4] = {z.x, z.y, z.z, z.w}, vs4[4] = {v.x, v.y, v.z, v.w};
           values(xs, ys, zs, vs4, 4, 8 * j);
