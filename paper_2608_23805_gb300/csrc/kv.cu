@@ -674,7 +674,8 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;
   const int tiles = kv_decode_tiles(a.max_rows * a.G, c.D);
   if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
-  a.ctas = kv->sms < 1024 ? kv->sms : 1024;
+  a.ctas = kv->sms < 512 ? kv->sms : 512;
+  if (tiles != 0) a.ctas *= 2;  // two of the decode form's share an SM
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;

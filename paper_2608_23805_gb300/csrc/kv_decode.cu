@@ -34,15 +34,16 @@ namespace {
 constexpr float kLazy = 8.0f;  // P may reach 2^8
 
 // Warps of a CTA, by the registers that a warp's outputs and queries take
-// (D x 8 NT of each): the more the better hidden are a step's latencies.
-__host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 16 : 8; }
+// (D x 8 NT of each): the more the better hidden are a step's latencies.  Two
+// CTAs share an SM, so that one reads while the other begins or ends a pair.
+__host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 8 : 4; }
 // What a pair costs a CTA beside its steps (queries, first loads, the warps'
 // sums), in steps.
 constexpr int kPairCost = 8;
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
-// Stages of a warp's ring: 192 KB a CTA, at most 8.
+// Stages of a warp's ring: 96 KB a CTA, at most 8.
 __host__ __device__ constexpr int dec_stages(int D, int NT) {
-  const int s = 192 * 1024 / dec_warps(D, NT) / dec_stage_bytes(D);
+  const int s = 96 * 1024 / dec_warps(D, NT) / dec_stage_bytes(D);
   return s > 8 ? 8 : s;
 }
 
@@ -119,7 +120,7 @@ struct StepInfo {
 };
 
 template <int D, int NT, int FMT, bool OBS>
-__global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvAttnArgs a) {
+__global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvAttnArgs a) {
   constexpr int kDecWarps = dec_warps(D, NT), kDecThreads = 32 * kDecWarps;
   constexpr int KS = D / 16;          // MMAs along a row, and column tiles of the output
   constexpr int CH = D / 64;          // 16-byte chunks of a key row a lane takes
@@ -518,59 +519,84 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 1) kv_decode_kernel(KvA
   }
 }
 
-// Joins the parts of the pair that begins in run x and goes on past it, row r:
-// weights 2^(M_i - M) over the parts, in the CTAs' order within each warp and
-// warp by warp.  Bound: latency.
-constexpr int kJoinThreads = 256;
+// Joins the parts of the pair that begins in run x and goes on past it: weights
+// 2^(M_i - M) over the parts, in the CTAs' order.  Bound: latency.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinFew = 32;
 
+// Up to 32 parts: a warp a row, no barriers.
 template <int D>
-__device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r) {
-  constexpr int W = kJoinThreads / 32;
-  __shared__ float s_f[1024], s_part[W][D], s_red[W];
+__device__ __forceinline__ void kv_join_few(const KvAttnArgs& a, int R, int x, int r) {
+  constexpr int V = D / 32, B = 8;  // a lane's columns, parts loaded at a time
+  const int lane = threadIdx.x & 31;
   const int4 at = a.split[x];  // first row, rows, head, parts
   const int parts = at.w;
-  if (r >= at.y || parts == 0) return;
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  if (r >= at.y || parts == 0 || parts > kJoinFew) return;
   const long long row = at.x + r / a.G;
   const int head = at.z * a.G + r % a.G;
   const bool failed = a.c.control[1] != 0;  // within the call
   auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
-  constexpr int V = D / 32;  // a lane's columns
-  if (parts <= 8) {  // one warp, no barriers
-    if (wid > 0) return;
-    const float pm = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + r] : -INFINITY;
-    const float pl = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + R + r] : 0.0f;
-    float acc[V], part[8][V];
+  const float pm = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + r] : -INFINITY;
+  const float pl = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + R + r] : 0.0f;
+  float acc[V], part[B][V];
+  auto load = [&](int i0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < B; ++i)
 #pragma unroll
-      for (int v = 0; v < V; ++v) part[i][v] = i < parts ? a.part_o[(slot_of(i) * R + r) * D + v * 32 + lane] : 0.0f;
-    float top = pm;
+      for (int v = 0; v < V; ++v) part[i][v] = i0 + i < parts ? a.part_o[(slot_of(i0 + i) * R + r) * D + v * 32 + lane] : 0.0f;
+  };
+  load(0);  // on its way while the weights are worked out
+  float top = pm;
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float f = pm == -INFINITY ? (pl == 0.0f ? 0.0f : pl) : ex2(pm - top);
-    float sum = pm == -INFINITY ? pl : pl * f;
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float f = pm == -INFINITY ? (pl == 0.0f ? 0.0f : pl) : ex2(pm - top);
+  float sum = pm == -INFINITY ? pl : pl * f;
 #pragma unroll
-    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    sum = __shfl_sync(0xffffffffu, sum, 0);
-    top = __shfl_sync(0xffffffffu, top, 0);
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] = 0.0f;
+  for (int v = 0; v < V; ++v) acc[v] = 0.0f;
+  for (int i0 = 0; i0 < parts; i0 += B) {
+    if (i0 > 0) load(i0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float w = __shfl_sync(0xffffffffu, f, i);
+    for (int i = 0; i < B; ++i) {
+      const float w = __shfl_sync(0xffffffffu, f, i0 + i);  // 0 past the last part
 #pragma unroll
       for (int v = 0; v < V; ++v) acc[v] = fmaf(w, part[i][v], acc[v]);
     }
-    const float inv = failed ? kv_nan() : sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      a.out[row * a.out_stride + (size_t)head * D + v * 32 + lane] = __float2bfloat16_rn(acc[v] * inv);
-    if (lane == 0 && a.lse != nullptr)
-      a.lse[row * a.H + head] = failed ? kv_nan() : sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
-    return;
   }
-  float mi[4], li[4];  // this thread's parts: W 128 / 32 = 1,024 CTAs at most
+  const float inv = failed ? kv_nan() : sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int v = 0; v < V; ++v) a.out[row * a.out_stride + (size_t)head * D + v * 32 + lane] = __float2bfloat16_rn(acc[v] * inv);
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[row * a.H + head] = failed ? kv_nan() : sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+// More: the n-th such pair, a CTA a row.
+template <int D>
+__device__ __forceinline__ void kv_join_many(const KvAttnArgs& a, int R, int n, int r) {
+  constexpr int W = kJoinWarps, V = D / 32;  // V: a lane's columns
+  __shared__ float s_f[1024], s_part[W][D], s_red[W];
+  __shared__ int s_scan[32], s_x;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  if (tid == 0) s_x = -1;
+  int base = 0;  // such pairs before this round's runs
+  for (int i0 = 0; i0 < a.ctas; i0 += kJoinThreads) {
+    const int many = i0 + tid < a.ctas && a.split[i0 + tid].w > kJoinFew;
+    const int in = block_scan(many, s_scan);
+    if (many && base + in - 1 == n) s_x = i0 + tid;
+    __syncthreads();
+    base += s_scan[31];  // the last warp's running total
+    __syncthreads();
+  }
+  const int x = s_x;
+  if (x < 0) return;
+  const int4 at = a.split[x];  // first row, rows, head, parts
+  const int parts = at.w;
+  if (r >= at.y) return;
+  const long long row = at.x + r / a.G;
+  const int head = at.z * a.G + r % a.G;
+  const bool failed = a.c.control[1] != 0;  // within the call
+  auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
+  float mi[4], li[4];  // this thread's parts: 1,024 CTAs at most
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -626,10 +652,8 @@ __device__ __forceinline__ void kv_join(const KvAttnArgs& a, int R, int x, int r
     for (int i = 0; i < W; ++i) v += s_part[i][d];
     a.out[row * a.out_stride + (size_t)head * D + d] = __float2bfloat16_rn(v * f);
   }
-  if (tid == 0) {
-    const float l2 = failed ? kv_nan() : sum == 0.0f ? -INFINITY : top + log2f(sum);
-    if (a.lse != nullptr) a.lse[row * a.H + head] = l2 * kLn2;
-  }
+  if (tid == 0 && a.lse != nullptr)
+    a.lse[row * a.H + head] = failed ? kv_nan() : sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // Attention weight of each block: over the heads, its 16-token granules and the
@@ -674,7 +698,8 @@ __device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w,
 }
 
 // The block weights (`ny` CTAs a sequence), which put the sums of a split pair's
-// rows together from its parts, and the joins (`joins` CTAs: runs by rows).
+// rows together from its parts, and the joins (`joins` CTAs: runs by 8 rows for
+// pairs of few parts, then the pairs of many by rows).
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, int R, int warps, int joins, int ny) {
   extern __shared__ __align__(16) float s_top[];
@@ -682,7 +707,9 @@ __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, i
   grid_release();
   const int obs = gridDim.x - joins;  // first: they take longer
   if ((int)blockIdx.x >= obs) {
-    kv_join<D>(a, R, (blockIdx.x - obs) % a.ctas, (blockIdx.x - obs) / a.ctas);
+    const int i = blockIdx.x - obs, few = a.ctas * (R / kJoinWarps);
+    if (i < few) kv_join_few<D>(a, R, i % a.ctas, i / a.ctas * kJoinWarps + (threadIdx.x >> 5));
+    else kv_join_many<D>(a, R, (i - few) / R, (i - few) % R);
     return;
   }
   const KvCache& c = a.c;
@@ -734,7 +761,7 @@ cudaError_t decode_as(const KvAttnArgs& a, cudaStream_t s) {
   e = launch_after(false, kv_decode_kernel<D, NT, FMT, OBS>, dim3(a.ctas), dim3(32 * W),
                    ring + (a.n + 1) * sizeof(long long), s, a);
   if (e != cudaSuccess) return e;
-  const int joins = a.ctas * a.max_rows * a.G;
+  const int joins = a.ctas * NT + a.ctas / kJoinFew * 8 * NT;  // no more than that have more than 32 parts
   // a turn of every warp of a CTA; longer tables take several
   const int sums = a.c.P / 16 * 8 * NT, per = kJoinThreads / 32 * (sums >= 128 ? 1 : 128 / sums);
   const int ny = min((min(a.c.max_blocks, a.c.n_blocks) + per - 1) / per, 64);

@@ -515,3 +515,12 @@ def test_chunk_refusals():
     out, _ = c.cache.attention(q, ints([0, 40, 80]), 40)
     assert out[10:40].isnan().all()
     assert c.cache.status() == N.MSI_ERR_INVALID_ARG
+
+
+def test_decode_parts_of_every_number():
+    """Pairs cut into few and into many parts in one call: one long sequence
+    among short ones (its parts are joined by whole CTAs, theirs by warps)."""
+    c = KvCase(n_seqs=6, K=2, D=64, P=16, n_blocks=1500, max_blocks=1200)
+    c.append(list(range(6)), [18000, 300, 40, 900, 16, 1])
+    c.attend([3, 0, 5, 1, 2, 4], [1, 2, 1, 1, 2, 1], 4, observe=True)
+    np.testing.assert_allclose(c.cache.weight.cpu().numpy(), c.model.weight, rtol=2e-5, atol=1e-9)
