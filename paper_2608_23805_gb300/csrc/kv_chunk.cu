@@ -696,61 +696,78 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   } else {
     // --------------------------------------------------------------- conversion
     // The tasks of all token tiles in order, 8 of keys then 8 of values a tile;
-    // this warp takes every seventh.  A task's block is looked up three turns
+    // this warp takes every seventh, so it has a part in every tile and operand and
+    // its waits cannot miss a phase.  A task's block is looked up three turns
     // ahead, its scales and codes are loaded two turns ahead.
     struct Task {
-      int t;         // token tile of the CTA; -1: none
-      int idx;       // of the tile's 16 tasks
-      int h, tok;    // the first of its tokens
-      int id;        // block
-      bool held;     // false: past the tokens held
+      int t;               // token tile of the CTA; -1: none
+      int idx;             // of the tile's 16 tasks
+      int id;              // block
+      bool held;           // false: past the tokens held
+      int h;
+      const uint8_t* src;  // the lane's first codes, were the block number 0
     };
     constexpr int SUB = D / C::TC;  // tasks of a granule's operand
     constexpr int RSTEP = C::TC == 64 ? 8 : 4;  // rows a load of the warp covers
     // eight lanes write two rows of one 64-column panel: no bank conflicts
     const int col = (lane & 3) + (C::TC == 64 ? 0 : (lane >> 4) << 2);  // 16-code chunk of the row
     const int row0 = (lane >> 2) & (RSTEP - 1);
-    const uint32_t to0 = (col >> 2) * C::NT * 128 + row0 * 128 + (((col & 3) * 2 ^ row0) << 4);  // rows 4 apart: chunk ^ 4
+    const uint32_t to0 = smem_u32(sK) + (col >> 2) * C::NT * 128 + row0 * 128 + (((col & 3) * 2 ^ row0) << 4);  // rows 4 apart: chunk ^ 4
+    const long long block_bytes = (long long)c.K * c.P * D;
+    const uint32_t bars = smem_u32(s_bar);
     int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
     int at = warp - kSoftWarps;            // the next task to look up
     bool more = true;
+    // of the part
+    const int* table = nullptr;
+    const uint8_t *keys = nullptr, *values = nullptr;
+    int tok_part = 0;                      // first token of its first tile, less the tiles before it
     auto look_up = [&]() {
-      Task k = {-1, 0, 0, 0, 0, false};
-      const int t = at >> 4;
+      Task k = {-1, 0, 0, false, 0, nullptr};
+      const int t = at >> 4, idx = at & 15;
       while (more && t >= base + n) {
         base += n;
         n = 0;
         more = walk.next(a, part);
-        if (more) n = part.last - part.first;
+        if (more) {
+          n = part.last - part.first;
+          table = c.table + (size_t)part.seq * c.max_blocks;
+          const size_t lane_at = ((size_t)part.h * c.P + row0) * D + col * 16;
+          keys = c.codes[0] + lane_at;
+          values = c.codes[1] + lane_at;
+          tok_part = (part.tile0 + part.first - base) * C::NT;
+        }
       }
       if (!more) return k;
+      const int tok = tok_part + t * C::NT + ((idx & 7) / SUB) * 16;
       k.t = t;
-      k.idx = at & 15;
+      k.idx = idx;
       k.h = part.h;
-      k.tok = (part.tile0 + part.first + t - base) * C::NT + ((at & 7) / SUB) * 16;
-      if (k.tok < part.held) {
-        // looked at when the codes are loaded: a wait for it here would cost a latency a task
-        k.id = c.table[(size_t)part.seq * c.max_blocks + (k.tok >> c.logP)];
-        k.held = true;
-      }
+      k.src = (idx < 8 ? keys : values) + ((tok & (c.P - 1)) * D + (idx & (SUB - 1)) * C::TC);
+      k.held = tok < part.held;
+      // looked at when the codes are loaded: a wait for it here would cost a latency a task
+      if (k.held) k.id = table[tok >> c.logP];
       at += kConvWarps;
       return k;
     };
     auto load = [&](const Task& k, uint4 (&x)[C::LOADS], float& ks, float& vs) {
-      const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
-      const bool there = k.id >= 0 && k.id < c.n_blocks;
-      ks = vs = k.held && !there ? kv_nan() : 1.0f;
+      ks = vs = 1.0f;
+      if (k.held && (unsigned)k.id < (unsigned)c.n_blocks) {
+        const uint8_t* src = k.src + k.id * block_bytes;
 #pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) x[i] = make_uint4(z, z, z, z);
-      if (k.held && !there && lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
-      if (!k.held || !there) return;
-      const uint8_t* src = c.codes[k.idx >> 3] + (((size_t)k.id * c.K + k.h) * c.P + (k.tok & (c.P - 1)) + row0) * D +
-                           (k.idx & (SUB - 1)) * C::TC + col * 16;
+        for (int i = 0; i < C::LOADS; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * RSTEP * D);
+        if (k.idx < 8 && (k.idx & (SUB - 1)) == 0) {
+          ks = c.scale[0][(size_t)k.id * c.K + k.h];
+          vs = c.scale[1][(size_t)k.id * c.K + k.h];
+        }
+      } else {
+        const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
 #pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * RSTEP * D);
-      if (k.idx < 8) {
-        ks = c.scale[0][(size_t)k.id * c.K + k.h];
-        vs = c.scale[1][(size_t)k.id * c.K + k.h];
+        for (int i = 0; i < C::LOADS; ++i) x[i] = make_uint4(z, z, z, z);
+        if (k.held) {
+          ks = vs = kv_nan();
+          if (lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
+        }
       }
     };
     Task k0 = look_up(), k1 = look_up(), k2 = look_up();
@@ -759,11 +776,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     load(k0, x0, ks0, vs0);
     load(k1, x1, ks1, vs1);
     auto turn = [&](const Task& k, uint4 (&x)[C::LOADS], float ks, float vs) {
-      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1;
-      const bool keys = k.idx < 8;
-      if (!mbar_wait_warp(keys ? &kempty[st] : &vempty[st], ph, abort_flag, kChunkWait)) return false;
-      const int g = (k.idx & 7) / SUB, panel0 = (k.idx & (SUB - 1)) * (C::TC / 64);
-      const uint32_t tile = smem_u32(keys ? sK : sV) + st * C::KBYTES + panel0 * C::NT * 128 + g * 16 * 128 + to0;
+      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1, v = k.idx >> 3, g = (k.idx & 7) / SUB;
+      // s_bar: full and empty barriers of keys, then of values
+      const uint32_t full = bars + (v * 4 + st) * 8;
+      if (!mbar_wait_warp(kempty + v * 4 + st, ph, abort_flag, kChunkWait)) return false;
+      const uint32_t tile = to0 + (2 * v + st) * C::KBYTES + (k.idx & (SUB - 1)) * (C::TC / 64) * C::NT * 128 + g * 16 * 128;
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
         // the swizzle: chunk ^ (row & 7), the row being row0 + i RSTEP
@@ -772,10 +789,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         st_shared_v4(to ^ 16, make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w)));
       }
       // the granule's scales: read by softmax after the scores, which follow kfull
-      if (keys && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, log2f(vs), vs > 0.0f ? 1.0f / vs : 1.0f, 0.0f};
+      if (k.idx < 8 && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(keys ? &kfull[st] : &vfull[st]);
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full) : "memory");
       return true;
     };
     while (k0.t >= 0) {
