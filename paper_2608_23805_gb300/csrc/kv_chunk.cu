@@ -54,7 +54,10 @@ constexpr int kChunkThreads = 32 * (kMmaWarp + 1);
 constexpr int kSoftRegs = 144, kConvRegs = 112;
 static_assert(kChunkThreads == 512 && 2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
 // What an item costs beside its tiles (queries, first scores, output), in tiles.
-constexpr int kItemCost = 2;
+// D = 256, 4 sequences of 3,000 on 3,000: 562, 473, 454, 470 us at 2, 4, 6, 8; 128
+// columns or fewer, where a long item hides it: 826 us at 1, 2 and 4.
+template <int D>
+constexpr int kItemCost = D == 256 ? 6 : 2;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
   uint64_t d;
@@ -107,7 +110,7 @@ __device__ __forceinline__ void set_regs() {
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int rows_tile, int nt) {
+__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int rows_tile, int nt, int cost) {
   __shared__ int s_scan[32], s_base[kKvMaxSeqs + 1], s_bad;
   __shared__ int4 s_work[kKvMaxSeqs];  // seq, first row, rows, tokens held
   __shared__ long long s_sum[32], s_pre[kPlanThreads + 1], s_total;
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
       const int r1 = min(w.z * a.G, (rt + 1) * rows_tile) - 1;
       const int see0 = w.w - w.z + rt * rows_tile / a.G, see1 = w.w - w.z + r1 / a.G;
       const int t0 = a.window > 0 ? max(0, see0 - a.window + 1) / nt : 0;
-      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0) + kItemCost;  // an item that sees nothing has a tile too
+      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0) + cost;  // an item that sees nothing has a tile too
       a.items[2 * i] = w;
       a.items[2 * i + 1] = make_int4(h, rt, t0, 0);
     }
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
     __syncthreads();
   }
   const long long total = s_total;
-  const int ctas = (int)min((long long)a.ctas, max(1LL, total / (kItemCost + 1)));
+  const int ctas = (int)min((long long)a.ctas, max(1LL, total / 2));
   // where each CTA's run begins
   const KvRuns runs = {total, ctas};
   for (int x = tid; x < ctas && items > 0; x += kPlanThreads) {
@@ -194,6 +197,7 @@ struct Part {
   int first, last, tiles;      // token tiles [first, last) of the item's `tiles` are this CTA's
 };
 
+template <int COST>
 struct PartWalk {
   long long u, end;
   int item;
@@ -208,7 +212,7 @@ struct PartWalk {
   }
   __device__ __forceinline__ bool next(const KvAttnArgs& a, Part& p) {
     while (u < end) {
-      const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
+      const long long p0 = a.item_pre[item] + COST, p1 = a.item_pre[item + 1];
       const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
       p.first = (int)max(u - p0, 0LL);
       p.last = (int)(min(p1, end) - p0);
@@ -367,13 +371,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   uint8_t* sV = sK + 2 * C::KBYTES;
   uint64_t *kfull = s_bar, *kempty = s_bar + 2, *vfull = s_bar + 4, *vempty = s_bar + 6;
   uint64_t *qfull = s_bar + 8, *sfull = s_bar + 10, *pfull = s_bar + 12, *ofull = s_bar + 14, *ofree = s_bar + 16;
-  uint64_t* drain = s_bar + 18;
+  uint64_t *olast = s_bar + 18, *drain = s_bar + 20;  // ofull: every product's end; olast: that of a part's last
   volatile int* abort_flag = &s_abort;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
-    const int soft = C::NQ == 2 ? 128 : 256;  // threads of a row tile
+    const int soft = C::NQ == 2 ? 4 : 8;  // warps of a row tile
     for (int i = 0; i < 2; ++i) {
       mbar_init(kfull + i, 8);
       mbar_init(kempty + i, 1);
@@ -383,6 +387,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       mbar_init(sfull + i, 1);
       mbar_init(pfull + i, soft);
       mbar_init(ofull + i, 1);
+      mbar_init(olast + i, 1);
       mbar_init(ofree + i, soft);
     }
     mbar_init(drain, 1);
@@ -416,7 +421,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (a.lse != nullptr) a.lse[i] = kv_nan();
   }
   __syncthreads();  // every warp whole again before the register split
-  PartWalk walk;
+  PartWalk<kItemCost<D>> walk;
   walk.u = walk.end = 0;
   if (ok && a.plan[0] > 0 && (int)blockIdx.x < a.plan[2]) walk.init(a, blockIdx.x);
   Part part;
@@ -432,30 +437,40 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     auto gone = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0) != 0; };
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float two_cap = CAP ? 2.0f * kLog2e / a.softcap : 0.0f;
-    uint32_t kv = 0, ns = 0, no = 0;  // token tiles before the part's; S tiles seen; PVs of this row tile
-    bool go = true;
-    while (go && walk.next(a, part)) {
-      const int n = part.last - part.first;
-      const int rows = part.rows * a.G;
-      if (q > 0 && rows - part.row_tile * C::ROWS <= 128) {  // no second row tile
-        kv += n;
-        continue;
+    uint32_t kv = 0, ns = 0, parts = 0;  // token tiles before the part's; S tiles and parts of this row tile
+    bool go = true, pending = false;  // pending: a part whose output is still in TMEM
+    const uint32_t to = tmem + C::TO + q * D + lanes;
+    // of the part in work, kept beyond the next one's queries
+    int n = 0, slot = 0, qh = 0;
+    long long row = 0;
+    bool valid = false, split = false;
+    float crow = 0.0f, m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+    while (true) {
+      bool have = false;
+      while (go && walk.next(a, part)) {
+        if (q > 0 && part.rows * a.G - part.row_tile * C::ROWS <= 128) {  // no second row tile
+          kv += part.last - part.first;
+          continue;
+        }
+        have = true;
+        break;
       }
-      const int r = part.row_tile * C::ROWS + q * 128 + tr;
-      const bool valid = r < rows;
-      const int qi = valid ? r / a.G : part.rows - 1, qh = part.h * a.G + (valid ? r - qi * a.G : 0);
-      const int see = part.held - part.rows + qi;
-      const long long row = part.row0 + qi;
-      // the query row (its half) in fp16's range; the scores of the part before
-      // have all been computed
-      constexpr int QV = D / 8 / (C::NQ == 2 ? 1 : 2);
-      float crow;
-      {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + row * a.q_stride + (size_t)qh * D) + half * QV;
+      const int rows = part.rows * a.G, r = part.row_tile * C::ROWS + q * 128 + tr;
+      const bool nvalid = have && r < rows;
+      const int qi = nvalid ? r / a.G : part.rows - 1, nqh = part.h * a.G + (nvalid ? r - qi * a.G : 0);
+      const long long nrow = part.row0 + qi;
+      float ncrow = 0.0f;
+      if (have) {
+        // the query row (its half) in fp16's range.  The scores of the part before
+        // have all been computed: its output is read after this, while the tensor
+        // core begins with the new rows.
+        constexpr int QV = D / 8 / (C::NQ == 2 ? 1 : 2);
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + nrow * a.q_stride + (size_t)nqh * D) + half * QV;
         uint4 v[QV];
         uint32_t amax = 0;
 #pragma unroll
-        for (int i = 0; i < QV; ++i) v[i] = valid ? src[i] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < QV; ++i) v[i] = nvalid ? src[i] : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < QV; ++i) {
           const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
@@ -471,16 +486,78 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         const uint32_t e = kv_row_exp(amax);
         const bool finite = amax < 0x7f800000u;
         const float down = __uint_as_float((254 - e) << 23);
-        crow = (finite ? __uint_as_float(e << 23) * a.scale : kv_nan()) * (CAP ? 1.0f : kLog2e);
+        ncrow = (finite ? __uint_as_float(e << 23) * a.scale : kv_nan()) * (CAP ? 1.0f : kLog2e);
         const uint32_t sq = smem_u32(sQ) + q * C::QBYTES + tr * 128;
 #pragma unroll
         for (int i = 0; i < QV; ++i) store_query(sq, tr, half * QV + i, finite ? v[i] : make_uint4(0, 0, 0, 0), down);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&qfull[q]);
+        __syncwarp();
       }
-      fence_proxy_async_smem();
-      mbar_arrive(&qfull[q]);
-
-      const uint32_t to = tmem + C::TO + q * D + lanes;
-      float m = -INFINITY, l = 0.0f;
+      if (pending) {
+        go = mbar_wait_warp(&olast[q], (parts - 1) & 1, abort_flag, kChunkWait);
+        if (!go) break;
+        tc_fence_after();
+        if (C::NQ == 1) {
+          s_pair[kSumAt][half][tr] = l;
+          pair_any(pair, false);
+          go = !gone();
+          if (!go) break;
+          l = s_pair[kSumAt][0][tr] + s_pair[kSumAt][1][tr];
+        }
+        const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+        __nv_bfloat16* dst = a.out + row * a.out_stride + (size_t)qh * D;
+        float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + q * 128 + tr;
+        constexpr int W = C::NQ == 2 ? D : D / 2;
+#pragma unroll 1
+        for (int d = half * W; d < (half + 1) * W; d += 32) {
+          uint32_t o[32];
+          tmem_ld32(to + d, o);
+          tmem_wait_regs(o);
+          if (valid && split) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              po[(size_t)(d / 4 + i) * C::ROWS] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                              __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+          } else if (valid) {
+            uint32_t v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(dst + d + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+          __syncwarp();  // whole again before the next load from TMEM
+        }
+        __syncwarp();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ofree[q]);
+        __syncwarp();
+        if (valid && half == 0) {
+          if (split) {
+            a.part_ml[(size_t)slot * 2 * C::ROWS + q * 128 + tr] = m;
+            a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + q * 128 + tr] = l;
+          } else if (a.lse != nullptr) {
+            a.lse[row * a.H + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+          }
+        }
+        __syncwarp();
+      }
+      if (!have) break;
+      pending = true;
+      ++parts;
+      n = part.last - part.first;
+      row = nrow;
+      qh = nqh;
+      valid = nvalid;
+      crow = ncrow;
+      split = part.first > 0 || part.last < part.tiles;
+      slot = 2 * blockIdx.x + (part.first > 0 ? 0 : 1);
+      m = -INFINITY;
+      l = 0.0f;
+      const int see = part.held - part.rows + qi;
       // tiles that every row of this row tile sees whole
       const int r_end = min(rows, part.row_tile * C::ROWS + q * 128 + 128) - 1;
       const int see_lo = part.held - part.rows + (part.row_tile * C::ROWS + q * 128) / a.G;
@@ -512,9 +589,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             }
             if (j > 0) {
               // the output so far, once the last product is in it (with two row
-              // tiles the scores of this tile came after it)
+              // tiles the scores of this tile came after it, else after the one
+              // before, so that the parity names one phase)
               if (C::NQ == 1) {
-                go = mbar_wait_warp(&ofull[0], (no - 1) & 1, abort_flag, kChunkWait);
+                go = mbar_wait_warp(&ofull[0], (ns - 2) & 1, abort_flag, kChunkWait);
                 if (!go) break;
                 tc_fence_after();
               }
@@ -553,63 +631,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&pfull[buf]);
-        ++no;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pfull[buf]);
+        __syncwarp();
       }
       kv += n;
       if (!go) break;
-      // The last product.  A parity names a phase only where the one before is
-      // known to be over: with two row tiles the last scores came after the last
-      // but one product, else only after the one before that.
-      if (C::NQ == 1 && n > 1) go = mbar_wait_warp(&ofull[q], no & 1, abort_flag, kChunkWait);
-      go = go && mbar_wait_warp(&ofull[q], (no - 1) & 1, abort_flag, kChunkWait);
-      if (!go) break;
-      tc_fence_after();
-      if (C::NQ == 1) {
-        s_pair[kSumAt][half][tr] = l;
-        pair_any(pair, false);
-        go = !gone();
-        if (!go) break;
-        l = s_pair[kSumAt][0][tr] + s_pair[kSumAt][1][tr];
-      }
-      const bool split = part.first > 0 || part.last < part.tiles;
-      const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-      const int slot = 2 * blockIdx.x + (part.first > 0 ? 0 : 1);
-      __nv_bfloat16* dst = a.out + row * a.out_stride + (size_t)qh * D;
-      float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + q * 128 + tr;
-      constexpr int W = C::NQ == 2 ? D : D / 2;
-#pragma unroll 1
-      for (int d = half * W; d < (half + 1) * W; d += 32) {
-        uint32_t o[32];
-        tmem_ld32(to + d, o);
-        tmem_wait_regs(o);
-        if (valid && split) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            po[(size_t)(d / 4 + i) * C::ROWS] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
-                                                            __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
-        } else if (valid) {
-          uint32_t v[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * f, __uint_as_float(o[2 * i + 1]) * f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint4*>(dst + d + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        }
-        __syncwarp();  // whole again before the next load from TMEM
-      }
-      __syncwarp();
-      tc_fence_before();
-      mbar_arrive(&ofree[q]);
-      if (valid && half == 0) {
-        if (split) {
-          a.part_ml[(size_t)slot * 2 * C::ROWS + q * 128 + tr] = m;
-          a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + q * 128 + tr] = l;
-        } else if (a.lse != nullptr) {
-          a.lse[row * a.H + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
-        }
-      }
-      __syncwarp();
     }
     if (C::NQ == 1 && gone()) pair_leave(pair);
   } else {
@@ -627,7 +654,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     uint32_t np0 = 0, np1 = 0;        // P tiles waited for, per S buffer
     uint32_t parts0 = 0, parts1 = 0;  // parts begun, per row tile
     bool go = true;
-    while (go && __any_sync(0xffffffffu, walk.next(a, part))) {
+    Part ahead;  // read a part early: its loads take as long as a tile
+    bool more = walk.next(a, ahead);
+    while (go && __any_sync(0xffffffffu, more)) {
+      part = ahead;
+      more = walk.next(a, ahead);
       const int n = (int)uniform(part.last - part.first);
       const int nq = C::NQ == 2 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > 128 ? 2 : 1;
       auto scores = [&](int q, int buf, int j, bool first_q, bool last_q) {  // S[buf] = Q[q] K(tile j)^T
@@ -662,7 +693,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           for (int k = 0; k < C::NT / 16; ++k)
             umma_f16_ts(tm + C::TO + q * D, tm + buf * C::NT + 8 * k,
                         desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, (j | k) != 0);
-          umma_commit(&ofull[q]);
+          if (C::NQ == 1) umma_commit(&ofull[0]);
+          if (j == n - 1) umma_commit(&olast[q]);
           if (last_q) umma_commit(&vempty[st]);
         }
         __syncwarp();
@@ -834,7 +866,7 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   const long long begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
   // the item that the next run begins with, if it has tiles in this one
   const int item = a.plan[4 + blockIdx.x + 1];
-  const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
+  const long long p0 = a.item_pre[item] + kItemCost<D>, p1 = a.item_pre[item + 1];
   if (p0 < begin || p0 >= end) return;
   const int parts = runs.owner(p1 - 1) - blockIdx.x + 1;
   const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
@@ -878,7 +910,7 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = smem_attr_once(kv_chunk_kernel<D, FMT, CAP>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT);
+  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT, kItemCost<D>);
   if (e != cudaSuccess) return e;
   e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(kChunkThreads), C::SMEM, s, a);
   if (e != cudaSuccess) return e;
