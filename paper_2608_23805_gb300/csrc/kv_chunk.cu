@@ -589,10 +589,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             }
             if (j > 0) {
               // the output so far, once the last product is in it (with two row
-              // tiles the scores of this tile came after it, else after the one
-              // before, so that the parity names one phase)
+              // tiles the scores of this tile came after it)
               if (C::NQ == 1) {
-                go = mbar_wait_warp(&ofull[0], (ns - 2) & 1, abort_flag, kChunkWait);
+                const uint32_t t = kv + j - 1;  // the tile before
+                go = mbar_wait_warp(&ofull[t & 1], (t >> 1) & 1, abort_flag, kChunkWait);
                 if (!go) break;
                 tc_fence_after();
               }
@@ -643,6 +643,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   set_regs<kConvRegs, false>();  // one instruction for the whole warpgroup
   if (warp == kMmaWarp) {
     // --------------------------------------------------------------- MMA issuer
+    // Issue runs little ahead of the tensor core, so what the warp does between
+    // its products shows: a row tile's output and next scores are issued in one go.
     const uint32_t desc_hi = (uint32_t)(sw128_desc(0) >> 32);
     const uint32_t q_lo = uniform((uint32_t)sw128_desc(smem_u32(sQ)));
     const uint32_t k_lo = uniform((uint32_t)sw128_desc(smem_u32(sK)));
@@ -650,69 +652,96 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const uint32_t v_lo = uniform((smem_u32(sV) >> 4) | ((uint32_t)(C::NT * 128) >> 4 << 16));
     const uint32_t tm = uniform(tmem);
     constexpr uint32_t id_s = idesc_f16(128, C::NT, 0), id_o = idesc_f16(128, D, 1);
-    uint32_t kv = 0;                  // token tiles before the part's
-    uint32_t np0 = 0, np1 = 0;        // P tiles waited for, per S buffer
-    uint32_t parts0 = 0, parts1 = 0;  // parts begun, per row tile
+    uint32_t kv = 0;        // token tiles before the part's
+    uint32_t parts[2] = {0, 0}, np[2] = {0, 0};  // of each row tile: parts and P tiles before
     bool go = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, kChunkWait); };
+    auto scores = [&](int q, uint32_t s, uint32_t st) {  // S = Q[q] K^T, one thread
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        umma_bf16(s, desc64(q_lo + ((q * C::QBYTES + (k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
+                  desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::NT * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
+    };
+    auto outputs = [&](int q, uint32_t p, uint32_t st, uint32_t add) {  // O[q] += P V, one thread
+#pragma unroll
+      for (int k = 0; k < C::NT / 16; ++k)
+        umma_f16_ts(tm + C::TO + q * D, p + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, k > 0 ? 1 : add);
+    };
     Part ahead;  // read a part early: its loads take as long as a tile
     bool more = walk.next(a, ahead);
     while (go && __any_sync(0xffffffffu, more)) {
       part = ahead;
       more = walk.next(a, ahead);
-      const int n = (int)uniform(part.last - part.first);
-      const int nq = C::NQ == 2 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > 128 ? 2 : 1;
-      auto scores = [&](int q, int buf, int j, bool first_q, bool last_q) {  // S[buf] = Q[q] K(tile j)^T
-        const uint32_t t = kv + j, st = t & 1;
-        if (first_q && !mbar_wait_warp(&kfull[st], (t >> 1) & 1, abort_flag, kChunkWait)) return false;
-        tc_fence_after();
-        if (elect_one()) {
+      const uint32_t n = uniform(part.last - part.first), t0 = uniform(kv);
+      if (C::NQ == 2) {
+        const bool two = (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > 128;
+        const uint32_t k0 = t0 & 1;
+        go = wait(&kfull[k0], t0 >> 1);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t qa = q_lo + ((q * C::QBYTES + (k >> 2) * 128 * 128 + (k & 3) * 32) >> 4);
-            const uint32_t kb = k_lo + ((st * C::KBYTES + (k >> 2) * C::NT * 128 + (k & 3) * 32) >> 4);
-            umma_bf16(tm + buf * C::NT, desc64(qa, desc_hi), desc64(kb, desc_hi), id_s, k != 0);
+        for (int q = 0; q < 2; ++q) {
+          if (!go || (q && !two)) break;
+          go = wait(&qfull[q], parts[q]);
+          if (!go) break;
+          tc_fence_after();
+          if (elect_one()) {
+            scores(q, tm + q * C::NT, k0);
+            umma_commit(&sfull[q]);
+            if (q || !two) umma_commit(&kempty[k0]);
           }
-          umma_commit(&sfull[buf]);
-          if (last_q) umma_commit(&kempty[st]);
+          __syncwarp();
         }
-        __syncwarp();
-        return true;
-      };
-      auto outputs = [&](int q, int buf, int j, bool first_q, bool last_q) {  // O[q] += P[buf] V(tile j)
-        const uint32_t t = kv + j, st = t & 1;
-        if (!mbar_wait_warp(&pfull[buf], (buf ? np1 : np0) & 1, abort_flag, kChunkWait)) return false;
-        if (buf) ++np1; else ++np0;
-        if (first_q && !mbar_wait_warp(&vfull[st], (t >> 1) & 1, abort_flag, kChunkWait)) return false;
-        if (j == 0) {
-          if (!mbar_wait_warp(&ofree[q], ((q ? parts1 : parts0) & 1) ^ 1, abort_flag, kChunkWait)) return false;
-          if (q) ++parts1; else ++parts0;
-        }
-        tc_fence_after();
-        if (elect_one()) {
+        for (uint32_t t = t0; go && t < t0 + n; ++t) {
+          const bool last = t + 1 == t0 + n;
+          const uint32_t vs = uniform(t & 1), ks = vs ^ 1;
+          go = wait(&vfull[vs], t >> 1) && (last || wait(&kfull[ks], (t + 1) >> 1));
 #pragma unroll
-          for (int k = 0; k < C::NT / 16; ++k)
-            umma_f16_ts(tm + C::TO + q * D, tm + buf * C::NT + 8 * k,
-                        desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, (j | k) != 0);
-          if (C::NQ == 1) umma_commit(&ofull[0]);
-          if (j == n - 1) umma_commit(&olast[q]);
-          if (last_q) umma_commit(&vempty[st]);
-        }
-        __syncwarp();
-        return true;
-      };
-      for (int q = 0; go && q < nq; ++q) {
-        go = mbar_wait_warp(&qfull[q], (q ? parts1 : parts0) & 1, abort_flag, kChunkWait);
-        go = go && scores(q, C::NQ == 2 ? q : kv & 1, 0, q == 0, q == nq - 1);
-      }
-      for (int j = 0; go && j < n; ++j) {
-        if (C::NQ == 2) {
-          for (int q = 0; go && q < nq; ++q) {
-            go = outputs(q, q, j, q == 0, q == nq - 1);
-            if (go && j + 1 < n) go = scores(q, q, j + 1, q == 0, q == nq - 1);
+          for (int q = 0; q < 2; ++q) {
+            if (!go || (q && !two)) break;
+            if (t == t0) go = wait(&ofree[q], parts[q]++ ^ 1);
+            go = go && wait(&pfull[q], np[q]++);
+            if (!go) break;
+            tc_fence_after();
+            if (elect_one()) {
+              outputs(q, tm + q * C::NT, vs, t != t0);
+              if (last) umma_commit(&olast[q]);
+              if (q || !two) umma_commit(&vempty[vs]);
+              if (!last) {
+                scores(q, tm + q * C::NT, ks);
+                umma_commit(&sfull[q]);
+                if (q || !two) umma_commit(&kempty[ks]);
+              }
+            }
+            __syncwarp();
           }
-        } else {
-          if (j + 1 < n) go = scores(0, (kv + j + 1) & 1, j + 1, true, true);
-          go = go && outputs(0, (kv + j) & 1, j, true, true);
+        }
+      } else {
+        auto first = [&](uint32_t t) {
+          go = go && wait(&kfull[t & 1], t >> 1);
+          if (!go) return;
+          tc_fence_after();
+          if (elect_one()) {
+            scores(0, tm + (t & 1) * C::NT, t & 1);
+            umma_commit(&sfull[t & 1]);
+            umma_commit(&kempty[t & 1]);
+          }
+          __syncwarp();
+        };
+        go = wait(&qfull[0], parts[0]);
+        first(t0);
+        go = go && wait(&ofree[0], parts[0]++ ^ 1);
+        for (uint32_t t = t0; go && t < t0 + n; ++t) {
+          const bool last = t + 1 == t0 + n;
+          if (!last) first(t + 1);
+          go = go && wait(&vfull[t & 1], t >> 1) && wait(&pfull[t & 1], t >> 1);
+          if (!go) break;
+          tc_fence_after();
+          if (elect_one()) {
+            outputs(0, tm + (t & 1) * C::NT, t & 1, t != t0);
+            umma_commit(&ofull[t & 1]);
+            if (last) umma_commit(&olast[0]);
+            umma_commit(&vempty[t & 1]);
+          }
+          __syncwarp();
         }
       }
       kv += n;
@@ -721,8 +750,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     __syncwarp();
     if (elect_one()) {
       umma_commit(drain);
-      const long long t0 = clock64();
-      while (!mbar_try_wait(drain, 0) && clock64() - t0 < kDrainCycles) {
+      const long long since = clock64();
+      while (!mbar_try_wait(drain, 0) && clock64() - since < kDrainCycles) {
       }
     }
   } else {
