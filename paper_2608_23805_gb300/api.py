@@ -408,7 +408,7 @@ class KvCache:
         self.h = h
         self._lib = lib
         self._device = self.table.device
-        self._ws = None
+        self._ws = self._ws_on = None  # workspace, and the stream that it was last used on
         self._need = {}
         if buffers is None:
             self.init(stream)
@@ -498,9 +498,14 @@ class KvCache:
         ws = self._ws
         if ws is None or ws.numel() < need:
             ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+            self._ws_on = None
         if stream is not None:
-            self._used_on(stream, out, lse, ws)
-        rc = self._lib.msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), self._on(stream))
+            self._used_on(stream, out, lse)
+        on = self._on(stream)
+        if on != self._ws_on:
+            ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self._ws_on = on
+        rc = self._lib.msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), on)
         if rc:
             N.check(rc, "msi_kv_attention")
         return out, lse
