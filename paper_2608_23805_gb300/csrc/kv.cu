@@ -674,6 +674,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;
   const int tiles = kv_decode_tiles(a.max_rows * a.G, c.D);
   if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
+  if (tiles != 0) a.groups = (a.max_rows * a.G + 8 * tiles - 1) / (8 * tiles);
   a.ctas = kv->sms < 512 ? kv->sms : 512;
   if (tiles != 0) a.ctas *= 2;  // two of the decode form's share an SM
   size_t at = 0;
@@ -697,7 +698,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
     a.item_pre = reinterpret_cast<long long*>(take(((size_t)a.n + 1) * sizeof(long long)));
     a.lse2 = reinterpret_cast<float*>(take((size_t)a.n_rows * a.H * 4));
     // no block belongs to two sequences: the pool bounds the steps
-    a.max_steps = ((long long)c.n_blocks * (c.P / 16) + (long long)a.n * kv_decode_pair_cost()) * c.K;
+    a.max_steps = ((long long)c.n_blocks * (c.P / 16) + (long long)a.n * kv_decode_pair_cost()) * c.K * a.groups;
     a.step_lse = reinterpret_cast<float*>(take((size_t)a.max_steps * rows * 4));
   }
   *bytes = at;

@@ -66,6 +66,7 @@ struct KvAttnArgs {
   float scale, softcap;
   int window, observe;
   int ctas;            // CTAs that share the work
+  int groups;          // decode form: most groups of rows of a sequence and head
   // workspace
   float* part_o;       // [2 ctas][rows][D] unnormalised outputs of the parts of split items
   float* part_ml;      // [2 ctas][2][rows] their reference exponents and sums
@@ -87,7 +88,7 @@ cudaError_t launch_kv_init(const KvCache& c, cudaStream_t s);
 // Decode form: rows of one sequence and key-value head (its part of the query
 // heads) as columns of the MMA.
 int kv_decode_pair_cost();               // units of work that a pair is counted beside its steps
-int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4), 0: not in decode form
+int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4) of a group of rows, 0: not in decode form
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s);
 // Chunk form: rows of one sequence and key-value head in tiles of the MMA's rows.
 int kv_chunk_rows(int D);  // rows of an item

@@ -1,6 +1,6 @@
 // Attention over the 8-bit key-value cache in decode form: the rows of one
-// sequence and key-value head (its query heads times a few tokens, R <= 32)
-// against everything that the sequence holds.
+// sequence and key-value head (its query heads times a few tokens, in groups of
+// R <= 32) against everything that the sequence holds.
 //
 // Mathematics.  With codes c and scales sk, sv of a token's block and head, a
 // row's score is s = scale * sk * (q . ck), its weight p = 2^(s log2 e - M), and
@@ -38,8 +38,9 @@ constexpr float kLazy = 8.0f;  // P may reach 2^8
 // CTAs share an SM, so that one reads while the other begins or ends a pair.
 __host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 8 : 4; }
 // What a pair costs a CTA beside its steps (queries, first loads, the warps'
-// sums), in steps.
-constexpr int kPairCost = 8;
+// sums), in steps.  12 sequences of 20,000, D = 256, 4 tokens: 56.6, 55.2, 49.6,
+// 46.7, 47.6 us at 0, 8, 32, 48, 96; 64 of 8,192: 45.7, 45.6, 46.0, 44.4, 45.9.
+constexpr int kPairCost = 48;
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
 // Stages of a warp's ring: 96 KB a CTA, at most 8.
 __host__ __device__ constexpr int dec_stages(int D, int NT) {
@@ -49,10 +50,12 @@ __host__ __device__ constexpr int dec_stages(int D, int NT) {
 
 // A pair's units of work: its fixed cost, then its steps.
 __device__ __forceinline__ int kv_units(const KvWork& w) { return w.steps > 0 ? w.steps + kPairCost : 0; }
+// Pairs of a sequence and head: groups of R rows.
+__device__ __forceinline__ int kv_groups(const KvAttnArgs& a, const KvWork& w, int R) { return (w.rows * a.G + R - 1) / R; }
 
 // The batch's work: s_pre[b] = units of the pairs before sequence b, over all
 // heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
-__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, long long* s_sum, int* s_bad) {
+__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, int R, long long* s_pre, long long* s_sum, int* s_bad) {
   const int tid = threadIdx.x, T = blockDim.x, lane = tid & 31, wid = tid >> 5;
   const int per = (a.n + T - 1) / T, b0 = min(a.n, tid * per), b1 = min(a.n, b0 + per);
   if (tid == 0) *s_bad = 0;
@@ -61,7 +64,7 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
   for (int b = b0; b < b1; ++b) {
     const KvWork w = kv_work(a, b);
     if (!w.ok) *s_bad = 1;
-    mine += (long long)kv_units(w) * a.c.K;
+    mine += (long long)kv_units(w) * a.c.K * (w.ok ? kv_groups(a, w, R) : 0);
   }
   long long v = mine;
 #pragma unroll
@@ -75,7 +78,8 @@ __device__ __forceinline__ bool kv_share(const KvAttnArgs& a, long long* s_pre, 
   for (int i = 0; i < wid; ++i) before += s_sum[i];
   for (int b = b0; b < b1; ++b) {
     s_pre[b] = before;
-    before += (long long)kv_units(kv_work(a, b)) * a.c.K;
+    const KvWork w = kv_work(a, b);
+    before += (long long)kv_units(w) * a.c.K * (w.ok ? kv_groups(a, w, R) : 0);
   }
   if (b0 < a.n && b1 == a.n) s_pre[a.n] = before;
   __syncthreads();
@@ -136,7 +140,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
   grid_release();
 
   const int status = c.control[1];
-  const bool ok = kv_share(a, s_pre, s_sum, &s_bad);
+  const bool ok = kv_share(a, R, s_pre, s_sum, &s_bad);
   const long long total = s_pre[a.n];
   if (tid == 0) a.split[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (OBS && blockIdx.x == 0)
@@ -190,8 +194,9 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
   while (u < u_end) {
     while (s_pre[b + 1] <= u) ++b;
     const KvWork w = kv_work(a, b);
-    const int units = kv_units(w), h = (int)((u - s_pre[b]) / units);
-    const long long item0 = s_pre[b] + (long long)h * units + kPairCost;  // the first step
+    const int units = kv_units(w), groups = kv_groups(a, w, R), pair = (int)((u - s_pre[b]) / units);
+    const int h = pair / groups, r0 = (pair - h * groups) * R;  // head, the pair's first row of it
+    const long long item0 = s_pre[b] + (long long)pair * units + kPairCost;  // the first step
     const int first = (int)max(u - item0, 0LL);
     const int last = (int)(min(item0 + w.steps, u_end) - item0);  // steps [first, last) of the pair are this CTA's
     u = item0 + last;
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
       u = u_end;
       break;
     }
-    const int n_rows = w.rows * a.G;
+    const int n_rows = min(R, w.rows * a.G - r0);
     const bool cap = a.softcap > 0.0f;
     const int* table = c.table + (size_t)w.seq * c.max_blocks;
 
@@ -215,8 +220,8 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
       for (int j = 0; j < CH; ++j) {
         v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
         if (r < n_rows) {
-          const __nv_bfloat16* p = a.q + (long long)(w.row0 + r / a.G) * a.q_stride +
-                                   (size_t)(h * a.G + r % a.G) * D + dec_kchunk<D>(t, j) * 16;
+          const __nv_bfloat16* p = a.q + (long long)(w.row0 + (r0 + r) / a.G) * a.q_stride +
+                                   (size_t)(h * a.G + (r0 + r) % a.G) * D + dec_kchunk<D>(t, j) * 16;
           v[j][0] = *reinterpret_cast<const uint4*>(p);
           v[j][1] = *reinterpret_cast<const uint4*>(p + 8);
         }
@@ -363,7 +368,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
           for (int q = 0; q < 4; ++q) {
             const int tok = tok0 + g + (q >> 1) * 8;
             // the last token that the row sees
-            const int see = w.held - w.rows + (8 * nt + 2 * t + (q & 1)) / a.G;
+            const int see = w.held - w.rows + (r0 + 8 * nt + 2 * t + (q & 1)) / a.G;
             if (tok > see || (a.window > 0 && tok <= see - a.window)) sc[nt][q] = -INFINITY;
           }
       }
@@ -502,10 +507,10 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
         *reinterpret_cast<float2*>(a.part_o + ((size_t)slot * R + r) * D + d) = make_float2(x, y);
         if (d == 0) a.part_ml[(size_t)slot * 2 * R + r] = top, a.part_ml[(size_t)slot * 2 * R + R + r] = sum;
         if (e == 0 && first == 0)
-          a.split[blockIdx.x] = make_int4(w.row0, n_rows, h, runs.owner(item0 + w.steps - 1) - blockIdx.x + 1);
+          a.split[blockIdx.x] = make_int4(w.row0, n_rows | r0 << 8, h, runs.owner(item0 + w.steps - 1) - blockIdx.x + 1);
       } else {
-        const long long row = w.row0 + r / a.G;
-        const int head = h * a.G + r % a.G;
+        const long long row = w.row0 + (r0 + r) / a.G;
+        const int head = h * a.G + (r0 + r) % a.G;
         const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
         *reinterpret_cast<uint32_t*>(a.out + row * a.out_stride + (size_t)head * D + d) = pack_bf16x2(x * f, y * f);
         if (d == 0) {
@@ -528,11 +533,12 @@ template <int D>
 __device__ __forceinline__ void kv_join_few(const KvAttnArgs& a, int R, int x, int r) {
   constexpr int V = D / 32, B = 8;  // a lane's columns, parts loaded at a time
   const int lane = threadIdx.x & 31;
-  const int4 at = a.split[x];  // first row, rows, head, parts
+  const int4 at = a.split[x];  // first row, rows and the first of them, head, parts
   const int parts = at.w;
-  if (r >= at.y || parts == 0 || parts > kJoinFew) return;
-  const long long row = at.x + r / a.G;
-  const int head = at.z * a.G + r % a.G;
+  if (r >= (at.y & 255) || parts == 0 || parts > kJoinFew) return;
+  const int hr = (at.y >> 8) + r;  // row of the head
+  const long long row = at.x + hr / a.G;
+  const int head = at.z * a.G + hr % a.G;
   const bool failed = a.c.control[1] != 0;  // within the call
   auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
   const float pm = lane < parts ? a.part_ml[slot_of(lane) * 2 * R + r] : -INFINITY;
@@ -589,11 +595,12 @@ __device__ __forceinline__ void kv_join_many(const KvAttnArgs& a, int R, int n, 
   }
   const int x = s_x;
   if (x < 0) return;
-  const int4 at = a.split[x];  // first row, rows, head, parts
+  const int4 at = a.split[x];  // first row, rows and the first of them, head, parts
   const int parts = at.w;
-  if (r >= at.y) return;
-  const long long row = at.x + r / a.G;
-  const int head = at.z * a.G + r % a.G;
+  if (r >= (at.y & 255)) return;
+  const int hr = (at.y >> 8) + r;  // row of the head
+  const long long row = at.x + hr / a.G;
+  const int head = at.z * a.G + hr % a.G;
   const bool failed = a.c.control[1] != 0;  // within the call
   auto slot_of = [&](int i) { return (size_t)(2 * (x + i) + (i == 0 ? 1 : 0)); };
   float mi[4], li[4];  // this thread's parts: 1,024 CTAs at most
@@ -661,11 +668,11 @@ __device__ __forceinline__ void kv_join_many(const KvAttnArgs& a, int R, int n, 
 // blocks lie together, so a lane takes four rows of one granule for every head,
 // and a warp the blocks that 128 of these sums hold (or one block, in passes).
 // Lanes are added in one order.  `warps` warps, of which this is the wid-th.
-// s_top: [K][R] log2 of the rows' sums; -inf: a row that is none.
+// s_top: [pairs][R] log2 of the rows' sums; -inf: a row that is none.
 __device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w, long long pre, int R, const float* s_top, int wid,
                                            int warps) {
   const KvCache& c = a.c;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, pairs = c.K * kv_groups(a, w, R);
   const int per = c.P / 16, sums = per * R;                // of a block and head: 8 .. 256, a power of two
   const int nb = sums >= 128 ? 1 : 128 / sums;             // blocks of a warp's turn
   const int lanes = sums >= 128 ? 32 : sums / 4;           // lanes of a block
@@ -682,7 +689,7 @@ __device__ __forceinline__ void kv_weights(const KvAttnArgs& a, const KvWork& w,
       if (step < 0 || step >= w.steps) continue;
       const float* p = a.step_lse + (pre + kPairCost + step) * R + r;
 #pragma unroll 4
-      for (int h = 0; h < c.K; ++h) {
+      for (int h = 0; h < pairs; ++h) {
         const float4 x = *reinterpret_cast<const float4*>(p + (long long)h * kv_units(w) * R);
         const float4 t = *reinterpret_cast<const float4*>(s_top + h * R + r);
         if (t.x != -INFINITY) v += ex2(x.x - t.x);
@@ -717,17 +724,17 @@ __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, i
   const KvWork w = kv_work(a, b);
   const long long pre = a.item_pre[b], total = a.item_pre[a.n];
   if (c.control[1] != 0 || w.steps == 0) return;
-  const int n = w.rows * a.G;
+  const int n = w.rows * a.G, groups = kv_groups(a, w, R);
   const KvRuns runs = {total, kv_ctas(total, a.ctas, warps)};
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  for (int i = wid; i < c.K * R; i += kJoinThreads / 32) {  // a warp a row
-    const int h = i / R, r = i - h * R;
+  for (int i = wid; i < c.K * groups * R; i += kJoinThreads / 32) {  // a warp a row
+    const int pair = i / R, r = i - pair * R, h = pair / groups, hr = (pair - h * groups) * R + r;
     float l2 = -INFINITY;
-    if (r < n) {
-      const long long u0 = pre + (long long)h * kv_units(w) + kPairCost;
+    if (hr < n) {
+      const long long u0 = pre + (long long)pair * kv_units(w) + kPairCost;
       const int c0 = runs.owner(u0), c1 = runs.owner(u0 + w.steps - 1);
       if (c0 == c1) {
-        l2 = a.lse2[(long long)(w.row0 + r / a.G) * a.H + h * a.G + r % a.G];
+        l2 = a.lse2[(long long)(w.row0 + hr / a.G) * a.H + h * a.G + hr % a.G];
       } else {
         float top = -INFINITY, sum = 0.0f;
         for (int x = c0 + lane; x <= c1; x += 32) {
@@ -766,7 +773,7 @@ cudaError_t decode_as(const KvAttnArgs& a, cudaStream_t s) {
   const int sums = a.c.P / 16 * 8 * NT, per = kJoinThreads / 32 * (sums >= 128 ? 1 : 128 / sums);
   const int ny = min((min(a.c.max_blocks, a.c.n_blocks) + per - 1) / per, 64);
   return launch_after(true, kv_finish_kernel<D>, dim3(joins + (OBS ? a.n * ny : 0)), dim3(kJoinThreads),
-                      OBS ? a.c.K * 8 * NT * sizeof(float) : 0, s, a, 8 * NT, W, joins, ny);
+                      OBS ? a.c.K * a.groups * 8 * NT * sizeof(float) : 0, s, a, 8 * NT, W, joins, ny);
 }
 
 template <int D, int NT, int FMT>
@@ -783,15 +790,22 @@ cudaError_t decode_fmt(const KvAttnArgs& a, cudaStream_t s) {
 
 int kv_decode_pair_cost() { return kPairCost; }
 
+// More rows than a group holds are several pairs: each reads the codes again, but
+// mostly from L2 (64 sequences of 8,192, D = 128: 63 us for 16 rows, 101 for 32 in
+// two groups, against 157 in one group of 32, whose registers spill; D = 64: 60
+// for 32 in one).  Chunk form takes over where it is as fast for many sequences
+// (D = 128, 48 rows 146 us, 56 rows in chunk form 141; D = 256 263 and 269; D = 64,
+// 64 rows 97 and 72 rows 127); for one sequence of 32,768 decode form has 22, 33
+// and 21 us there, chunk form 66, 88 and 51.
 int kv_decode_tiles(int rows, int D) {
-  return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 && D < 256 ? 4 : 0;
+  return rows <= 8 ? 1 : rows <= 16 ? 2 : D == 64 ? (rows <= 64 ? 4 : 0) : rows <= 48 ? 2 : 0;
 }
 
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   const int nt = kv_decode_tiles(a.max_rows * a.G, a.c.D);
   *launches = 2;
   if (a.c.D == 64) return nt == 1 ? decode_fmt<64, 1>(a, s) : nt == 2 ? decode_fmt<64, 2>(a, s) : decode_fmt<64, 4>(a, s);
-  if (a.c.D == 128) return nt == 1 ? decode_fmt<128, 1>(a, s) : nt == 2 ? decode_fmt<128, 2>(a, s) : decode_fmt<128, 4>(a, s);
+  if (a.c.D == 128) return nt == 1 ? decode_fmt<128, 1>(a, s) : decode_fmt<128, 2>(a, s);
   return nt == 1 ? decode_fmt<256, 1>(a, s) : decode_fmt<256, 2>(a, s);
 }
 
