@@ -906,23 +906,39 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   const int dw = threadIdx.x >> 5;  // this warp's columns: 4 dw, + 32, ..
   const bool failed = c.control[1] != 0;
   auto slot_of = [&](int i) { return (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)); };
+  // several parts' loads on their way at once: an item of few rows and many
+  // tokens has up to a part a CTA
   float top = -INFINITY, sum = 0.0f;
+#pragma unroll 8
   for (int i = 0; i < parts; ++i) top = fmaxf(top, a.part_ml[slot_of(i) * 2 * C::ROWS + tr]);
   float4 acc[D / 32];
 #pragma unroll
   for (int k = 0; k < D / 32; ++k) acc[k] = make_float4(0, 0, 0, 0);
-  for (int i = 0; i < parts; ++i) {
-    const float mi = a.part_ml[slot_of(i) * 2 * C::ROWS + tr], li = a.part_ml[slot_of(i) * 2 * C::ROWS + C::ROWS + tr];
-    const float f = mi == -INFINITY ? (li == 0.0f ? 0.0f : li) : ex2(mi - top);
-    sum += mi == -INFINITY ? li : li * f;
-    const float4* po = reinterpret_cast<const float4*>(a.part_o) + slot_of(i) * (D / 4) * C::ROWS + tr;
+  constexpr int B = D == 256 ? 2 : 4;
+  for (int i0 = 0; i0 < parts; i0 += B) {
+    float4 v[B][D / 32];
+    float mi[B], li[B];
 #pragma unroll
-    for (int k = 0; k < D / 32; ++k) {
-      const float4 v = po[(size_t)(dw + 8 * k) * C::ROWS];
-      acc[k].x = fmaf(f, v.x, acc[k].x);
-      acc[k].y = fmaf(f, v.y, acc[k].y);
-      acc[k].z = fmaf(f, v.z, acc[k].z);
-      acc[k].w = fmaf(f, v.w, acc[k].w);
+    for (int b = 0; b < B; ++b) {
+      const bool there = i0 + b < parts;
+      const size_t slot = slot_of(there ? i0 + b : 0);
+      mi[b] = there ? a.part_ml[slot * 2 * C::ROWS + tr] : -INFINITY;
+      li[b] = there ? a.part_ml[slot * 2 * C::ROWS + C::ROWS + tr] : 0.0f;
+      const float4* po = reinterpret_cast<const float4*>(a.part_o) + slot * (D / 4) * C::ROWS + tr;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) v[b][k] = there ? po[(size_t)(dw + 8 * k) * C::ROWS] : make_float4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const float f = mi[b] == -INFINITY ? (li[b] == 0.0f ? 0.0f : li[b]) : ex2(mi[b] - top);
+      sum += mi[b] == -INFINITY ? li[b] : li[b] * f;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        acc[k].x = fmaf(f, v[b][k].x, acc[k].x);
+        acc[k].y = fmaf(f, v[b][k].y, acc[k].y);
+        acc[k].z = fmaf(f, v[b][k].z, acc[k].z);
+        acc[k].w = fmaf(f, v[b][k].w, acc[k].w);
+      }
     }
   }
   const float f = failed ? kv_nan() : sum == 0.0f ? 0.0f : 1.0f / sum;
