@@ -89,8 +89,9 @@ __device__ __forceinline__ uint32_t round_e4m3(uint32_t a, uint32_t b, float inv
 // A block of one head, keys or values, is a task: rounded in one pass over its
 // rows, which stay in registers between the maximum and the rounding.  A CTA
 // takes every gridDim-th task, so that the bookkeeping is paid for once in
-// several blocks.  Bound: memory (16-bit rows in, codes out) for prompts,
-// latency for single tokens.
+// several blocks.  Bound: memory (16-bit rows in, codes out) for prompts (32,768
+// tokens of 2 heads of 128: 14 us, 3.6 TB/s), latency for single tokens (64
+// sequences: 6 us).
 constexpr int append_threads(int vpt) { return vpt <= 4 ? 1024 : 512; }  // of an SM, by the registers a thread takes
 
 template <int THREADS, int VPT>
@@ -303,7 +304,9 @@ __device__ __forceinline__ unsigned kv_key(float w) {
 // then the later block), which takes two barriers each, and the entries after
 // them move down.  More: the threshold weight by a radix selection (four passes
 // over 8 bits, whole-number histograms, so the result does not depend on any
-// order), then one pass over the table in order that keeps or frees.  Bound:
+// order), then one pass over the table in order that keeps or frees.  64 sequences
+// of 257 blocks that give up one, with the append before: 13.0 us, 17.1 by the
+// radix selection; three of 4,004 that give up four: 14.5 and 21.6.  Bound:
 // latency (dependent passes over a few KB).
 __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(KvEvictArgs a) {
   extern __shared__ unsigned s_key[];

@@ -26,6 +26,11 @@
 // pairs; each CTA takes an equal run of it, whatever the lengths.  A pair that
 // lies in one CTA is finished there; parts of split ones are joined by
 // kv_finish_kernel in the CTAs' order, so results do not depend on timing.
+//
+// Measured: 64 sequences of 8,192, 2 heads of 128 with 8 query heads each, block
+// weights added up: 44 us, 3.6 TB/s of codes and scales; one of 32,768: 15 us.
+// Bound: issue slots and latency (about 500 instructions a step, half of them
+// conversions and byte interleaving; without the copies 0.86 of the time).
 #include "kv.cuh"
 
 namespace msi {
@@ -34,7 +39,8 @@ namespace {
 constexpr float kLazy = 8.0f;  // P may reach 2^8
 
 // Warps of a CTA, by the registers that a warp's outputs and queries take
-// (D x 8 NT of each): the more the better hidden are a step's latencies.  Two
+// (D x 8 NT of each): the more the better hidden are a step's latencies (D = 128,
+// 8 rows, 64 sequences of 8,192: 45.6 us with 8 warps, 46.9 with 4).  Two
 // CTAs share an SM, so that one reads while the other begins or ends a pair.
 __host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 8 : 4; }
 // What a pair costs a CTA beside its steps (queries, first loads, the warps'
@@ -525,7 +531,9 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
 }
 
 // Joins the parts of the pair that begins in run x and goes on past it: weights
-// 2^(M_i - M) over the parts, in the CTAs' order.  Bound: latency.
+// 2^(M_i - M) over the parts, in the CTAs' order.  Bound: latency (with the kernel
+// before, 64 sequences of 8,192 take 45.6 us by warps and 49.8 by CTAs, one of
+// 1,000 8.8 and 13.5; a warp has one lane a part, so more than 32 go to a CTA).
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinFew = 32;
 
 // Up to 32 parts: a warp a row, no barriers.
