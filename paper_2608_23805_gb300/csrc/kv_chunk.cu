@@ -42,17 +42,25 @@ constexpr float kChunkTop = 2048.0f;            // sums of 16 weights above it m
 
 template <int D>
 struct Chunk {
-  static constexpr int NQ = D == 256 ? 1 : 2;     // row tiles of 128
-  static constexpr int NT = D == 256 ? 64 : 128;  // tokens of a tile
-  static constexpr int ROWS = 128 * NQ;
+  static constexpr bool PAIR = D >= 128;          // two CTAs on one item
+  static constexpr int NQ = D == 256 ? 1 : 2;     // row tiles
+  static constexpr int NT = 128;                  // tokens of a tile
+  static constexpr int TROWS = PAIR ? 256 : 128;  // rows of a row tile, 128 a CTA
+  static constexpr int ROWS = TROWS * NQ;
   static constexpr int NG = NT / 16;              // 16-token granules
   static constexpr int COLS = NQ == 2 ? NT : NT / 2;  // S columns a softmax thread takes
-  static constexpr int QBYTES = 128 * D * 2;      // one row tile
-  static constexpr int KBYTES = NT * D * 2;
+  static constexpr int KROWS = PAIR ? NT / 2 : NT;    // a CTA's tokens of the keys,
+  static constexpr int VCOLS = PAIR ? D / 2 : D;      // and columns of the values
+  static constexpr int QBYTES = 128 * D * 2;      // a CTA's part of a row tile
+  static constexpr int KBYTES = KROWS * D * 2;    // and of a tile's keys, or values
   static constexpr int SMEM = NQ * QBYTES + 4 * KBYTES + 1024;
-  // a conversion task: 16 tokens, up to 128 columns; 8 of them an operand and tile
-  static constexpr int TC = D < 128 ? D : 128;
-  static constexpr int LOADS = TC / 32;           // 16-byte loads a lane
+  // conversion tasks: 16 tokens of keys, up to 128 columns; 16 tokens of values, or 32 of 64 columns
+  static constexpr int KC = D < 128 ? D : 128, VC = VCOLS < 128 ? VCOLS : 128;
+  static constexpr int SUB = D / KC;              // tasks of 16 tokens' keys
+  static constexpr int VT = PAIR && VC == 64 ? 32 : 16;
+  static constexpr int KTASKS = KROWS / 16 * SUB, VTASKS = NT / VT;
+  static constexpr int LOADS = KC / 32;           // 16-byte loads a lane
+  static_assert(VT * VC == 16 * KC && VC == VCOLS, "all tasks of one size");
   static constexpr int TO = 256;                  // first column of O in TMEM
 };
 // 8 softmax warps, 7 conversion warps, the MMA warp; the groups share 512 x 128
@@ -65,7 +73,7 @@ static_assert(kChunkThreads == 512 && 2 * kSoftRegs + 2 * kConvRegs <= 512, "reg
 // D = 256, 4 sequences of 3,000 on 3,000: 562, 473, 454, 470 us at 2, 4, 6, 8; 128
 // columns or fewer, where a long item hides it: 826 us at 1, 2 and 4.
 template <int D>
-constexpr int kItemCost = D == 256 ? 6 : 2;
+constexpr int kItemCost = D == 256 ? 3 : 2;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
   uint64_t d;
@@ -82,6 +90,16 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same for both CTAs of a pair: each has its rows of A and its columns of B.
+__device__ __forceinline__ void umma_f16_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                                 uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // kind::f16 with fp16 operands and fp32 sums; mn: B's columns are contiguous
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int mn) {
   return (1u << 4) | ((uint32_t)mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -95,14 +113,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
       "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
       "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
       "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "
-      "%13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -138,7 +148,10 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
   s_base[tid] = in - tiles;
   if (tid == kPlanThreads - 1) s_base[kPlanThreads] = in;
   __syncthreads();
-  const bool ok = s_bad == 0 && s_base[kPlanThreads] <= a.max_items;
+  // one CTA reads the status word for all: it may change while the others start
+  const int status = c.control[1];
+  const bool ok = s_bad == 0 && s_base[kPlanThreads] <= a.max_items && status == 0;
+  if (!ok && status == 0 && tid == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
   const int items = ok ? s_base[kPlanThreads] : 0;
   for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
     const int i = i0 + tid;
@@ -377,19 +390,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   uint8_t* sQ = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sK = sQ + C::NQ * C::QBYTES;
   uint8_t* sV = sK + 2 * C::KBYTES;
+  const int rank = C::PAIR ? (int)cluster_ctarank() : 0, run = C::PAIR ? blockIdx.x >> 1 : blockIdx.x;
   uint64_t *kfull = s_bar, *kempty = s_bar + 2, *vfull = s_bar + 4, *vempty = s_bar + 6;
   uint64_t *qfull = s_bar + 8, *sfull = s_bar + 10, *pfull = s_bar + 12, *ofull = s_bar + 14, *ofree = s_bar + 16;
   uint64_t *olast = s_bar + 18, *drain = s_bar + 20;  // ofull: every product's end; olast: that of a part's last
+  // What the MMA warp waits for (kfull, vfull, qfull, pfull, ofree) is counted at
+  // the first CTA of a pair, for both; what it signals arrives at both.
+  const uint32_t lead = C::PAIR ? mapa_shared(smem_u32(s_bar), 0) : smem_u32(s_bar);
+  const uint32_t lead_qfull = lead + 8 * 8, lead_pfull = lead + 12 * 8, lead_ofree = lead + 16 * 8;
   volatile int* abort_flag = &s_abort;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
-    const int soft = C::NQ == 2 ? 4 : 8;  // warps of a row tile
+    const int both = C::PAIR ? 2 : 1, soft = both * (C::NQ == 2 ? 4 : 8);  // warps of a row tile
     for (int i = 0; i < 2; ++i) {
-      mbar_init(kfull + i, 8);
+      mbar_init(kfull + i, both * C::KTASKS);
       mbar_init(kempty + i, 1);
-      mbar_init(vfull + i, 8);
+      mbar_init(vfull + i, both * C::VTASKS);
       mbar_init(vempty + i, 1);
       mbar_init(qfull + i, soft);
       mbar_init(sfull + i, 1);
@@ -403,20 +421,23 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     s_abort = 0;
   }
   if (warp == kMmaWarp) {
-    tmem_alloc(&s_tmem, 512);
-    tmem_relinquish();
+    if (C::PAIR) {
+      tmem_alloc_pair(&s_tmem, 512);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(&s_tmem, 512);
+      tmem_relinquish();
+    }
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = s_tmem;
   grid_wait();
   grid_release();
-
-  const int status = c.control[1];
-  const bool ok = a.plan[1] != 0 && status == 0;
+  tc_fence_before();
+  __syncthreads();
+  if (C::PAIR) cluster_sync_all();  // also: both CTAs' barriers are there before any arrival from the other
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const bool ok = a.plan[1] != 0;
   if (!ok) {
-    if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
     // fail closed: no row of the call can be read as an answer
     const long long vecs = (long long)a.n_rows * a.H * (D / 8);
     for (long long i = (long long)blockIdx.x * kChunkThreads + tid; i < vecs; i += (long long)gridDim.x * kChunkThreads) {
@@ -431,7 +452,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   __syncthreads();  // every warp whole again before the register split
   PartWalk<kItemCost<D>> walk;
   walk.u = walk.end = 0;
-  if (ok && a.plan[0] > 0 && (int)blockIdx.x < a.plan[2]) walk.init(a, blockIdx.x);
+  if (ok && a.plan[0] > 0 && run < a.plan[2]) walk.init(a, run);
   Part part;
 
   if (warp < kSoftWarps) {
@@ -441,6 +462,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const int q = C::NQ == 2 ? warp >> 2 : 0, half = C::NQ == 2 ? 0 : warp >> 2;
     const int tr = tid & 127;  // row in the row tile
     const int pair = 1 + (warp & 3);
+    const int lr = q * C::TROWS + rank * 128;  // the CTA's first row of the row tile, in the item's
     constexpr int kTopAt = C::NQ == 1 ? 1 : 0, kSumAt = C::NQ == 1 ? 2 : 0;
     auto gone = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0) != 0; };
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -457,14 +479,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     while (true) {
       bool have = false;
       while (go && walk.next(a, part)) {
-        if (q > 0 && part.rows * a.G - part.row_tile * C::ROWS <= 128) {  // no second row tile
+        if (q > 0 && part.rows * a.G - part.row_tile * C::ROWS <= C::TROWS) {  // no second row tile
           kv += part.last - part.first;
           continue;
         }
         have = true;
         break;
       }
-      const int rows = part.rows * a.G, r = part.row_tile * C::ROWS + q * 128 + tr;
+      const int rows = part.rows * a.G, r = part.row_tile * C::ROWS + lr + tr;
       const bool nvalid = have && r < rows;
       const int qi = nvalid ? r / a.G : part.rows - 1, nqh = part.h * a.G + (nvalid ? r - qi * a.G : 0);
       const long long nrow = part.row0 + qi;
@@ -500,7 +522,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         for (int i = 0; i < QV; ++i) store_query(sq, tr, half * QV + i, finite ? v[i] : make_uint4(0, 0, 0, 0), down);
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&qfull[q]);
+        if (lane == 0) mbar_arrive_remote(lead_qfull + 8 * q);
         __syncwarp();
       }
       if (pending) {
@@ -516,7 +538,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         }
         const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
         __nv_bfloat16* dst = a.out + row * a.out_stride + (size_t)qh * D;
-        float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + q * 128 + tr;
+        float4* po = reinterpret_cast<float4*>(a.part_o) + (size_t)slot * (D / 4) * C::ROWS + lr + tr;
         constexpr int W = C::NQ == 2 ? D : D / 2;
 #pragma unroll 1
         for (int d = half * W; d < (half + 1) * W; d += 32) {
@@ -541,12 +563,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         __syncwarp();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&ofree[q]);
+        if (lane == 0) mbar_arrive_remote(lead_ofree + 8 * q);
         __syncwarp();
         if (valid && half == 0) {
           if (split) {
-            a.part_ml[(size_t)slot * 2 * C::ROWS + q * 128 + tr] = m;
-            a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + q * 128 + tr] = l;
+            a.part_ml[(size_t)slot * 2 * C::ROWS + lr + tr] = m;
+            a.part_ml[(size_t)slot * 2 * C::ROWS + C::ROWS + lr + tr] = l;
           } else if (a.lse != nullptr) {
             a.lse[row * a.H + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
           }
@@ -562,13 +584,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       valid = nvalid;
       crow = ncrow;
       split = part.first > 0 || part.last < part.tiles;
-      slot = 2 * blockIdx.x + (part.first > 0 ? 0 : 1);
+      slot = 2 * run + (part.first > 0 ? 0 : 1);
       m = -INFINITY;
       l = 0.0f;
       const int see = part.held - part.rows + qi;
       // tiles that every row of this row tile sees whole
-      const int r_end = min(rows, part.row_tile * C::ROWS + q * 128 + 128) - 1;
-      const int see_lo = part.held - part.rows + (part.row_tile * C::ROWS + q * 128) / a.G;
+      const int r_end = min(rows, part.row_tile * C::ROWS + lr + 128) - 1;
+      const int see_lo = part.held - part.rows + (part.row_tile * C::ROWS + lr) / a.G;
       const int see_hi = part.held - part.rows + r_end / a.G;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
@@ -635,12 +657,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           tmem_st32(ts, p);
           tmem_st32(ts + 32, p + 32);
         } else {
-          tmem_st16(ts + half * 16, p);
+          tmem_st32(ts + half * (C::COLS / 2), p);
         }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&pfull[buf]);
+        if (lane == 0) mbar_arrive_remote(lead_pfull + 8 * buf);
         __syncwarp();
       }
       kv += n;
@@ -659,30 +681,33 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     // columns contiguous: 64 of them a panel, panels NT rows of 128 bytes apart
     const uint32_t v_lo = uniform((smem_u32(sV) >> 4) | ((uint32_t)(C::NT * 128) >> 4 << 16));
     const uint32_t tm = uniform(tmem);
-    constexpr uint32_t id_s = idesc_f16(128, C::NT, 0), id_o = idesc_f16(128, D, 1);
+    constexpr uint32_t id_s = idesc_f16(C::TROWS, C::NT, 0), id_o = idesc_f16(C::TROWS, D, 1);
     uint32_t kv = 0;        // token tiles before the part's
     uint32_t parts[2] = {0, 0}, np[2] = {0, 0};  // of each row tile: parts and P tiles before
     bool go = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, kChunkWait); };
+    auto commit = [](uint64_t* bar) { C::PAIR ? umma_commit_pair(bar) : umma_commit(bar); };
     auto scores = [&](int q, uint32_t s, uint32_t st) {  // S = Q[q] K^T, one thread
 #pragma unroll
       for (int k = 0; k < D / 16; ++k)
-        umma_bf16(s, desc64(q_lo + ((q * C::QBYTES + (k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
-                  desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::NT * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
+        (C::PAIR ? umma_bf16_pair : umma_bf16)(
+            s, desc64(q_lo + ((q * C::QBYTES + (k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
+            desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::KROWS * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
     };
     auto outputs = [&](int q, uint32_t p, uint32_t st, uint32_t add) {  // O[q] += P V, one thread
 #pragma unroll
       for (int k = 0; k < C::NT / 16; ++k)
-        umma_f16_ts(tm + C::TO + q * D, p + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, k > 0 ? 1 : add);
+        (C::PAIR ? umma_f16_ts_pair : umma_f16_ts)(
+            tm + C::TO + q * D, p + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, k > 0 ? 1 : add);
     };
     Part ahead;  // read a part early: its loads take as long as a tile
-    bool more = walk.next(a, ahead);
+    bool more = rank == 0 && walk.next(a, ahead);  // the first CTA of a pair issues for both
     while (go && __any_sync(0xffffffffu, more)) {
       part = ahead;
       more = walk.next(a, ahead);
       const uint32_t n = uniform(part.last - part.first), t0 = uniform(kv);
       if (C::NQ == 2) {
-        const bool two = (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > 128;
+        const bool two = (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > C::TROWS;
         const uint32_t k0 = t0 & 1;
         go = wait(&kfull[k0], t0 >> 1);
 #pragma unroll
@@ -693,8 +718,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           tc_fence_after();
           if (elect_one()) {
             scores(q, tm + q * C::NT, k0);
-            umma_commit(&sfull[q]);
-            if (q || !two) umma_commit(&kempty[k0]);
+            commit(&sfull[q]);
+            if (q || !two) commit(&kempty[k0]);
           }
           __syncwarp();
         }
@@ -711,12 +736,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             tc_fence_after();
             if (elect_one()) {
               outputs(q, tm + q * C::NT, vs, t != t0);
-              if (last) umma_commit(&olast[q]);
-              if (q || !two) umma_commit(&vempty[vs]);
+              if (last) commit(&olast[q]);
+              if (q || !two) commit(&vempty[vs]);
               if (!last) {
                 scores(q, tm + q * C::NT, ks);
-                umma_commit(&sfull[q]);
-                if (q || !two) umma_commit(&kempty[ks]);
+                commit(&sfull[q]);
+                if (q || !two) commit(&kempty[ks]);
               }
             }
             __syncwarp();
@@ -729,8 +754,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           tc_fence_after();
           if (elect_one()) {
             scores(0, tm + (t & 1) * C::NT, t & 1);
-            umma_commit(&sfull[t & 1]);
-            umma_commit(&kempty[t & 1]);
+            commit(&sfull[t & 1]);
+            commit(&kempty[t & 1]);
           }
           __syncwarp();
         };
@@ -745,9 +770,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           tc_fence_after();
           if (elect_one()) {
             outputs(0, tm + (t & 1) * C::NT, t & 1, t != t0);
-            umma_commit(&ofull[t & 1]);
-            if (last) umma_commit(&olast[0]);
-            umma_commit(&vempty[t & 1]);
+            commit(&ofull[t & 1]);
+            if (last) commit(&olast[0]);
+            commit(&vempty[t & 1]);
           }
           __syncwarp();
         }
@@ -756,34 +781,41 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     }
     // every MMA this warp issued has completed before TMEM is released
     __syncwarp();
-    if (elect_one()) {
-      umma_commit(drain);
+    if (rank == 0 && elect_one()) {
+      commit(drain);
       const long long since = clock64();
       while (!mbar_try_wait(drain, 0) && clock64() - since < kDrainCycles) {
       }
     }
   } else {
     // --------------------------------------------------------------- conversion
-    // The tasks of all token tiles in order, 8 of keys then 8 of values a tile;
-    // this warp takes every seventh, so it has a part in every tile and operand and
-    // its waits cannot miss a phase.  A task's block is looked up three turns
-    // ahead, its scales and codes are loaded two turns ahead.
+    // The tasks of all token tiles in order, a tile's keys and then its values;
+    // this warp takes every seventh.  Its waits cannot miss a phase: the task before
+    // has waited for a product of at most three tiles back, and that one came after
+    // the product that freed this task's stage the time before.  A task's block is
+    // looked up three turns ahead, its scales and codes are loaded two turns ahead.
+    // Lanes 16 and up look up the second 16 tokens of a task of 32, and of a pair's
+    // keys the 16 tokens that the other CTA converts at the same time: each CTA
+    // needs the scales of all.
     struct Task {
-      int t;               // token tile of the CTA; -1: none
-      int idx;             // of the tile's 16 tasks
-      int id;              // block
-      bool held;           // false: past the tokens held
+      int t;    // token tile of the CTA; -1: none
+      int idx;  // of the tile's tasks
+      int id;   // block; -2: past the tokens held
       int h;
       const uint8_t* src;  // the lane's first codes, were the block number 0
+      int second;          // from there to the second 16 tokens' codes, in a task of 32
     };
-    constexpr int SUB = D / C::TC;  // tasks of a granule's operand
-    constexpr int RSTEP = C::TC == 64 ? 8 : 4;  // rows a load of the warp covers
+    constexpr int TASKS = C::KTASKS + C::VTASKS;
     // eight lanes write two rows of one 64-column panel: no bank conflicts
-    const int col = (lane & 3) + (C::TC == 64 ? 0 : (lane >> 4) << 2);  // 16-code chunk of the row
-    const int row0 = (lane >> 2) & (RSTEP - 1);
-    const uint32_t to0 = smem_u32(sK) + (col >> 2) * C::NT * 128 + row0 * 128 + (((col & 3) * 2 ^ row0) << 4);  // rows 4 apart: chunk ^ 4
+    auto col_of = [&](int width) { return (lane & 3) + (width == 64 ? 0 : (lane >> 4) << 2); };  // 16-code chunk of the row
+    auto row_of = [&](int width) { return (lane >> 2) & (width == 64 ? 7 : 3); };
+    auto to_of = [&](uint8_t* base, int width, int rows) {  // rows 4 apart: chunk ^ 4
+      const int col = col_of(width), row = row_of(width);
+      return smem_u32(base) + (col >> 2) * rows * 128 + row * 128 + (((col & 3) * 2 ^ row) << 4);
+    };
+    const uint32_t to_k = to_of(sK, C::KC, C::KROWS), to_v = to_of(sV, C::VC, C::NT);
+    const int at_k = row_of(C::KC) * D + col_of(C::KC) * 16, at_v = row_of(C::VC) * D + col_of(C::VC) * 16 + rank * C::VCOLS;
     const long long block_bytes = (long long)c.K * c.P * D;
-    const uint32_t bars = smem_u32(s_bar);
     int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
     int at = warp - kSoftWarps;            // the next task to look up
     bool more = true;
@@ -792,8 +824,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const uint8_t *keys = nullptr, *values = nullptr;
     int tok_part = 0;                      // first token of its first tile, less the tiles before it
     auto look_up = [&]() {
-      Task k = {-1, 0, 0, false, 0, nullptr};
-      const int t = at >> 4, idx = at & 15;
+      Task k = {-1, 0, -2, 0, nullptr, 0};
+      const int t = at / TASKS, idx = at % TASKS;
       while (more && t >= base + n) {
         base += n;
         n = 0;
@@ -801,42 +833,46 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         if (more) {
           n = part.last - part.first;
           table = c.table + (size_t)part.seq * c.max_blocks;
-          const size_t lane_at = ((size_t)part.h * c.P + row0) * D + col * 16;
-          keys = c.codes[0] + lane_at;
-          values = c.codes[1] + lane_at;
+          keys = c.codes[0] + (size_t)part.h * c.P * D + at_k;
+          values = c.codes[1] + (size_t)part.h * c.P * D + at_v;
           tok_part = (part.tile0 + part.first - base) * C::NT;
         }
       }
       if (!more) return k;
-      const int tok = tok_part + t * C::NT + ((idx & 7) / SUB) * 16;
+      const bool v = idx >= C::KTASKS;
+      const int i = v ? idx - C::KTASKS : idx;
+      const int tok = tok_part + t * C::NT + (v ? i * C::VT : rank * C::KROWS + i / C::SUB * 16);
+      const int mine = tok + (lane < 16 || !C::PAIR ? 0 : v ? C::VT - 16 : rank == 0 ? C::KROWS : -C::KROWS);
       k.t = t;
       k.idx = idx;
       k.h = part.h;
-      k.src = (idx < 8 ? keys : values) + ((tok & (c.P - 1)) * D + (idx & (SUB - 1)) * C::TC);
-      k.held = tok < part.held;
+      k.src = (v ? values : keys + i % C::SUB * C::KC) + (tok & (c.P - 1)) * D;
+      if (C::VT == 32) k.second = (((tok + 16) & (c.P - 1)) - (tok & (c.P - 1))) * D;
       // looked at when the codes are loaded: a wait for it here would cost a latency a task
-      if (k.held) k.id = table[tok >> c.logP];
+      if (mine < part.held) k.id = table[mine >> c.logP];
       at += kConvWarps;
       return k;
     };
     auto load = [&](const Task& k, uint4 (&x)[C::LOADS], float& ks, float& vs) {
-      ks = vs = 1.0f;
-      if (k.held && (unsigned)k.id < (unsigned)c.n_blocks) {
-        const uint8_t* src = k.src + k.id * block_bytes;
+      const bool v = k.idx >= C::KTASKS;
+      const int id0 = __shfl_sync(0xffffffffu, k.id, 0), id1 = C::VT == 32 && v ? __shfl_sync(0xffffffffu, k.id, 16) : id0;
+      const bool fine = (unsigned)k.id < (unsigned)c.n_blocks;
+      ks = vs = k.id == -2 ? 1.0f : kv_nan();
+      if (!fine && k.id != -2) kv_raise(c, MSI_ERR_INVALID_ARG);
+      const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
+      const int step = v && C::VC == 64 ? 8 * D : C::KC == 64 ? 8 * D : 4 * D;  // codes of the rows a load of the warp covers
 #pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * RSTEP * D);
-        if (k.idx < 8 && (k.idx & (SUB - 1)) == 0) {
-          ks = c.scale[0][(size_t)k.id * c.K + k.h];
-          vs = c.scale[1][(size_t)k.id * c.K + k.h];
-        }
-      } else {
-        const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
-#pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) x[i] = make_uint4(z, z, z, z);
-        if (k.held) {
-          ks = vs = kv_nan();
-          if (lane == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
-        }
+      for (int i = 0; i < C::LOADS; ++i) {
+        const bool up = C::VT == 32 && v && i >= C::LOADS / 2;
+        const int id = up ? id1 : id0;
+        // in a task of 32 tokens the second 16 are two loads on
+        const uint8_t* src = k.src + id * block_bytes + (up ? k.second + (i - C::LOADS / 2) * step : i * step);
+        x[i] = make_uint4(z, z, z, z);
+        if ((unsigned)id < (unsigned)c.n_blocks) x[i] = *reinterpret_cast<const uint4*>(src);
+      }
+      if (!v && k.idx % C::SUB == 0 && fine) {
+        ks = c.scale[0][(size_t)k.id * c.K + k.h];
+        vs = c.scale[1][(size_t)k.id * c.K + k.h];
       }
     };
     Task k0 = look_up(), k1 = look_up(), k2 = look_up();
@@ -845,23 +881,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     load(k0, x0, ks0, vs0);
     load(k1, x1, ks1, vs1);
     auto turn = [&](const Task& k, uint4 (&x)[C::LOADS], float ks, float vs) {
-      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1, v = k.idx >> 3, g = (k.idx & 7) / SUB;
+      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1, v = k.idx >= C::KTASKS;
+      const int i = v ? k.idx - C::KTASKS : k.idx;
       // s_bar: full and empty barriers of keys, then of values
-      const uint32_t full = bars + (v * 4 + st) * 8;
       if (!mbar_wait_warp(kempty + v * 4 + st, ph, abort_flag, kChunkWait)) return false;
-      const uint32_t tile = to0 + (2 * v + st) * C::KBYTES + (k.idx & (SUB - 1)) * (C::TC / 64) * C::NT * 128 + g * 16 * 128;
+      const uint32_t tile = st * C::KBYTES + (v ? to_v + i * C::VT * 128 : to_k + i / C::SUB * 16 * 128 + i % C::SUB * (C::KC / 64) * C::KROWS * 128);
+      // the swizzle: chunk ^ (row & 7), the row being its first + a multiple of 8, or of 4
+      const bool eight = C::KC == 64 || (C::VC == 64 && v);
+      const uint32_t step = eight ? 1024 : 512, flip = eight ? 0 : 64;
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
-        // the swizzle: chunk ^ (row & 7), the row being row0 + i RSTEP
-        const uint32_t to = RSTEP == 4 && (i & 1) ? (tile ^ 64) + i * RSTEP * 128 : tile + i * RSTEP * 128;
+        const uint32_t to = (i & 1 ? tile ^ flip : tile) + i * step;
         st_shared_v4(to, make_uint4(kv_f16x2<FMT, false>(x[i].x), kv_f16x2<FMT, true>(x[i].x), kv_f16x2<FMT, false>(x[i].y), kv_f16x2<FMT, true>(x[i].y)));
         st_shared_v4(to ^ 16, make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w)));
       }
-      // the granule's scales: read by softmax after the scores, which follow kfull
-      if (k.idx < 8 && lane == 0 && (k.idx & (SUB - 1)) == 0) s_info[k.t & 3][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
+      // the granules' scales: read by softmax after the scores, which follow kfull
+      if (!v && i % C::SUB == 0 && (lane & (C::PAIR ? 15 : 31)) == 0) {
+        const int g = i / C::SUB + (C::PAIR ? (rank ^ (lane >> 4)) * (C::KROWS / 16) : 0);
+        s_info[k.t & 3][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
+      }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full) : "memory");
+      if (lane == 0) mbar_arrive_remote(lead + (v * 4 + st) * 8);
       return true;
     };
     while (k0.t >= 0) {
@@ -880,8 +921,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (C::PAIR) cluster_sync_all();  // neither CTA leaves while the other may still reach it
   tc_fence_after();
-  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+  if (warp == kMmaWarp) C::PAIR ? tmem_dealloc_pair(tmem, 512) : tmem_dealloc(tmem, 512);
   if (tid == 0 && s_abort != 0) kv_raise(c, MSI_ERR_TIMEOUT);
 }
 
@@ -965,7 +1007,24 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT, kItemCost<D>);
   if (e != cudaSuccess) return e;
-  e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(kChunkThreads), C::SMEM, s, a);
+  if (C::PAIR) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(2 * a.ctas);
+    cfg.blockDim = dim3(kChunkThreads);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, kv_chunk_kernel<D, FMT, CAP>, a);
+  } else {
+    e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(kChunkThreads), C::SMEM, s, a);
+  }
   if (e != cudaSuccess) return e;
   e = launch_after(true, kv_chunk_join_kernel<D>, dim3(a.ctas, C::ROWS / kChunkJoinRows), dim3(kChunkJoinThreads), 0, s, a);
   *launches = 3;
@@ -981,7 +1040,8 @@ cudaError_t chunk_d(const KvAttnArgs& a, int* launches, cudaStream_t s) {
 
 }  // namespace
 
-int kv_chunk_rows(int D) { return D == 256 ? 128 : 256; }
+int kv_chunk_rows(int D) { return D == 64 ? Chunk<64>::ROWS : D == 128 ? Chunk<128>::ROWS : Chunk<256>::ROWS; }
+int kv_chunk_runs(int D, int sms) { return D == 64 ? sms : sms / 2; }
 
 cudaError_t launch_kv_chunk(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   return a.c.D == 64 ? chunk_d<64>(a, launches, s) : a.c.D == 128 ? chunk_d<128>(a, launches, s) : chunk_d<256>(a, launches, s);

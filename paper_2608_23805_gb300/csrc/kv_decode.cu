@@ -153,15 +153,16 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
     for (int i = tid; i <= a.n; i += kDecThreads) a.item_pre[i] = s_pre[i];
   if (!ok || status != 0 || (OBS && total > a.max_steps)) {
     if (status == 0 && tid == 0 && blockIdx.x == 0) kv_raise(c, MSI_ERR_INVALID_ARG);
-    // fail closed: no row of the call can be read as an answer
+    // fail closed: no row of the call can be read as an answer.  If the word was
+    // raised by this call, other CTAs are at work: this one covers its rows itself.
+    const int from = ok ? 0 : blockIdx.x, step = ok ? 1 : gridDim.x;
     const long long vecs = (long long)a.n_rows * a.H * (D / 8);
-    for (long long i = (long long)blockIdx.x * kDecThreads + tid; i < vecs; i += (long long)gridDim.x * kDecThreads) {
+    for (long long i = (long long)from * kDecThreads + tid; i < vecs; i += (long long)step * kDecThreads) {
       const long long row = i / (a.H * (D / 8));
       *reinterpret_cast<uint4*>(a.out + row * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
           make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
     }
-    for (long long i = (long long)blockIdx.x * kDecThreads + tid; i < (long long)a.n_rows * a.H;
-         i += (long long)gridDim.x * kDecThreads)
+    for (long long i = (long long)from * kDecThreads + tid; i < (long long)a.n_rows * a.H; i += (long long)step * kDecThreads)
       if (a.lse != nullptr) a.lse[i] = kv_nan();
     return;
   }
