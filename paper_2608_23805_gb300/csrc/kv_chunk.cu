@@ -44,16 +44,17 @@ template <int D>
 struct Chunk {
   static constexpr bool PAIR = D >= 128;          // two CTAs on one item
   static constexpr int NQ = D == 256 ? 1 : 2;     // row tiles
-  static constexpr int NT = 128;                  // tokens of a tile
+  static constexpr int NT = D == 256 ? 128 : 64;  // tokens of a tile: two S of each row tile and O fill TMEM
+  static constexpr int ST = D == 256 ? 2 : 4;     // stages of keys and values
   static constexpr int TROWS = PAIR ? 256 : 128;  // rows of a row tile, 128 a CTA
   static constexpr int ROWS = TROWS * NQ;
   static constexpr int NG = NT / 16;              // 16-token granules
-  static constexpr int COLS = NQ == 2 ? NT : NT / 2;  // S columns a softmax thread takes
+  static constexpr int COLS = 64;                 // S columns a softmax thread takes
   static constexpr int KROWS = PAIR ? NT / 2 : NT;    // a CTA's tokens of the keys,
   static constexpr int VCOLS = PAIR ? D / 2 : D;      // and columns of the values
   static constexpr int QBYTES = 128 * D * 2;      // a CTA's part of a row tile
   static constexpr int KBYTES = KROWS * D * 2;    // and of a tile's keys, or values
-  static constexpr int SMEM = NQ * QBYTES + 4 * KBYTES + 1024;
+  static constexpr int SMEM = NQ * QBYTES + 2 * ST * KBYTES + 1024;
   // conversion tasks: 16 tokens of keys, up to 128 columns; 16 tokens of values, or 32 of 64 columns
   static constexpr int KC = D < 128 ? D : 128, VC = VCOLS < 128 ? VCOLS : 128;
   static constexpr int SUB = D / KC;              // tasks of 16 tokens' keys
@@ -62,18 +63,18 @@ struct Chunk {
   static constexpr int LOADS = KC / 32;           // 16-byte loads a lane
   static_assert(VT * VC == 16 * KC && VC == VCOLS, "all tasks of one size");
   static constexpr int TO = 256;                  // first column of O in TMEM
+  // 8 softmax warps, then conversion warps, then an MMA warp a row tile
+  static constexpr int SOFT = 8, MMA = 16 - NQ, CONV = MMA - SOFT;
 };
-// 8 softmax warps, 7 conversion warps, the MMA warp; the groups share 512 x 128
-// registers out: 2 x 144 + 2 x 112 a thread.
-constexpr int kSoftWarps = 8, kConvWarps = 7, kMmaWarp = kSoftWarps + kConvWarps;
-constexpr int kChunkThreads = 32 * (kMmaWarp + 1);
+// 16 warps; the groups share 512 x 128 registers out: 2 x 144 + 2 x 112 a thread.
+constexpr int kChunkThreads = 512;
 constexpr int kSoftRegs = 144, kConvRegs = 112;
-static_assert(kChunkThreads == 512 && 2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
+static_assert(2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
 // What an item costs beside its tiles (queries, first scores, output), in tiles.
 // D = 256, 4 sequences of 3,000 on 3,000: 562, 473, 454, 470 us at 2, 4, 6, 8; 128
 // columns or fewer, where a long item hides it: 826 us at 1, 2 and 4.
 template <int D>
-constexpr int kItemCost = D == 256 ? 3 : 2;
+constexpr int kItemCost = 4;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
   uint64_t d;
@@ -382,45 +383,52 @@ template <int D, int FMT, bool CAP>
 __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a) {
   using C = Chunk<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bar[32];
-  __shared__ __align__(16) Granule s_info[4][C::NG];
+  __shared__ __align__(8) uint64_t s_bar[40];
+  __shared__ __align__(16) Granule s_info[2 * C::ST][C::NG];
   __shared__ float s_pair[C::NQ == 1 ? 3 : 1][2][128];  // of two warps that share rows: query maximum, reference, sum
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   uint8_t* sQ = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sK = sQ + C::NQ * C::QBYTES;
-  uint8_t* sV = sK + 2 * C::KBYTES;
+  uint8_t* sV = sK + C::ST * C::KBYTES;
   const int rank = C::PAIR ? (int)cluster_ctarank() : 0, run = C::PAIR ? blockIdx.x >> 1 : blockIdx.x;
-  uint64_t *kfull = s_bar, *kempty = s_bar + 2, *vfull = s_bar + 4, *vempty = s_bar + 6;
-  uint64_t *qfull = s_bar + 8, *sfull = s_bar + 10, *pfull = s_bar + 12, *ofull = s_bar + 14, *ofree = s_bar + 16;
-  uint64_t *olast = s_bar + 18, *drain = s_bar + 20;  // ofull: every product's end; olast: that of a part's last
-  // What the MMA warp waits for (kfull, vfull, qfull, pfull, ofree) is counted at
-  // the first CTA of a pair, for both; what it signals arrives at both.
+  // of each stage: keys full and empty, values full and empty
+  uint64_t *kfull = s_bar, *kempty = s_bar + C::ST, *vfull = s_bar + 2 * C::ST, *vempty = s_bar + 3 * C::ST;
+  // of each row tile and S: scores, weights and product done; of each row tile:
+  // queries there, O free, a part's last product done
+  uint64_t *sfull = s_bar + 16, *pfull = s_bar + 20, *ofull = s_bar + 24;
+  uint64_t *qfull = s_bar + 28, *ofree = s_bar + 30, *olast = s_bar + 32, *drain = s_bar + 34;
+  // What the MMA warps wait for (kfull, vfull, qfull, pfull, ofree) is counted at
+  // the first CTA of a pair, for both; what they signal arrives at both.
   const uint32_t lead = C::PAIR ? mapa_shared(smem_u32(s_bar), 0) : smem_u32(s_bar);
-  const uint32_t lead_qfull = lead + 8 * 8, lead_pfull = lead + 12 * 8, lead_ofree = lead + 16 * 8;
+  const uint32_t lead_pfull = lead + 20 * 8, lead_qfull = lead + 28 * 8, lead_ofree = lead + 30 * 8;
   volatile int* abort_flag = &s_abort;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     const int both = C::PAIR ? 2 : 1, soft = both * (C::NQ == 2 ? 4 : 8);  // warps of a row tile
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < C::ST; ++i) {
       mbar_init(kfull + i, both * C::KTASKS);
-      mbar_init(kempty + i, 1);
+      mbar_init(kempty + i, C::NQ);
       mbar_init(vfull + i, both * C::VTASKS);
-      mbar_init(vempty + i, 1);
-      mbar_init(qfull + i, soft);
+      mbar_init(vempty + i, C::NQ);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(sfull + i, 1);
       mbar_init(pfull + i, soft);
       mbar_init(ofull + i, 1);
-      mbar_init(olast + i, 1);
-      mbar_init(ofree + i, soft);
     }
-    mbar_init(drain, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(qfull + i, soft);
+      mbar_init(ofree + i, soft);
+      mbar_init(olast + i, 1);
+      mbar_init(drain + i, 1);
+    }
     mbar_fence_init();
     s_abort = 0;
   }
-  if (warp == kMmaWarp) {
+  if (warp == C::MMA) {
     if (C::PAIR) {
       tmem_alloc_pair(&s_tmem, 512);
       tmem_relinquish_pair();
@@ -455,7 +463,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   if (ok && a.plan[0] > 0 && run < a.plan[2]) walk.init(a, run);
   Part part;
 
-  if (warp < kSoftWarps) {
+  if (warp < C::SOFT) {
     // ------------------------------------------------------------------ softmax
     set_regs<kSoftRegs, true>();
     // a row a thread; D = 256: two threads, each half of the columns
@@ -594,12 +602,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const int see_hi = part.held - part.rows + r_end / a.G;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const int buf = C::NQ == 2 ? q : (kv + j) & 1;
-        go = mbar_wait_warp(&sfull[buf], (C::NQ == 2 ? ns : (kv + j) >> 1) & 1, abort_flag, kChunkWait);
+        const uint32_t mine = ns++;
+        const int buf = 2 * q + (mine & 1);
+        go = mbar_wait_warp(&sfull[buf], (mine >> 1) & 1, abort_flag, kChunkWait);
         if (!go) break;
-        ++ns;
         tc_fence_after();
-        const Granule* info = s_info[(kv + j) & 3] + half * (C::COLS / 16);
+        const Granule* info = s_info[(kv + j) & (2 * C::ST - 1)] + half * (C::COLS / 16);
         const int tok0 = (part.tile0 + part.first + j) * C::NT + half * C::COLS;
         const uint32_t ts = tmem + buf * C::NT + lanes;
         const bool mask = tok0 + C::COLS - 1 > see_lo || (a.window > 0 && tok0 <= see_hi - a.window);
@@ -618,14 +626,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
               top = fmaxf(top, s_pair[kTopAt][half ^ 1][tr]);
             }
             if (j > 0) {
-              // the output so far, once the last product is in it (with two row
-              // tiles the scores of this tile came after it)
-              if (C::NQ == 1) {
-                const uint32_t t = kv + j - 1;  // the tile before
-                go = mbar_wait_warp(&ofull[t & 1], (t >> 1) & 1, abort_flag, kChunkWait);
-                if (!go) break;
-                tc_fence_after();
-              }
+              // the output so far, once the last product is in it
+              const uint32_t last = mine - 1;
+              go = mbar_wait_warp(&ofull[2 * q + (last & 1)], (last >> 1) & 1, abort_flag, kChunkWait);
+              if (!go) break;
+              tc_fence_after();
               const float f = top == -INFINITY ? 1.0f : ex2(m - top);
               l *= f;
               constexpr int W = C::NQ == 2 ? D : D / 2;
@@ -653,12 +658,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         }
         if (!go) break;
         l += sum;
-        if constexpr (C::NQ == 2) {
-          tmem_st32(ts, p);
-          tmem_st32(ts + 32, p + 32);
-        } else {
-          tmem_st32(ts + half * (C::COLS / 2), p);
-        }
+        tmem_st32(ts + half * (C::COLS / 2), p);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -671,139 +671,105 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     if (C::NQ == 1 && gone()) pair_leave(pair);
   } else {
   set_regs<kConvRegs, false>();  // one instruction for the whole warpgroup
-  if (warp == kMmaWarp) {
-    // --------------------------------------------------------------- MMA issuer
-    // Issue runs little ahead of the tensor core, so what the warp does between
-    // its products shows: a row tile's output and next scores are issued in one go.
+  if (warp >= C::MMA) {
+    // -------------------------------------------- MMA issuers, one of each row tile
+    // Issue runs only three or four products ahead of the tensor core, so what a
+    // warp does between them (waits, addresses) shows unless the other's fill it.
+    // A tile's scores are issued before the weights of the one before are waited for.
+    const int q = warp - C::MMA;
     const uint32_t desc_hi = (uint32_t)(sw128_desc(0) >> 32);
-    const uint32_t q_lo = uniform((uint32_t)sw128_desc(smem_u32(sQ)));
+    const uint32_t q_lo = uniform((uint32_t)sw128_desc(smem_u32(sQ)) + q * (C::QBYTES >> 4));
     const uint32_t k_lo = uniform((uint32_t)sw128_desc(smem_u32(sK)));
     // columns contiguous: 64 of them a panel, panels NT rows of 128 bytes apart
     const uint32_t v_lo = uniform((smem_u32(sV) >> 4) | ((uint32_t)(C::NT * 128) >> 4 << 16));
-    const uint32_t tm = uniform(tmem);
+    const uint32_t tm = uniform(tmem + q * 2 * C::NT), to = uniform(tmem + C::TO + q * D);
     constexpr uint32_t id_s = idesc_f16(C::TROWS, C::NT, 0), id_o = idesc_f16(C::TROWS, D, 1);
-    uint32_t kv = 0;        // token tiles before the part's
-    uint32_t parts[2] = {0, 0}, np[2] = {0, 0};  // of each row tile: parts and P tiles before
+    uint32_t kv = 0;            // token tiles before the part's
+    uint32_t parts = 0, ns = 0;  // parts begun, and S tiles begun before the part's, of this row tile
     bool go = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, kChunkWait); };
     auto commit = [](uint64_t* bar) { C::PAIR ? umma_commit_pair(bar) : umma_commit(bar); };
-    auto scores = [&](int q, uint32_t s, uint32_t st) {  // S = Q[q] K^T, one thread
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        (C::PAIR ? umma_bf16_pair : umma_bf16)(
-            s, desc64(q_lo + ((q * C::QBYTES + (k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
-            desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::KROWS * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
-    };
-    auto outputs = [&](int q, uint32_t p, uint32_t st, uint32_t add) {  // O[q] += P V, one thread
-#pragma unroll
-      for (int k = 0; k < C::NT / 16; ++k)
-        (C::PAIR ? umma_f16_ts_pair : umma_f16_ts)(
-            tm + C::TO + q * D, p + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, k > 0 ? 1 : add);
-    };
+    auto stage = [](uint32_t t) { return t & (C::ST - 1); };
+    auto phase = [](uint32_t t) { return t / C::ST; };
     Part ahead;  // read a part early: its loads take as long as a tile
     bool more = rank == 0 && walk.next(a, ahead);  // the first CTA of a pair issues for both
     while (go && __any_sync(0xffffffffu, more)) {
       part = ahead;
       more = walk.next(a, ahead);
-      const uint32_t n = uniform(part.last - part.first), t0 = uniform(kv);
-      if (C::NQ == 2) {
-        const bool two = (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) > C::TROWS;
-        const uint32_t k0 = t0 & 1;
-        go = wait(&kfull[k0], t0 >> 1);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          if (!go || (q && !two)) break;
-          go = wait(&qfull[q], parts[q]);
-          if (!go) break;
-          tc_fence_after();
-          if (elect_one()) {
-            scores(q, tm + q * C::NT, k0);
-            commit(&sfull[q]);
-            if (q || !two) commit(&kempty[k0]);
-          }
-          __syncwarp();
-        }
-        for (uint32_t t = t0; go && t < t0 + n; ++t) {
-          const bool last = t + 1 == t0 + n;
-          const uint32_t vs = uniform(t & 1), ks = vs ^ 1;
-          go = wait(&vfull[vs], t >> 1) && (last || wait(&kfull[ks], (t + 1) >> 1));
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            if (!go || (q && !two)) break;
-            if (t == t0) go = wait(&ofree[q], parts[q]++ ^ 1);
-            go = go && wait(&pfull[q], np[q]++);
-            if (!go) break;
-            tc_fence_after();
-            if (elect_one()) {
-              outputs(q, tm + q * C::NT, vs, t != t0);
-              if (last) commit(&olast[q]);
-              if (q || !two) commit(&vempty[vs]);
-              if (!last) {
-                scores(q, tm + q * C::NT, ks);
-                commit(&sfull[q]);
-                if (q || !two) commit(&kempty[ks]);
-              }
-            }
-            __syncwarp();
-          }
-        }
-      } else {
-        auto first = [&](uint32_t t) {
-          go = go && wait(&kfull[t & 1], t >> 1);
-          if (!go) return;
-          tc_fence_after();
-          if (elect_one()) {
-            scores(0, tm + (t & 1) * C::NT, t & 1);
-            commit(&sfull[t & 1]);
-            commit(&kempty[t & 1]);
-          }
-          __syncwarp();
-        };
-        go = wait(&qfull[0], parts[0]);
-        first(t0);
-        go = go && wait(&ofree[0], parts[0]++ ^ 1);
-        for (uint32_t t = t0; go && t < t0 + n; ++t) {
-          const bool last = t + 1 == t0 + n;
-          if (!last) first(t + 1);
-          go = go && wait(&vfull[t & 1], t >> 1) && wait(&pfull[t & 1], t >> 1);
-          if (!go) break;
-          tc_fence_after();
-          if (elect_one()) {
-            outputs(0, tm + (t & 1) * C::NT, t & 1, t != t0);
-            commit(&ofull[t & 1]);
-            if (last) commit(&olast[0]);
-            commit(&vempty[t & 1]);
-          }
-          __syncwarp();
-        }
-      }
+      const uint32_t n = uniform(part.last - part.first), t0 = uniform(kv), n0 = uniform(ns);
       kv += n;
+      if (q > 0 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) <= C::TROWS) {  // no second row tile
+        for (uint32_t t = t0; go && t < t0 + n; ++t) {
+          go = wait(&kfull[stage(t)], phase(t));
+          if (go && elect_one()) commit(&kempty[stage(t)]);
+          __syncwarp();
+          go = go && wait(&vfull[stage(t)], phase(t));
+          if (go && elect_one()) commit(&vempty[stage(t)]);
+          __syncwarp();
+        }
+        continue;
+      }
+      auto scores = [&](uint32_t j) {
+        const uint32_t st = uniform(stage(t0 + j)), buf = uniform((n0 + j) & 1);
+        go = go && wait(&kfull[st], phase(t0 + j));
+        if (!go) return;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            (C::PAIR ? umma_bf16_pair : umma_bf16)(
+                tm + buf * C::NT, desc64(q_lo + (((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
+                desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::KROWS * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
+          commit(&sfull[2 * q + buf]);
+          commit(&kempty[st]);
+        }
+        __syncwarp();
+      };
+      go = wait(&qfull[q], parts);
+      scores(0);
+      go = go && wait(&ofree[q], parts ^ 1);
+      for (uint32_t j = 0; go && j < n; ++j) {
+        if (j + 1 < n) scores(j + 1);
+        const uint32_t st = uniform(stage(t0 + j)), buf = uniform((n0 + j) & 1);
+        go = go && wait(&vfull[st], phase(t0 + j)) && wait(&pfull[2 * q + buf], (n0 + j) >> 1);
+        if (!go) break;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < C::NT / 16; ++k)
+            (C::PAIR ? umma_f16_ts_pair : umma_f16_ts)(
+                to, tm + buf * C::NT + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, (j | k) != 0);
+          commit(&ofull[2 * q + buf]);
+          if (j + 1 == n) commit(&olast[q]);
+          commit(&vempty[st]);
+        }
+        __syncwarp();
+      }
+      ++parts;
+      ns += n;
     }
     // every MMA this warp issued has completed before TMEM is released
     __syncwarp();
     if (rank == 0 && elect_one()) {
-      commit(drain);
+      commit(drain + q);
       const long long since = clock64();
-      while (!mbar_try_wait(drain, 0) && clock64() - since < kDrainCycles) {
+      while (!mbar_try_wait(drain + q, 0) && clock64() - since < kDrainCycles) {
       }
     }
   } else {
     // --------------------------------------------------------------- conversion
     // The tasks of all token tiles in order, a tile's keys and then its values;
-    // this warp takes every seventh.  Its waits cannot miss a phase: the task before
-    // has waited for a product of at most three tiles back, and that one came after
+    // this warp takes every CONV-th.  Its waits cannot miss a phase: the task before
+    // has waited for a product of at most ST + 2 tiles back, and that one came after
     // the product that freed this task's stage the time before.  A task's block is
     // looked up three turns ahead, its scales and codes are loaded two turns ahead.
     // Lanes 16 and up look up the second 16 tokens of a task of 32, and of a pair's
     // keys the 16 tokens that the other CTA converts at the same time: each CTA
     // needs the scales of all.
     struct Task {
-      int t;    // token tile of the CTA; -1: none
-      int idx;  // of the tile's tasks
+      int n;    // in order; -1: none
       int id;   // block; -2: past the tokens held
-      int h;
-      const uint8_t* src;  // the lane's first codes, were the block number 0
-      int second;          // from there to the second 16 tokens' codes, in a task of 32
+      int off;  // the lane's first code in the block
     };
     constexpr int TASKS = C::KTASKS + C::VTASKS;
     // eight lanes write two rows of one 64-column panel: no bank conflicts
@@ -816,15 +782,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const uint32_t to_k = to_of(sK, C::KC, C::KROWS), to_v = to_of(sV, C::VC, C::NT);
     const int at_k = row_of(C::KC) * D + col_of(C::KC) * 16, at_v = row_of(C::VC) * D + col_of(C::VC) * 16 + rank * C::VCOLS;
     const long long block_bytes = (long long)c.K * c.P * D;
+    const int log_row = c.logP + (D == 64 ? 6 : D == 128 ? 7 : 8);  // codes of a block and head
     int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
-    int at = warp - kSoftWarps;            // the next task to look up
+    int at = warp - C::SOFT;            // the next task to look up
     bool more = true;
     // of the part
     const int* table = nullptr;
-    const uint8_t *keys = nullptr, *values = nullptr;
     int tok_part = 0;                      // first token of its first tile, less the tiles before it
     auto look_up = [&]() {
-      Task k = {-1, 0, -2, 0, nullptr, 0};
+      Task k = {-1, -2, 0};
       const int t = at / TASKS, idx = at % TASKS;
       while (more && t >= base + n) {
         base += n;
@@ -833,8 +799,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         if (more) {
           n = part.last - part.first;
           table = c.table + (size_t)part.seq * c.max_blocks;
-          keys = c.codes[0] + (size_t)part.h * c.P * D + at_k;
-          values = c.codes[1] + (size_t)part.h * c.P * D + at_v;
           tok_part = (part.tile0 + part.first - base) * C::NT;
         }
       }
@@ -843,36 +807,36 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const int i = v ? idx - C::KTASKS : idx;
       const int tok = tok_part + t * C::NT + (v ? i * C::VT : rank * C::KROWS + i / C::SUB * 16);
       const int mine = tok + (lane < 16 || !C::PAIR ? 0 : v ? C::VT - 16 : rank == 0 ? C::KROWS : -C::KROWS);
-      k.t = t;
-      k.idx = idx;
-      k.h = part.h;
-      k.src = (v ? values : keys + i % C::SUB * C::KC) + (tok & (c.P - 1)) * D;
-      if (C::VT == 32) k.second = (((tok + 16) & (c.P - 1)) - (tok & (c.P - 1))) * D;
+      k.n = at;
+      k.off = (part.h << log_row) + (tok & (c.P - 1)) * D + (v ? at_v : at_k + i % C::SUB * C::KC);
       // looked at when the codes are loaded: a wait for it here would cost a latency a task
       if (mine < part.held) k.id = table[mine >> c.logP];
-      at += kConvWarps;
+      at += C::CONV;
       return k;
     };
     auto load = [&](const Task& k, uint4 (&x)[C::LOADS], float& ks, float& vs) {
-      const bool v = k.idx >= C::KTASKS;
+      const int idx = k.n % TASKS;
+      const bool v = idx >= C::KTASKS;
       const int id0 = __shfl_sync(0xffffffffu, k.id, 0), id1 = C::VT == 32 && v ? __shfl_sync(0xffffffffu, k.id, 16) : id0;
       const bool fine = (unsigned)k.id < (unsigned)c.n_blocks;
       ks = vs = k.id == -2 ? 1.0f : kv_nan();
       if (!fine && k.id != -2) kv_raise(c, MSI_ERR_INVALID_ARG);
       const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
+      const uint8_t* codes = c.codes[v] + k.off;
       const int step = v && C::VC == 64 ? 8 * D : C::KC == 64 ? 8 * D : 4 * D;  // codes of the rows a load of the warp covers
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
         const bool up = C::VT == 32 && v && i >= C::LOADS / 2;
         const int id = up ? id1 : id0;
-        // in a task of 32 tokens the second 16 are two loads on
-        const uint8_t* src = k.src + id * block_bytes + (up ? k.second + (i - C::LOADS / 2) * step : i * step);
+        // the second 16 tokens of a task of 32: the next rows, or those of the next block
+        const uint8_t* src = codes + id * block_bytes + (up && c.P == 16 ? (i - C::LOADS / 2) * step : i * step);
         x[i] = make_uint4(z, z, z, z);
         if ((unsigned)id < (unsigned)c.n_blocks) x[i] = *reinterpret_cast<const uint4*>(src);
       }
-      if (!v && k.idx % C::SUB == 0 && fine) {
-        ks = c.scale[0][(size_t)k.id * c.K + k.h];
-        vs = c.scale[1][(size_t)k.id * c.K + k.h];
+      if (!v && idx % C::SUB == 0 && fine) {
+        const size_t at = (size_t)k.id * c.K + (k.off >> log_row);
+        ks = c.scale[0][at];
+        vs = c.scale[1][at];
       }
     };
     Task k0 = look_up(), k1 = look_up(), k2 = look_up();
@@ -881,10 +845,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     load(k0, x0, ks0, vs0);
     load(k1, x1, ks1, vs1);
     auto turn = [&](const Task& k, uint4 (&x)[C::LOADS], float ks, float vs) {
-      const uint32_t st = k.t & 1, ph = ((k.t >> 1) & 1) ^ 1, v = k.idx >= C::KTASKS;
-      const int i = v ? k.idx - C::KTASKS : k.idx;
+      const uint32_t t = k.n / TASKS, idx = k.n % TASKS, st = t & (C::ST - 1), ph = ((t / C::ST) & 1) ^ 1, v = idx >= C::KTASKS;
+      const int i = v ? idx - C::KTASKS : idx;
       // s_bar: full and empty barriers of keys, then of values
-      if (!mbar_wait_warp(kempty + v * 4 + st, ph, abort_flag, kChunkWait)) return false;
+      if (!mbar_wait_warp(kempty + v * 2 * C::ST + st, ph, abort_flag, kChunkWait)) return false;
       const uint32_t tile = st * C::KBYTES + (v ? to_v + i * C::VT * 128 : to_k + i / C::SUB * 16 * 128 + i % C::SUB * (C::KC / 64) * C::KROWS * 128);
       // the swizzle: chunk ^ (row & 7), the row being its first + a multiple of 8, or of 4
       const bool eight = C::KC == 64 || (C::VC == 64 && v);
@@ -898,19 +862,19 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       // the granules' scales: read by softmax after the scores, which follow kfull
       if (!v && i % C::SUB == 0 && (lane & (C::PAIR ? 15 : 31)) == 0) {
         const int g = i / C::SUB + (C::PAIR ? (rank ^ (lane >> 4)) * (C::KROWS / 16) : 0);
-        s_info[k.t & 3][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
+        s_info[t & (2 * C::ST - 1)][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_remote(lead + (v * 4 + st) * 8);
+      if (lane == 0) mbar_arrive_remote(lead + (v * 2 * C::ST + st) * 8);
       return true;
     };
-    while (k0.t >= 0) {
+    while (k0.n >= 0) {
       if (!turn(k0, x0, ks0, vs0)) break;
       k0 = k2;
       load(k0, x0, ks0, vs0);
       k2 = look_up();
-      if (k1.t < 0 || !turn(k1, x1, ks1, vs1)) break;
+      if (k1.n < 0 || !turn(k1, x1, ks1, vs1)) break;
       k1 = k2;
       load(k1, x1, ks1, vs1);
       k2 = look_up();
@@ -923,7 +887,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   __syncthreads();
   if (C::PAIR) cluster_sync_all();  // neither CTA leaves while the other may still reach it
   tc_fence_after();
-  if (warp == kMmaWarp) C::PAIR ? tmem_dealloc_pair(tmem, 512) : tmem_dealloc(tmem, 512);
+  if (warp == C::MMA) C::PAIR ? tmem_dealloc_pair(tmem, 512) : tmem_dealloc(tmem, 512);
   if (tid == 0 && s_abort != 0) kv_raise(c, MSI_ERR_TIMEOUT);
 }
 
