@@ -60,9 +60,7 @@ def build(force: bool = False, verbose_ptxas: bool = False, jobs: int = 0) -> st
 
     def compile_one(item):
         src, obj = item
-        # many kernels a file: compiled in parallel
-        many = ["--split-compile=0"] if os.path.basename(src).startswith("kv") else []
-        cmd = [cc] + _flags(verbose_ptxas) + many + ["-c", src, "-o", obj]
+        cmd = [cc] + _flags(verbose_ptxas) + ["-c", src, "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError("nvcc failed on %s:\n%s\n%s" % (src, r.stdout, r.stderr))

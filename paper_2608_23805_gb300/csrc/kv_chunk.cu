@@ -4,31 +4,34 @@
 // and queries, fp32 scores, the value's scale in the exponent, weights rounded
 // once to fp16.
 //
-// An item is one sequence, key-value head and tile of 128 or 256 rows (query
-// tokens times the head's query heads, so a tile reads the shared keys once).
-// A CTA works on one item at a time, in tiles of NT tokens:
+// An item is one sequence, key-value head and tile of 256 or 512 rows (query
+// tokens times the head's query heads, so a tile reads the shared keys once).  At
+// 128 columns and more two CTAs share an item: each has half of the rows and of
+// the outputs, and converts and holds half of the keys (tokens) and values
+// (columns) for both (cta_group::2).  Tiles of NT tokens go through
 //   conversion warps: 16 tokens of keys or values at a time, from global memory
 //     to registers two turns ahead, to fp16 (two instructions a pair), to
 //     swizzled shared memory;
-//   MMA warp: S = Q K^T (both from shared memory), O += P V (P from TMEM, V with
-//     the columns contiguous);
-//   softmax warps, a row a thread: S from TMEM, P = 2^(c s + log2 sv - M) to
-//     TMEM over S.  M is a running reference: a tile is done in one pass with
-//     the old M unless some sum of 16 weights passes 2^11 (a bound on each of
-//     them, so no maximum is taken); only then is M moved and O rescaled.
-// With two row tiles the tensor core works on one while softmax works on the
-// other; D = 256 leaves TMEM for one row tile, with two S buffers, and two
-// warps share each row's columns.
+//   MMA warps, one a row tile, of the first CTA: S = Q K^T (both from shared
+//     memory), O += P V (P from TMEM, V with the columns contiguous).  Two S of
+//     each row tile, so that the next scores are ready when softmax is;
+//   softmax warps, a row a thread (D = 256: two, each half of the columns): S
+//     from TMEM, P = 2^(c s + log2 sv - M) to TMEM over S.  M is a running
+//     reference: a tile is done in one pass with the old M unless some sum of 16
+//     weights passes 2^11 (a bound on each of them, so no maximum is taken); only
+//     then is M moved and O rescaled.
+// Two row tiles of 128 rows a CTA, and at D = 256, whose O takes half of TMEM, one.
 //
-// The work is the list of all token tiles of all items; each CTA takes an equal
-// run, parts of split items are joined by kv_chunk_join_kernel in order.
+// The work is the list of all token tiles of all items; each CTA (pair) takes an
+// equal run, parts of split items are joined by kv_chunk_join_kernel in order.
 //
-// Measured: 4,096 rows on 32,768 tokens, 16 heads of 128 over 2: 790 us,
-// 1,305 TFLOP/s; four chunks of 3,000 on themselves, D = 256, capped: 457 us.
-// Bound at D <= 128: the gaps between products (the tensor core takes only three
-// or four ahead, so the issuing warp's waits show: 637 us are left without
-// conversion and softmax) and shared memory (the scores' operands take its whole
-// bandwidth, conversion writes 64 KB a tile); at D = 256 the softmax warps' chain.
+// Measured: 4,096 rows on 32,768 tokens, 16 heads of 128 over 2: 692 us,
+// 1,490 TFLOP/s, 0.77 of a large library product; four chunks of 3,000 on
+// themselves, D = 256, capped: 331 us.  Single CTAs with one S a row tile had 790
+// and 457 us (conversion and operand reads filled shared memory), pairs with one S
+// 770 and 364 (a row tile's softmax, its products and the signals between them
+// follow one another).  Bound: the softmax warps (without their arithmetic 566 and
+// 271 us).
 //
 // Every wait is bounded: on expiry the CTA gives up, drains its MMAs, frees
 // TMEM and raises MSI_ERR_TIMEOUT.
@@ -71,9 +74,8 @@ constexpr int kChunkThreads = 512;
 constexpr int kSoftRegs = 144, kConvRegs = 112;
 static_assert(2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
 // What an item costs beside its tiles (queries, first scores, output), in tiles.
-// D = 256, 4 sequences of 3,000 on 3,000: 562, 473, 454, 470 us at 2, 4, 6, 8; 128
-// columns or fewer, where a long item hides it: 826 us at 1, 2 and 4.
-template <int D>
+// D = 256, four chunks of 3,000: 399, 360, 331, 328, 353 us at 2, 3, 4, 5, 6; 8 of
+// 500, D = 64: 24.1, 24.5, 25.5 us at 3, 4, 5; a long item hides it.
 constexpr int kItemCost = 4;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
@@ -320,14 +322,18 @@ __device__ __forceinline__ float chunk_weights(uint32_t ts, const Granule* info,
   float sum = 0.0f;
   over = m == -INFINITY;
   const float mu = over ? 0.0f : m;
-  uint32_t s[2][16];
-  tmem_ld16(ts, s[0]);
+  uint32_t s[2][32];
+  tmem_ld32(ts, s[0]);
+  tmem_wait_regs(s[0]);
+  tmem_ld32(ts + 32, s[1]);
+  Granule all_g[N];
+#pragma unroll
+  for (int gr = 0; gr < N; ++gr) all_g[gr] = info[gr];
 #pragma unroll
   for (int gr = 0; gr < N; ++gr) {
-    tmem_ld_wait(s[gr & 1]);
-    if (gr + 1 < N) tmem_ld16(ts + 16 * (gr + 1), s[(gr + 1) & 1]);
-    const uint32_t (&x)[16] = s[gr & 1];
-    const Granule g = info[gr];
+    if (gr == 2) tmem_wait_regs(s[1]);
+    const uint32_t* x = s[gr >> 1] + 16 * (gr & 1);
+    const Granule g = all_g[gr];
     const float c = crow * g.ks, ad = g.lv - mu;
     uint64_t part[2] = {0, 0};
 #pragma unroll
@@ -458,7 +464,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (a.lse != nullptr) a.lse[i] = kv_nan();
   }
   __syncthreads();  // every warp whole again before the register split
-  PartWalk<kItemCost<D>> walk;
+  PartWalk<kItemCost> walk;
   walk.u = walk.end = 0;
   if (ok && a.plan[0] > 0 && run < a.plan[2]) walk.init(a, run);
   Part part;
@@ -909,7 +915,7 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   const long long begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
   // the item that the next run begins with, if it has tiles in this one
   const int item = a.plan[4 + blockIdx.x + 1];
-  const long long p0 = a.item_pre[item] + kItemCost<D>, p1 = a.item_pre[item + 1];
+  const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
   if (p0 < begin || p0 >= end) return;
   const int parts = runs.owner(p1 - 1) - blockIdx.x + 1;
   const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
@@ -969,7 +975,7 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = smem_attr_once(kv_chunk_kernel<D, FMT, CAP>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT, kItemCost<D>);
+  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT, kItemCost);
   if (e != cudaSuccess) return e;
   if (C::PAIR) {
     cudaLaunchConfig_t cfg = {};
