@@ -621,7 +621,7 @@ typedef struct {
 
 /* Device workspace of one call (256-byte aligned, not shared by calls that may
  * overlap).  *decode_form (may be NULL) receives 1 where the call runs in decode
- * form: max_rows * n_heads / K at most 48, or 64 for D = 64. */
+ * form: max_rows * n_heads / K at most 64, or 48 for D = 256. */
 msi_status msi_kv_workspace_size(const msi_kv* kv, const msi_kv_attention_args* args, size_t* bytes,
                                  int* decode_form);
 

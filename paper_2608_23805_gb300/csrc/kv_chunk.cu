@@ -131,7 +131,7 @@ __device__ __forceinline__ void set_regs() {
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int rows_tile, int nt, int cost) {
+__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int rows_tile, int nt) {
   __shared__ int s_scan[32], s_base[kKvMaxSeqs + 1], s_bad;
   __shared__ int4 s_work[kKvMaxSeqs];  // seq, first row, rows, tokens held
   __shared__ long long s_sum[32], s_pre[kPlanThreads + 1], s_total;
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(KvAttnArgs a, int
       const int r1 = min(w.z * a.G, (rt + 1) * rows_tile) - 1;
       const int see0 = w.w - w.z + rt * rows_tile / a.G, see1 = w.w - w.z + r1 / a.G;
       const int t0 = a.window > 0 ? max(0, see0 - a.window + 1) / nt : 0;
-      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0) + cost;  // an item that sees nothing has a tile too
+      n = max(1, see1 < 0 ? 0 : see1 / nt + 1 - t0) + kItemCost;  // an item that sees nothing has a tile too
       a.items[2 * i] = w;
       a.items[2 * i + 1] = make_int4(h, rt, t0, 0);
     }
@@ -221,7 +221,6 @@ struct Part {
   int first, last, tiles;      // token tiles [first, last) of the item's `tiles` are this CTA's
 };
 
-template <int COST>
 struct PartWalk {
   long long u, end;
   int item;
@@ -236,7 +235,7 @@ struct PartWalk {
   }
   __device__ __forceinline__ bool next(const KvAttnArgs& a, Part& p) {
     while (u < end) {
-      const long long p0 = a.item_pre[item] + COST, p1 = a.item_pre[item + 1];
+      const long long p0 = a.item_pre[item] + kItemCost, p1 = a.item_pre[item + 1];
       const int4 w = a.items[2 * item], it = a.items[2 * item + 1];
       p.first = (int)max(u - p0, 0LL);
       p.last = (int)(min(p1, end) - p0);
@@ -464,7 +463,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (a.lse != nullptr) a.lse[i] = kv_nan();
   }
   __syncthreads();  // every warp whole again before the register split
-  PartWalk<kItemCost> walk;
+  PartWalk walk;
   walk.u = walk.end = 0;
   if (ok && a.plan[0] > 0 && run < a.plan[2]) walk.init(a, run);
   Part part;
@@ -975,7 +974,7 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = smem_attr_once(kv_chunk_kernel<D, FMT, CAP>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT, kItemCost);
+  e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT);
   if (e != cudaSuccess) return e;
   if (C::PAIR) {
     cudaLaunchConfig_t cfg = {};

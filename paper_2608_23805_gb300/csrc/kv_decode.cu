@@ -802,12 +802,12 @@ int kv_decode_pair_cost() { return kPairCost; }
 // More rows than a group holds are several pairs: each reads the codes again, but
 // mostly from L2 (64 sequences of 8,192, D = 128: 63 us for 16 rows, 101 for 32 in
 // two groups, against 157 in one group of 32, whose registers spill; D = 64: 60
-// for 32 in one).  Chunk form takes over where it is as fast for many sequences
-// (D = 128, 48 rows 146 us, 56 rows in chunk form 141; D = 256 263 and 269; D = 64,
-// 64 rows 97 and 72 rows 127); for one sequence of 32,768 decode form has 22, 33
-// and 21 us there, chunk form 66, 88 and 51.
+// for 32 in one).  Chunk form takes over about where it is as fast for many
+// sequences and the gap for one is small (decode form at its most rows, chunk form
+// just above; 64 sequences of 8,192 / one of 32,768): D = 64 95 and 142 / 19 and
+// 33 us, D = 128 181 and 167 / 23 and 33, D = 256 267 and 276 / 32 and 45.
 int kv_decode_tiles(int rows, int D) {
-  return rows <= 8 ? 1 : rows <= 16 ? 2 : D == 64 ? (rows <= 64 ? 4 : 0) : rows <= 48 ? 2 : 0;
+  return rows > (D == 256 ? 48 : 64) ? 0 : rows <= 8 ? 1 : rows <= 16 || D > 64 ? 2 : 4;
 }
 
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s) {

@@ -56,7 +56,7 @@ def test_chunk_of_many_sequences():
     c.attend(order, [65 + i % 2 for i in range(300)], 4)
 
 
-@pytest.mark.parametrize("D,most", [(64, 64), (128, 48), (256, 48)])
+@pytest.mark.parametrize("D,most", [(64, 64), (128, 64), (256, 48)])
 def test_the_largest_decode_call_and_the_next(D, most):
     for rows in (most, most + 1):
         c = KvCase(D=D, K=1, P=32, seed=rows)
