@@ -477,14 +477,16 @@ class KvCache:
         n, heads = cu.numel() - 1, q.shape[1]
         qp, q_stride, rows = self._rows(q, "q", heads)
         if out is None:
-            out = torch.empty_like(q)
-        op, out_stride, out_rows = self._rows(out, "out", heads)
+            out = torch.empty_like(q)  # contiguous: q's rows are
+            op, out_stride = out.data_ptr() if rows else None, heads * self.D
+        else:
+            op, out_stride, out_rows = self._rows(out, "out", heads)
+            if out_rows != rows:
+                raise ValueError("out: the shape of q is needed")
         if lse is None:
             lse = torch.empty((rows, heads), dtype=torch.float32, device=self._device)
         elif tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
             raise ValueError("lse: a contiguous fp32 CUDA tensor [n, heads] is needed")
-        if out_rows != rows:
-            raise ValueError("out: the shape of q is needed")
         a = N.msi_kv_attention_args(n, self._index(seqs, "seqs", n), self._index(cu, "cu"), rows, max_rows, heads, qp,
                                     q_stride, op, out_stride, lse.data_ptr() if rows else None,
                                     self.D ** -0.5 if scale is None else scale, softcap, window,
