@@ -593,7 +593,7 @@ __device__ __forceinline__ void kv_join_many(const KvAttnArgs& a, int R, int n, 
   __shared__ int s_scan[32], s_x;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   if (tid == 0) s_x = -1;
-  int base = 0;  // such pairs before this round's runs
+  int base = 0;  // such pairs before these runs
   for (int i0 = 0; i0 < a.ctas; i0 += kJoinThreads) {
     const int many = i0 + tid < a.ctas && a.split[i0 + tid].w > kJoinFew;
     const int in = block_scan(many, s_scan);
