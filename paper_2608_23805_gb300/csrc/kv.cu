@@ -679,7 +679,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
   if (tiles != 0) a.groups = (a.max_rows * a.G + 8 * tiles - 1) / (8 * tiles);
   a.ctas = kv->sms < 512 ? kv->sms : 512;
-  a.ctas = tiles != 0 ? 2 * a.ctas : kv_chunk_runs(c.D, a.ctas);  // two of the decode form's share an SM
+  a.ctas = tiles != 0 ? 2 * a.ctas : a.ctas / 2;  // two of the decode form's share an SM, two of the chunk form's an item
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;

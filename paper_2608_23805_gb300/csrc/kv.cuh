@@ -92,7 +92,6 @@ int kv_decode_tiles(int rows, int D);  // n8 tiles (1, 2 or 4) of a group of row
 cudaError_t launch_kv_decode(const KvAttnArgs& a, int* launches, cudaStream_t s);
 // Chunk form: rows of one sequence and key-value head in tiles of the MMA's rows.
 int kv_chunk_rows(int D);  // rows of an item
-int kv_chunk_runs(int D, int sms);  // parts that the work is cut into
 cudaError_t launch_kv_chunk(const KvAttnArgs& a, int* launches, cudaStream_t s);
 
 #if defined(__CUDACC__)

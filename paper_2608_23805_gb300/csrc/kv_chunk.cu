@@ -5,10 +5,10 @@
 // once to fp16.
 //
 // An item is one sequence, key-value head and tile of 256 or 512 rows (query
-// tokens times the head's query heads, so a tile reads the shared keys once).  At
-// 128 columns and more two CTAs share an item: each has half of the rows and of
-// the outputs, and converts and holds half of the keys (tokens) and values
-// (columns) for both (cta_group::2).  Tiles of NT tokens go through
+// tokens times the head's query heads, so a tile reads the shared keys once).  Two
+// CTAs share an item: each has half of the rows and of the outputs, and converts
+// and holds half of the keys (tokens) and values (columns) for both (cta_group::2).
+// Tiles of NT tokens go through
 //   conversion warps: 16 tokens of keys or values at a time, from global memory
 //     to registers two turns ahead, to fp16 (two instructions a pair), to
 //     swizzled shared memory;
@@ -22,7 +22,7 @@
 //     then is M moved and O rescaled.
 // Two row tiles of 128 rows a CTA, and at D = 256, whose O takes half of TMEM, one.
 //
-// The work is the list of all token tiles of all items; each CTA (pair) takes an
+// The work is the list of all token tiles of all items; each pair takes an
 // equal run, parts of split items are joined by kv_chunk_join_kernel in order.
 //
 // Measured: 4,096 rows on 32,768 tokens, 16 heads of 128 over 2: 692 us,
@@ -45,26 +45,27 @@ constexpr float kChunkTop = 2048.0f;            // sums of 16 weights above it m
 
 template <int D>
 struct Chunk {
-  static constexpr bool PAIR = D >= 128;          // two CTAs on one item
   static constexpr int NQ = D == 256 ? 1 : 2;     // row tiles
   static constexpr int NT = D == 256 ? 128 : 64;  // tokens of a tile: two S of each row tile and O fill TMEM
   static constexpr int ST = D == 256 ? 2 : 4;     // stages of keys and values
-  static constexpr int TROWS = PAIR ? 256 : 128;  // rows of a row tile, 128 a CTA
+  static constexpr int TROWS = 256;               // rows of a row tile, 128 a CTA
   static constexpr int ROWS = TROWS * NQ;
   static constexpr int NG = NT / 16;              // 16-token granules
   static constexpr int COLS = 64;                 // S columns a softmax thread takes
-  static constexpr int KROWS = PAIR ? NT / 2 : NT;    // a CTA's tokens of the keys,
-  static constexpr int VCOLS = PAIR ? D / 2 : D;      // and columns of the values
+  static constexpr int KROWS = NT / 2;            // a CTA's tokens of the keys,
+  static constexpr int VCOLS = D / 2;             // and columns of the values
   static constexpr int QBYTES = 128 * D * 2;      // a CTA's part of a row tile
   static constexpr int KBYTES = KROWS * D * 2;    // and of a tile's keys, or values
   static constexpr int SMEM = NQ * QBYTES + 2 * ST * KBYTES + 1024;
-  // conversion tasks: 16 tokens of keys, up to 128 columns; 16 tokens of values, or 32 of 64 columns
-  static constexpr int KC = D < 128 ? D : 128, VC = VCOLS < 128 ? VCOLS : 128;
+  // conversion tasks: 16 tokens of keys, up to 128 columns; 16 tokens of values, or 32 of 64 columns or fewer
+  static constexpr int KC = D < 128 ? D : 128;
   static constexpr int SUB = D / KC;              // tasks of 16 tokens' keys
-  static constexpr int VT = PAIR && VC == 64 ? 32 : 16;
+  static constexpr int VT = D == 256 ? 16 : 32;
+  // values: rows of one panel's columns, 128 bytes of 64 or (D = 64) 64 bytes of 32, swizzled by as many
+  static constexpr int VROW = VCOLS < 64 ? 64 : 128;
   static constexpr int KTASKS = KROWS / 16 * SUB, VTASKS = NT / VT;
   static constexpr int LOADS = KC / 32;           // 16-byte loads a lane
-  static_assert(VT * VC == 16 * KC && VC == VCOLS, "all tasks of one size");
+  static_assert(VT * VCOLS == 16 * KC, "all tasks of one size");
   static constexpr int TO = 256;                  // first column of O in TMEM
   // 8 softmax warps, then conversion warps, then an MMA warp a row tile
   static constexpr int SOFT = 8, MMA = 16 - NQ, CONV = MMA - SOFT;
@@ -83,17 +84,8 @@ __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
   asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
   return d;
 }
-// D[tmem] (+)= A[tmem] * B[smem], fp16
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// The same for both CTAs of a pair: each has its rows of A and its columns of B.
+// D[tmem] (+)= A[tmem] * B[smem], fp16, both CTAs of a pair: each has its rows of A
+// and its columns of B
 __device__ __forceinline__ void umma_f16_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                                  uint32_t accumulate) {
   asm volatile(
@@ -396,7 +388,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   uint8_t* sQ = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sK = sQ + C::NQ * C::QBYTES;
   uint8_t* sV = sK + C::ST * C::KBYTES;
-  const int rank = C::PAIR ? (int)cluster_ctarank() : 0, run = C::PAIR ? blockIdx.x >> 1 : blockIdx.x;
+  const int rank = cluster_ctarank(), run = blockIdx.x >> 1;
   // of each stage: keys full and empty, values full and empty
   uint64_t *kfull = s_bar, *kempty = s_bar + C::ST, *vfull = s_bar + 2 * C::ST, *vempty = s_bar + 3 * C::ST;
   // of each row tile and S: scores, weights and product done; of each row tile:
@@ -405,18 +397,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   uint64_t *qfull = s_bar + 28, *ofree = s_bar + 30, *olast = s_bar + 32, *drain = s_bar + 34;
   // What the MMA warps wait for (kfull, vfull, qfull, pfull, ofree) is counted at
   // the first CTA of a pair, for both; what they signal arrives at both.
-  const uint32_t lead = C::PAIR ? mapa_shared(smem_u32(s_bar), 0) : smem_u32(s_bar);
+  const uint32_t lead = mapa_shared(smem_u32(s_bar), 0);
   const uint32_t lead_pfull = lead + 20 * 8, lead_qfull = lead + 28 * 8, lead_ofree = lead + 30 * 8;
   volatile int* abort_flag = &s_abort;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
-    const int both = C::PAIR ? 2 : 1, soft = both * (C::NQ == 2 ? 4 : 8);  // warps of a row tile
+    const int soft = C::NQ == 2 ? 8 : 16;  // warps of a row tile
     for (int i = 0; i < C::ST; ++i) {
-      mbar_init(kfull + i, both * C::KTASKS);
+      mbar_init(kfull + i, 2 * C::KTASKS);
       mbar_init(kempty + i, C::NQ);
-      mbar_init(vfull + i, both * C::VTASKS);
+      mbar_init(vfull + i, 2 * C::VTASKS);
       mbar_init(vempty + i, C::NQ);
     }
     for (int i = 0; i < 4; ++i) {
@@ -434,19 +426,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     s_abort = 0;
   }
   if (warp == C::MMA) {
-    if (C::PAIR) {
-      tmem_alloc_pair(&s_tmem, 512);
-      tmem_relinquish_pair();
-    } else {
-      tmem_alloc(&s_tmem, 512);
-      tmem_relinquish();
-    }
+    tmem_alloc_pair(&s_tmem, 512);
+    tmem_relinquish_pair();
   }
   grid_wait();
   grid_release();
   tc_fence_before();
   __syncthreads();
-  if (C::PAIR) cluster_sync_all();  // also: both CTAs' barriers are there before any arrival from the other
+  cluster_sync_all();  // also: both CTAs' barriers are there before any arrival from the other
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   const bool ok = a.plan[1] != 0;
@@ -685,15 +672,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const uint32_t desc_hi = (uint32_t)(sw128_desc(0) >> 32);
     const uint32_t q_lo = uniform((uint32_t)sw128_desc(smem_u32(sQ)) + q * (C::QBYTES >> 4));
     const uint32_t k_lo = uniform((uint32_t)sw128_desc(smem_u32(sK)));
-    // columns contiguous: 64 of them a panel, panels NT rows of 128 bytes apart
-    const uint32_t v_lo = uniform((smem_u32(sV) >> 4) | ((uint32_t)(C::NT * 128) >> 4 << 16));
+    // columns contiguous: a panel's rows, panels NT rows apart; groups of 8 rows;
+    // descriptor version 1, swizzle mode 2 (128 bytes) or 4 (64)
+    const uint32_t v_lo = uniform((smem_u32(sV) >> 4) | ((uint32_t)(C::NT * C::VROW) >> 4 << 16));
+    constexpr uint32_t v_hi = 8 * C::VROW >> 4 | 1u << 14 | (C::VROW == 128 ? 2u : 4u) << 29;
     const uint32_t tm = uniform(tmem + q * 2 * C::NT), to = uniform(tmem + C::TO + q * D);
     constexpr uint32_t id_s = idesc_f16(C::TROWS, C::NT, 0), id_o = idesc_f16(C::TROWS, D, 1);
     uint32_t kv = 0;            // token tiles before the part's
     uint32_t parts = 0, ns = 0;  // parts begun, and S tiles begun before the part's, of this row tile
     bool go = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, kChunkWait); };
-    auto commit = [](uint64_t* bar) { C::PAIR ? umma_commit_pair(bar) : umma_commit(bar); };
     auto stage = [](uint32_t t) { return t & (C::ST - 1); };
     auto phase = [](uint32_t t) { return t / C::ST; };
     Part ahead;  // read a part early: its loads take as long as a tile
@@ -706,10 +694,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (q > 0 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) <= C::TROWS) {  // no second row tile
         for (uint32_t t = t0; go && t < t0 + n; ++t) {
           go = wait(&kfull[stage(t)], phase(t));
-          if (go && elect_one()) commit(&kempty[stage(t)]);
+          if (go && elect_one()) umma_commit_pair(&kempty[stage(t)]);
           __syncwarp();
           go = go && wait(&vfull[stage(t)], phase(t));
-          if (go && elect_one()) commit(&vempty[stage(t)]);
+          if (go && elect_one()) umma_commit_pair(&vempty[stage(t)]);
           __syncwarp();
         }
         continue;
@@ -722,11 +710,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
-            (C::PAIR ? umma_bf16_pair : umma_bf16)(
+            umma_bf16_pair(
                 tm + buf * C::NT, desc64(q_lo + (((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), desc_hi),
                 desc64(k_lo + ((st * C::KBYTES + (k >> 2) * C::KROWS * 128 + (k & 3) * 32) >> 4), desc_hi), id_s, k != 0);
-          commit(&sfull[2 * q + buf]);
-          commit(&kempty[st]);
+          umma_commit_pair(&sfull[2 * q + buf]);
+          umma_commit_pair(&kempty[st]);
         }
         __syncwarp();
       };
@@ -742,11 +730,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < C::NT / 16; ++k)
-            (C::PAIR ? umma_f16_ts_pair : umma_f16_ts)(
-                to, tm + buf * C::NT + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 2048) >> 4), desc_hi), id_o, (j | k) != 0);
-          commit(&ofull[2 * q + buf]);
-          if (j + 1 == n) commit(&olast[q]);
-          commit(&vempty[st]);
+            umma_f16_ts_pair(
+                to, tm + buf * C::NT + 8 * k, desc64(v_lo + ((st * C::KBYTES + k * 16 * C::VROW) >> 4), v_hi), id_o, (j | k) != 0);
+          umma_commit_pair(&ofull[2 * q + buf]);
+          if (j + 1 == n) umma_commit_pair(&olast[q]);
+          umma_commit_pair(&vempty[st]);
         }
         __syncwarp();
       }
@@ -756,7 +744,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     // every MMA this warp issued has completed before TMEM is released
     __syncwarp();
     if (rank == 0 && elect_one()) {
-      commit(drain + q);
+      umma_commit_pair(drain + q);
       const long long since = clock64();
       while (!mbar_try_wait(drain + q, 0) && clock64() - since < kDrainCycles) {
       }
@@ -777,15 +765,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       int off;  // the lane's first code in the block
     };
     constexpr int TASKS = C::KTASKS + C::VTASKS;
-    // eight lanes write two rows of one 64-column panel: no bank conflicts
-    auto col_of = [&](int width) { return (lane & 3) + (width == 64 ? 0 : (lane >> 4) << 2); };  // 16-code chunk of the row
-    auto row_of = [&](int width) { return (lane >> 2) & (width == 64 ? 7 : 3); };
-    auto to_of = [&](uint8_t* base, int width, int rows) {  // rows 4 apart: chunk ^ 4
+    // `width` columns a row: a lane's 16 codes of the row, and its first row
+    auto col_of = [&](int width) { return width == 32 ? lane & 1 : (lane & 3) + (width == 64 ? 0 : (lane >> 4) << 2); };
+    auto row_of = [&](int width) { return width == 32 ? lane >> 1 : (lane >> 2) & (width == 64 ? 7 : 3); };
+    // where they go: eight lanes write two rows of one 64-column panel, no bank
+    // conflicts; rows 4 apart: chunk ^ 4.  32 columns: rows of 64 bytes, swizzled in pairs
+    auto to_of = [&](uint8_t* base, int width, int rows) {
       const int col = col_of(width), row = row_of(width);
+      if (width == 32) return smem_u32(base) + row * 64 + ((col * 2 ^ ((row >> 1) & 3)) << 4);
       return smem_u32(base) + (col >> 2) * rows * 128 + row * 128 + (((col & 3) * 2 ^ row) << 4);
     };
-    const uint32_t to_k = to_of(sK, C::KC, C::KROWS), to_v = to_of(sV, C::VC, C::NT);
-    const int at_k = row_of(C::KC) * D + col_of(C::KC) * 16, at_v = row_of(C::VC) * D + col_of(C::VC) * 16 + rank * C::VCOLS;
+    const uint32_t to_k = to_of(sK, C::KC, C::KROWS), to_v = to_of(sV, C::VCOLS, C::NT);
+    const int at_k = row_of(C::KC) * D + col_of(C::KC) * 16, at_v = row_of(C::VCOLS) * D + col_of(C::VCOLS) * 16 + rank * C::VCOLS;
     const long long block_bytes = (long long)c.K * c.P * D;
     const int log_row = c.logP + (D == 64 ? 6 : D == 128 ? 7 : 8);  // codes of a block and head
     int n = 0, base = 0;                   // the walk's part: its tiles, the CTA's tiles before it
@@ -811,7 +802,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const bool v = idx >= C::KTASKS;
       const int i = v ? idx - C::KTASKS : idx;
       const int tok = tok_part + t * C::NT + (v ? i * C::VT : rank * C::KROWS + i / C::SUB * 16);
-      const int mine = tok + (lane < 16 || !C::PAIR ? 0 : v ? C::VT - 16 : rank == 0 ? C::KROWS : -C::KROWS);
+      const int mine = tok + (lane < 16 ? 0 : v ? C::VT - 16 : rank == 0 ? C::KROWS : -C::KROWS);
       k.n = at;
       k.off = (part.h << log_row) + (tok & (c.P - 1)) * D + (v ? at_v : at_k + i % C::SUB * C::KC);
       // looked at when the codes are loaded: a wait for it here would cost a latency a task
@@ -828,7 +819,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (!fine && k.id != -2) kv_raise(c, MSI_ERR_INVALID_ARG);
       const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
       const uint8_t* codes = c.codes[v] + k.off;
-      const int step = v && C::VC == 64 ? 8 * D : C::KC == 64 ? 8 * D : 4 * D;  // codes of the rows a load of the warp covers
+      const int step = 512 / (v ? C::VCOLS : C::KC) * D;  // codes of the rows a load of the warp covers
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
         const bool up = C::VT == 32 && v && i >= C::LOADS / 2;
@@ -854,10 +845,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const int i = v ? idx - C::KTASKS : idx;
       // s_bar: full and empty barriers of keys, then of values
       if (!mbar_wait_warp(kempty + v * 2 * C::ST + st, ph, abort_flag, kChunkWait)) return false;
-      const uint32_t tile = st * C::KBYTES + (v ? to_v + i * C::VT * 128 : to_k + i / C::SUB * 16 * 128 + i % C::SUB * (C::KC / 64) * C::KROWS * 128);
-      // the swizzle: chunk ^ (row & 7), the row being its first + a multiple of 8, or of 4
-      const bool eight = C::KC == 64 || (C::VC == 64 && v);
-      const uint32_t step = eight ? 1024 : 512, flip = eight ? 0 : 64;
+      const uint32_t tile = st * C::KBYTES + (v ? to_v + i * C::VT * C::VROW : to_k + i / C::SUB * 16 * 128 + i % C::SUB * (C::KC / 64) * C::KROWS * 128);
+      // the swizzle: chunk ^ (row & 7), the row being its first + a multiple of 4, of
+      // 8, or (32 columns, where it has a period of 8) of 16
+      const bool four = (v ? C::VCOLS : C::KC) == 128;
+      const uint32_t step = four ? 512 : 1024, flip = four ? 64 : 0;
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
         const uint32_t to = (i & 1 ? tile ^ flip : tile) + i * step;
@@ -865,8 +857,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         st_shared_v4(to ^ 16, make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w)));
       }
       // the granules' scales: read by softmax after the scores, which follow kfull
-      if (!v && i % C::SUB == 0 && (lane & (C::PAIR ? 15 : 31)) == 0) {
-        const int g = i / C::SUB + (C::PAIR ? (rank ^ (lane >> 4)) * (C::KROWS / 16) : 0);
+      if (!v && i % C::SUB == 0 && (lane & 15) == 0) {
+        const int g = i / C::SUB + (rank ^ (lane >> 4)) * (C::KROWS / 16);
         s_info[t & (2 * C::ST - 1)][g] = Granule{ks, lg2(vs), vs > 0.0f ? __fdividef(1.0f, vs) : 1.0f, 0.0f};
       }
       fence_proxy_async_smem();
@@ -890,9 +882,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (C::PAIR) cluster_sync_all();  // neither CTA leaves while the other may still reach it
+  cluster_sync_all();  // neither CTA leaves while the other may still reach it
   tc_fence_after();
-  if (warp == C::MMA) C::PAIR ? tmem_dealloc_pair(tmem, 512) : tmem_dealloc(tmem, 512);
+  if (warp == C::MMA) tmem_dealloc_pair(tmem, 512);
   if (tid == 0 && s_abort != 0) kv_raise(c, MSI_ERR_TIMEOUT);
 }
 
@@ -976,24 +968,20 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   e = launch_after(false, kv_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, C::ROWS, C::NT);
   if (e != cudaSuccess) return e;
-  if (C::PAIR) {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(2 * a.ctas);
-    cfg.blockDim = dim3(kChunkThreads);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = s;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, kv_chunk_kernel<D, FMT, CAP>, a);
-  } else {
-    e = launch_after(true, kv_chunk_kernel<D, FMT, CAP>, dim3(a.ctas), dim3(kChunkThreads), C::SMEM, s, a);
-  }
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(2 * a.ctas);
+  cfg.blockDim = dim3(kChunkThreads);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, kv_chunk_kernel<D, FMT, CAP>, a);
   if (e != cudaSuccess) return e;
   e = launch_after(true, kv_chunk_join_kernel<D>, dim3(a.ctas, C::ROWS / kChunkJoinRows), dim3(kChunkJoinThreads), 0, s, a);
   *launches = 3;
@@ -1010,7 +998,6 @@ cudaError_t chunk_d(const KvAttnArgs& a, int* launches, cudaStream_t s) {
 }  // namespace
 
 int kv_chunk_rows(int D) { return D == 64 ? Chunk<64>::ROWS : D == 128 ? Chunk<128>::ROWS : Chunk<256>::ROWS; }
-int kv_chunk_runs(int D, int sms) { return D == 64 ? sms : sms / 2; }
 
 cudaError_t launch_kv_chunk(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   return a.c.D == 64 ? chunk_d<64>(a, launches, s) : a.c.D == 128 ? chunk_d<128>(a, launches, s) : chunk_d<256>(a, launches, s);
