@@ -379,7 +379,10 @@ class KvCache:
     ``BUFFERS``, shapes as in msi_kv_desc; a cache that a program restores or
     shares): if it is given, it has to name all of them, and the cache is not
     emptied.  Every index argument is an int32 CUDA tensor; ``seqs`` None means
-    sequences 0, 1, ...  Nothing here waits for the GPU but ``status``."""
+    sequences 0, 1, ...  Nothing here waits for the GPU but ``status``.
+
+    A step captured in a graph may be replayed between other calls, larger ones
+    too, as long as the cache lives: a workspace that a graph knows is kept."""
 
     BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "recent", "table", "seq_state", "free_ids", "control",
                "weight")
@@ -409,6 +412,8 @@ class KvCache:
         self._lib = lib
         self._device = self.table.device
         self._ws = self._ws_on = None  # workspace, and the stream that it was last used on
+        self._ws_captured = False      # whether a graph holds its address
+        self._ws_kept = []             # workspaces that were replaced after that: the graphs write to them
         self._need = {}
         if buffers is None:
             self.init(stream)
@@ -443,6 +448,13 @@ class KvCache:
         if stream is None:  # the current stream, without making an object for it
             return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return stream.cuda_stream
+
+    @staticmethod
+    def _capturing(stream):
+        if stream is None:
+            return torch._C._cuda_isCurrentStreamCapturing()
+        with torch.cuda.stream(stream):
+            return torch._C._cuda_isCurrentStreamCapturing()
 
     @staticmethod
     def _used_on(stream, *tensors):
@@ -499,6 +511,9 @@ class KvCache:
             need = self._need[key] = b.value
         ws = self._ws
         if ws is None or ws.numel() < need:
+            if self._ws_captured:
+                self._ws_kept.append(ws)
+                self._ws_captured = False
             ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
             self._ws_on = None
         if stream is not None:
@@ -507,6 +522,8 @@ class KvCache:
         if on != self._ws_on:
             ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
             self._ws_on = on
+        if not self._ws_captured:
+            self._ws_captured = self._capturing(stream)
         rc = self._lib.msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), on)
         if rc:
             N.check(rc, "msi_kv_attention")
