@@ -352,22 +352,23 @@ __device__ __forceinline__ float chunk_weights(uint32_t ts, const Granule* info,
   return sum;
 }
 
-// The two warps that share rows (D = 256): whether any lane of either says so.
-// A warp that gives up arrives once (pair_leave) after the abort flag is set;
-// its partner looks at the flag after each of these barriers.
-__device__ __forceinline__ bool pair_any(int id, bool v) {
+// A vote of the two warps that share rows (D = 256): how many of their lanes say
+// so.  The barrier is met by both or by none: a warp whose wait for a tile runs
+// out comes to the vote that would have been its next one with all lanes, the
+// others never have more than one, and both stop after it.  (After each of those
+// waits there is another vote, and both warps have the same votes in the same order.)
+constexpr uint32_t kPairLeave = 32;
+__device__ __forceinline__ uint32_t pair_vote(int id, bool v) {
   uint32_t r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
+      "{\n\t.reg .pred p;\n\t"
       "setp.ne.u32 p, %2, 0;\n\t"
-      "barrier.cta.red.or.pred q, %1, 64, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
+      "barrier.cta.red.popc.u32 %0, %1, 64, p;\n\t}"
       : "=r"(r)
       : "r"(id), "r"((uint32_t)v)
       : "memory");
-  return r != 0;
+  return r;
 }
-__device__ __forceinline__ void pair_leave(int id) { asm volatile("barrier.cta.arrive %0, 64;" ::"r"(id) : "memory"); }
 
 // 16 query elements a step to fp16, in the row's power of two, to swizzled shared memory
 __device__ __forceinline__ void store_query(uint32_t sq, int row, int c8, const uint4& v, float down) {
@@ -464,7 +465,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     const int pair = 1 + (warp & 3);
     const int lr = q * C::TROWS + rank * 128;  // the CTA's first row of the row tile, in the item's
     constexpr int kTopAt = C::NQ == 1 ? 1 : 0, kSumAt = C::NQ == 1 ? 2 : 0;
-    auto gone = [&]() { return __any_sync(0xffffffffu, *abort_flag != 0) != 0; };
+    // a vote (D = 256): whether any lane says so, or kPairLeave
+    auto vote = [&](bool v) { return pair_vote(pair, __any_sync(0xffffffffu, v) && lane == 0); };
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float two_cap = CAP ? 2.0f * kLog2e / a.softcap : 0.0f;
     uint32_t kv = 0, ns = 0, parts = 0;  // token tiles before the part's; S tiles and parts of this row tile
@@ -509,8 +511,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         }
         if (C::NQ == 1) {
           s_pair[0][half][tr] = __uint_as_float(amax);
-          pair_any(pair, false);
-          if (gone()) break;
+          if (vote(false) >= kPairLeave) goto left;
           amax = max(amax, __float_as_uint(s_pair[0][half ^ 1][tr]));
         }
         const uint32_t e = kv_row_exp(amax);
@@ -531,9 +532,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         tc_fence_after();
         if (C::NQ == 1) {
           s_pair[kSumAt][half][tr] = l;
-          pair_any(pair, false);
-          go = !gone();
-          if (!go) break;
+          if (vote(false) >= kPairLeave) goto left;
           l = s_pair[kSumAt][0][tr] + s_pair[kSumAt][1][tr];
         }
         const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
@@ -612,9 +611,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             float top = fmaxf(m, chunk_max<D, CAP, true>(ts + half * C::COLS, info, crow, a.softcap, two_cap, lim, low));
             if (C::NQ == 1) {
               s_pair[kTopAt][half][tr] = top;
-              pair_any(pair, false);
-              go = !gone();
-              if (!go) break;
+              if (vote(false) >= kPairLeave) goto left;
               top = fmaxf(top, s_pair[kTopAt][half ^ 1][tr]);
             }
             if (j > 0) {
@@ -644,9 +641,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
                      : chunk_weights<D, CAP, false>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over);
           over = over && pass == 0;
           // both warps of a pair are through with S here: P goes over it
-          const bool again = C::NQ == 1 ? pair_any(pair, over) : __any_sync(0xffffffffu, over);
-          if (C::NQ == 1) go = !gone();
-          if (!again || !go) break;
+          const uint32_t again = C::NQ == 1 ? vote(over) : __any_sync(0xffffffffu, over);
+          if (C::NQ == 1 && again >= kPairLeave) goto left;
+          if (again == 0) break;
         }
         if (!go) break;
         l += sum;
@@ -660,7 +657,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       kv += n;
       if (!go) break;
     }
-    if (C::NQ == 1 && gone()) pair_leave(pair);
+    if (C::NQ == 1 && !go) pair_vote(pair, true);  // a wait ran out: the partner learns of it at its next vote
+  left:;
   } else {
   set_regs<kConvRegs, false>();  // one instruction for the whole warpgroup
   if (warp >= C::MMA) {
