@@ -382,7 +382,10 @@ class KvCache:
     sequences 0, 1, ...  Nothing here waits for the GPU but ``status``.
 
     A step captured in a graph may be replayed between other calls, larger ones
-    too, as long as the cache lives: a workspace that a graph knows is kept."""
+    too, as long as the cache lives: a workspace that a graph knows is kept.
+
+    A call with `stream` runs there (None: the current stream); calls on one
+    cache have to follow one another on the GPU, which is the caller's to see to."""
 
     BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "recent", "table", "seq_state", "free_ids", "control",
                "weight")
@@ -397,24 +400,26 @@ class KvCache:
                   "recent": ((n_seqs, 2, K, 2 * P, D), torch.bfloat16), "table": ((n_seqs, max_blocks), torch.int32),
                   "seq_state": ((n_seqs, 4), torch.int32), "free_ids": ((n_blocks,), torch.int32),
                   "control": ((8,), torch.int32), "weight": ((n_blocks,), torch.float32)}
-        for name, (shape, dtype) in shapes.items():
-            if buffers is None:
-                t = torch.empty(shape, dtype=dtype, device="cuda")
-            else:
-                t = buffers[name]
-                if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-                    raise ValueError("%s: a contiguous CUDA tensor %s of %s is needed" % (name, shape, dtype))
-            setattr(self, name, t)
+        with torch.cuda.stream(stream):  # None: the current one
+            for name, (shape, dtype) in shapes.items():
+                if buffers is None:
+                    t = torch.empty(shape, dtype=dtype, device="cuda")
+                else:
+                    t = buffers[name]
+                    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+                        raise ValueError("%s: a contiguous CUDA tensor %s of %s is needed" % (name, shape, dtype))
+                setattr(self, name, t)
         d = N.msi_kv_desc(n_seqs, max_blocks, n_blocks, K, D, P, fmt, *[getattr(self, n).data_ptr() for n in self.BUFFERS])
         h = ctypes.c_void_p()
         N.check(lib.msi_kv_create(ctypes.byref(d), ctypes.byref(h)), "msi_kv_create")
         self.h = h
         self._lib = lib
         self._device = self.table.device
-        self._ws = self._ws_on = None  # workspace, and the stream that it was last used on
-        self._ws_captured = False      # whether a graph holds its address
-        self._ws_kept = []             # workspaces that were replaced after that: the graphs write to them
+        self._ws, self._ws_on = None, set()  # workspace, and the streams that it was used on
+        self._ws_captured = False            # whether a graph holds its address
+        self._ws_kept = []                   # workspaces that were replaced after that: the graphs write to them
         self._need = {}
+        self._used_on = set()                # the streams that the buffers were used on
         if buffers is None:
             self.init(stream)
 
@@ -443,40 +448,53 @@ class KvCache:
                 return t.data_ptr(), row if n > 1 else heads * D, n
         raise ValueError("%s: bf16 CUDA rows [n, %d, %d], each contiguous, are needed" % (name, heads, D))
 
-    @staticmethod
-    def _on(stream):
-        if stream is None:  # the current stream, without making an object for it
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-        return stream.cuda_stream
+    # Every call runs on the current stream: one with another stream makes that
+    # the current one (_elsewhere).  What the allocator gives a call then belongs
+    # to the stream that the call's kernels run on.
+
+    def _here(self):
+        """The current stream, on which the cache's buffers are about to be used."""
+        on = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())  # no object is made for it
+        if on not in self._used_on:
+            self._used_on.add(on)
+            stream = torch.cuda.current_stream()
+            for name in self.BUFFERS:
+                getattr(self, name).record_stream(stream)
+        return on
 
     @staticmethod
-    def _capturing(stream):
-        if stream is None:
-            return torch._C._cuda_isCurrentStreamCapturing()
+    def _elsewhere(stream, call, *args):
+        """The call on `stream`: its arguments stay allocated until that stream
+        has used them, and what it makes until the caller's stream has."""
+        here = torch.cuda.current_stream()
         with torch.cuda.stream(stream):
-            return torch._C._cuda_isCurrentStreamCapturing()
-
-    @staticmethod
-    def _used_on(stream, *tensors):
-        """Tensors made here on the current stream and used on another one."""
-        for t in tensors:
-            t.record_stream(stream)
+            made = call(*args)
+        for t in args:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        for t in made or ():
+            t.record_stream(here)
+        return made
 
     def init(self, stream=None):
         """Empty the cache: every block free, no tokens, status 0."""
-        N.check(N.lib().msi_kv_init(self.h, self._on(stream)), "msi_kv_init")
+        if stream is not None:
+            return self._elsewhere(stream, self.init)
+        N.check(N.lib().msi_kv_init(self.h, self._here()), "msi_kv_init")
 
     def append(self, k, v, cu, seqs=None, start=None, stream=None):
         """Rows cu[b] .. cu[b+1] of k and v [n, kv_heads, head_dim] (rows may be
         strided alike) become the tokens of sequence seqs[b] from start[b] on
         (None: at its end); tokens held from there on are dropped first."""
+        if stream is not None:
+            return self._elsewhere(stream, self.append, k, v, cu, seqs, start)
         n = cu.numel() - 1
         kp, stride, rows = self._rows(k, "k", self.K)
         vp, v_stride, v_rows = self._rows(v, "v", self.K)
         if v_rows != rows or v_stride != stride:
             raise ValueError("k and v: as many rows, with the same stride, are needed")
         rc = self._lib.msi_kv_append(self.h, n, self._index(seqs, "seqs", n), self._index(cu, "cu"),
-                                     self._index(start, "start", n), kp, vp, stride, rows, self._on(stream))
+                                     self._index(start, "start", n), kp, vp, stride, rows, self._here())
         if rc:
             N.check(rc, "msi_kv_append")
 
@@ -486,6 +504,8 @@ class KvCache:
         tokens of sequence seqs[b], over what it holds.  max_rows: at least the
         rows of any one sequence.  scale None: head_dim ** -0.5.  observe: add up
         each block's attention weight (decode form).  Returns (out, lse)."""
+        if stream is not None:
+            return self._elsewhere(stream, self.attention, q, cu, max_rows, seqs, out, lse, scale, softcap, window, observe)
         n, heads = cu.numel() - 1, q.shape[1]
         qp, q_stride, rows = self._rows(q, "q", heads)
         if out is None:
@@ -509,21 +529,19 @@ class KvCache:
             b = ctypes.c_size_t()
             N.check(N.lib().msi_kv_workspace_size(self.h, ctypes.byref(a), ctypes.byref(b), None), "msi_kv_workspace_size")
             need = self._need[key] = b.value
+        on = self._here()
         ws = self._ws
         if ws is None or ws.numel() < need:
             if self._ws_captured:
                 self._ws_kept.append(ws)
                 self._ws_captured = False
             ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
-            self._ws_on = None
-        if stream is not None:
-            self._used_on(stream, out, lse)
-        on = self._on(stream)
-        if on != self._ws_on:
-            ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
-            self._ws_on = on
+            self._ws_on = {on}
+        elif on not in self._ws_on:
+            self._ws_on.add(on)
+            ws.record_stream(torch.cuda.current_stream())
         if not self._ws_captured:
-            self._ws_captured = self._capturing(stream)
+            self._ws_captured = torch._C._cuda_isCurrentStreamCapturing()
         rc = self._lib.msi_kv_attention(self.h, ctypes.byref(a), ws.data_ptr(), ws.numel(), on)
         if rc:
             N.check(rc, "msi_kv_attention")
@@ -536,27 +554,31 @@ class KvCache:
         """Sequences that hold more than `keep` blocks keep their first `sinks`,
         their last `recent` and the heaviest others.  seqs: a tensor, or the
         number of sequences 0, 1, ..."""
+        if stream is not None:
+            return self._elsewhere(stream, self.evict, seqs, keep, sinks, recent)
         n, ids = self._which(seqs)
-        rc = self._lib.msi_kv_evict(self.h, n, ids, keep, sinks, recent, self._on(stream))
+        rc = self._lib.msi_kv_evict(self.h, n, ids, keep, sinks, recent, self._here())
         if rc:
             N.check(rc, "msi_kv_evict")
 
     def release(self, seqs, stream=None):
         """End sequences (a tensor, or the number of sequences 0, 1, ...)."""
+        if stream is not None:
+            return self._elsewhere(stream, self.release, seqs)
         n, ids = self._which(seqs)
-        N.check(self._lib.msi_kv_release(self.h, n, ids, self._on(stream)), "msi_kv_release")
+        N.check(self._lib.msi_kv_release(self.h, n, ids, self._here()), "msi_kv_release")
 
     def read(self, cu, rows, seqs=None, first=None, stream=None):
         """The tokens from first[b] on (None: 0) of sequence seqs[b] as bf16 rows
         cu[b] .. cu[b+1] of (k, v) [rows, kv_heads, head_dim]; rows = cu[-1]."""
+        if stream is not None:
+            return self._elsewhere(stream, self.read, cu, rows, seqs, first)
         n = cu.numel() - 1
         k = torch.empty((rows, self.K, self.D), dtype=torch.bfloat16, device=self._device)
         v = torch.empty_like(k)
-        if stream is not None:
-            self._used_on(stream, k, v)
         rc = self._lib.msi_kv_read(self.h, n, self._index(seqs, "seqs", n), self._index(first, "first", n),
                                    self._index(cu, "cu"), rows, k.data_ptr() if rows else None,
-                                   v.data_ptr() if rows else None, self._on(stream))
+                                   v.data_ptr() if rows else None, self._here())
         if rc:
             N.check(rc, "msi_kv_read")
         return k, v
@@ -564,7 +586,7 @@ class KvCache:
     def status(self, stream=None) -> int:
         """Wait for the stream; the cache's status word (MSI_OK: 0), which is cleared."""
         s = ctypes.c_int()
-        N.check(N.lib().msi_kv_status(self.h, self._on(stream), ctypes.byref(s)), "msi_kv_status")
+        N.check(N.lib().msi_kv_status(self.h, _stream(stream), ctypes.byref(s)), "msi_kv_status")
         return s.value
 
     def launches(self) -> int:
