@@ -7,7 +7,7 @@ from kv_case import KvCase, ints, tensor
 from paper_2608_23805_gb300 import api
 
 pytestmark = pytest.mark.gpu
-LONG = 100_000_000  # clock cycles that a stream is kept busy: some 50 ms
+LONG = 400_000_000  # clock cycles that a stream is kept busy: some 200 ms
 
 
 def cache_of(D=128):
@@ -24,7 +24,7 @@ def settle():
 
 
 def test_results_do_not_take_memory_that_the_current_stream_still_reads():
-    n = 600  # a decode call: its kernels need no whole SM, which a busy stream might hold
+    n = 600
     c = KvCase(n_seqs=n, K=2, D=128, P=16, max_blocks=4, n_blocks=4 * n)
     c.append(list(range(n)), [20] * n)
     q, cu = tensor(c.rows(n, 16)), ints(range(n + 1))
@@ -32,15 +32,16 @@ def test_results_do_not_take_memory_that_the_current_stream_still_reads():
     ref, ref_lse = c.cache.attention(q, cu, 1)
     settle()
     # temporaries as large as what the call makes, read late and let go at once
-    old = [torch.full_like(ref, 3.0) for _ in range(4)] + [torch.full_like(ref_lse, 3.0) for _ in range(4)]
+    old = [torch.full_like(ref, 3.0) for _ in range(24)] + [torch.full_like(ref_lse, 3.0) for _ in range(64)]
     torch.cuda.synchronize()
     torch.cuda._sleep(LONG)
     sums = [t.sum(dtype=torch.float32) for t in old]
-    sizes = [t.numel() for t in old]
+    sizes, ptrs = [t.numel() for t in old], [t.data_ptr() for t in old]
     del old
     out, lse = c.cache.attention(q, cu, 1, stream=side)
-    side.synchronize()
     torch.cuda.synchronize()
+    # its kernels may have waited for the busy SM, but nothing orders them with it
+    assert out.data_ptr() not in ptrs and lse.data_ptr() not in ptrs
     assert [float(s) for s in sums] == [3.0 * n for n in sizes]
     assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
 
@@ -109,14 +110,17 @@ def test_a_cache_let_go_with_work_under_way():
     k, v, cu = tensor(c.rows(16000)), tensor(c.rows(16000)), ints([0, 16000])
     cache, c.cache = c.cache, None
     side = torch.cuda.Stream()
+    size, ptrs = cache.k_codes.shape, [cache.k_codes.data_ptr(), cache.v_codes.data_ptr()]
+    torch.full(size, 0x5A, dtype=torch.uint8, device="cuda")  # its kernel is loaded
     settle()
     with torch.cuda.stream(side):
         torch.cuda._sleep(LONG)
     cache.append(k, v, cu, stream=side)
-    size = cache.k_codes.shape
     del cache
-    others = [torch.full(size, 0x5A, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    others = [torch.full(size, 0x5A, dtype=torch.uint8, device="cuda") for _ in range(40)]
+    busy = not side.query()
     torch.cuda.synchronize()
+    assert busy and not set(ptrs) & {t.data_ptr() for t in others}
     assert all(bool((t == 0x5A).all()) for t in others)
 
 
