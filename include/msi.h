@@ -541,8 +541,10 @@ uint64_t msi_kernel_launches(const msi_plan* plan);
  * range, no free block) raise the cache's status word and fail closed: the
  * call that finds one changes nothing else, and while the word is not 0 append,
  * evict and release change nothing and attention writes NaN to every row.  (A
- * table entry out of range is found block by block: its block alone is skipped,
- * rows that would read it are NaN.)  msi_kv_status reads and clears the word.
+ * block number out of range, in a table or among the free ones, is found block
+ * by block: the block alone is skipped, the rest of an append is done; rows that
+ * would read it are NaN, and other rows of that attention call may be.)
+ * msi_kv_status reads and clears the word.
  * ------------------------------------------------------------------------- */
 enum { MSI_KV_Q8 = 0, MSI_KV_E4M3 = 1 };
 

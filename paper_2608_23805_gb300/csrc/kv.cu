@@ -92,6 +92,7 @@ __device__ __forceinline__ uint32_t round_e4m3(uint32_t a, uint32_t b, float inv
 // several blocks.  Bound: memory (16-bit rows in, codes out) for prompts (32,768
 // tokens of 2 heads of 128: 14 us, 3.6 TB/s), latency for single tokens (64
 // sequences: 6 us).
+constexpr int kWrongBlock = 1 << 16;  // in the ticket: CTAs that met a wrong block number, above those that are done
 constexpr int append_threads(int vpt) { return vpt <= 4 ? 1024 : 512; }  // of an SM, by the registers a thread takes
 
 template <int THREADS, int VPT>
@@ -152,6 +153,9 @@ __global__ void __launch_bounds__(THREADS, append_threads(VPT) / THREADS) kv_app
                                                     : 0;
   const bool go = bad == 0 && status == 0;
 
+  // A block number out of range is told to the last CTA with the ticket: the status
+  // word stays as it is until every CTA has looked at it.
+  int wrong = 0;
   const int tasks = go ? s_tot[0] * 2 * c.K : 0;
   for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
     const int block = task / (2 * c.K), h = (task - block * 2 * c.K) >> 1, w = task & 1;
@@ -211,15 +215,13 @@ __global__ void __launch_bounds__(THREADS, append_threads(VPT) / THREADS) kv_app
             c.fmt == MSI_KV_Q8 ? make_uint2(round_q8(q.x, q.y, inv), round_q8(q.z, q.w, inv))
                                : make_uint2(round_e4m3(q.x, q.y, inv), round_e4m3(q.z, q.w, inv));
       }
-      if (tid == 0) {
-        c.scale[w][(size_t)id * c.K + h] = finite ? scale : kv_nan();
-        if (j >= s.had && h == 0 && w == 0) {
-          c.table[(size_t)s.seq * c.max_blocks + j] = id;
-          c.weight[id] = 0.0f;
-        }
-      }
-    } else if (tid == 0) {
-      kv_raise(c, MSI_ERR_INVALID_ARG);
+      if (tid == 0) c.scale[w][(size_t)id * c.K + h] = finite ? scale : kv_nan();
+    } else {
+      wrong = kWrongBlock;
+    }
+    if (tid == 0 && j >= s.had && h == 0 && w == 0) {
+      c.table[(size_t)s.seq * c.max_blocks + j] = id;  // a wrong one too: what reads it finds it so
+      if (id_ok) c.weight[id] = 0.0f;
     }
 
     // the last two blocks' new rows into `recent`.  The ring has two blocks: a
@@ -252,7 +254,8 @@ __global__ void __launch_bounds__(THREADS, append_threads(VPT) / THREADS) kv_app
   __syncthreads();
   if (tid == 0) {
     __threadfence();
-    s_last = atomicAdd(reinterpret_cast<unsigned*>(c.control + 2), 1u) == gridDim.x - 1;
+    const unsigned before = atomicAdd(reinterpret_cast<unsigned*>(c.control + 2), 1u + wrong);
+    s_last = before % kWrongBlock == gridDim.x - 1 ? 1 + (before + wrong) / kWrongBlock : 0;
   }
   __syncthreads();
   if (s_last == 0) return;
@@ -267,10 +270,9 @@ __global__ void __launch_bounds__(THREADS, append_threads(VPT) / THREADS) kv_app
       const int lo = (((pos - 1) >> c.logP) - 1) * c.P;
       c.seq[s.seq] = make_int4(s.end, pos, max(min(s.from, s.start + s.shift), lo), 0);
     }
-  } else if (tid == 0 && bad != 0) {
-    kv_raise(c, bad);
   }
   if (tid == 0) {
+    if (bad != 0 || s_last > 1) kv_raise(c, bad != 0 ? bad : (int)MSI_ERR_INVALID_ARG);
     c.control[2] = 0;
     if (go) c.control[0] = n_free - s_tot[1] + s_tot[2];
   }
