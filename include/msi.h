@@ -632,7 +632,9 @@ msi_status msi_kv_workspace_size(const msi_kv* kv, const msi_kv_attention_args* 
  * the tokens up to it (append first, then attend).  A row that sees no token
  * gives 0 and lse -inf.  Scores, sums and statistics are fp32; the attention
  * weights are rounded to fp16 before they multiply the values.  MSI_KV_OBSERVE
- * outside decode form returns MSI_ERR_UNSUPPORTED. */
+ * outside decode form returns MSI_ERR_UNSUPPORTED.  Device error beside those of
+ * all calls: MSI_ERR_TIMEOUT, a wait within the chunk form's kernel ran out;
+ * every row is NaN then. */
 msi_status msi_kv_attention(msi_kv* kv, const msi_kv_attention_args* args, void* workspace,
                             size_t workspace_bytes, msi_stream stream);
 
@@ -658,6 +660,19 @@ msi_status msi_kv_read(msi_kv* kv, int n, const int32_t* seqs, const int32_t* fi
 /* Wait for `stream`, return the cache's status word (an msi_status value) and
  * clear it. */
 msi_status msi_kv_status(msi_kv* kv, msi_stream stream, int* device_status);
+
+/* Limit of every device wait of the chunk form's kernel, in SM clock cycles
+ * (clock64); cycles <= 0 restores the default of 4e9 (~2 s at GB300 clocks).  A
+ * wait that runs out raises MSI_ERR_TIMEOUT; the kernel still waits, with its own
+ * ~10 ms bound, for the MMAs that it issued, frees its TMEM and returns, so the
+ * context stays usable.  Applies to calls enqueued after this one. */
+msi_status msi_kv_set_wait_cycles(msi_kv* kv, int64_t cycles);
+
+/* For tests of that path (no GPU fault): in the next attention call in chunk
+ * form one warp of the named kind waits on a barrier that nothing arrives at.
+ * 0 takes the request back. */
+enum { MSI_KV_STALL_SOFTMAX = 1, MSI_KV_STALL_MMA = 2, MSI_KV_STALL_CONVERSION = 3 };
+msi_status msi_kv_inject_stall(msi_kv* kv, int where);
 
 /* Number of kernels launched through the handle. */
 uint64_t msi_kv_kernel_launches(const msi_kv* kv);

@@ -589,6 +589,14 @@ class KvCache:
         N.check(N.lib().msi_kv_status(self.h, _stream(stream), ctypes.byref(s)), "msi_kv_status")
         return s.value
 
+    def set_wait_cycles(self, cycles: int):
+        """Limit of the chunk form's device waits (msi_kv_set_wait_cycles); 0: the default."""
+        N.check(N.lib().msi_kv_set_wait_cycles(self.h, int(cycles)), "msi_kv_set_wait_cycles")
+
+    def inject_stall(self, where: int):
+        """A warp of the next chunk call waits in vain (msi_kv_inject_stall)."""
+        N.check(N.lib().msi_kv_inject_stall(self.h, int(where)), "msi_kv_inject_stall")
+
     def launches(self) -> int:
         return int(N.lib().msi_kv_kernel_launches(self.h))
 

@@ -628,6 +628,8 @@ struct msi_kv {
   KvCache c;
   int dev, sms;
   std::atomic<unsigned long long> launches;
+  std::atomic<long long> wait_cycles{kKvWaitCycles};
+  std::atomic<int> stall{0};  // of the next call in chunk form
 };
 
 namespace {
@@ -818,8 +820,14 @@ msi_status msi_kv_attention(msi_kv* kv, const msi_kv_attention_args* args, void*
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)
     return MSI_ERR_WORKSPACE;
   int kernels = 0;
-  const cudaError_t e = kv_decode_tiles(a.max_rows * a.G, a.c.D) != 0 ? launch_kv_decode(a, &kernels, stream)
-                                                                      : launch_kv_chunk(a, &kernels, stream);
+  cudaError_t e;
+  if (kv_decode_tiles(a.max_rows * a.G, a.c.D) != 0) {
+    e = launch_kv_decode(a, &kernels, stream);
+  } else {
+    a.wait_limit = kv->wait_cycles.load();
+    a.stall = kv->stall.exchange(0);
+    e = launch_kv_chunk(a, &kernels, stream);
+  }
   return launched(kv, e, "msi_kv_attention", kernels);
 }
 
@@ -862,6 +870,18 @@ msi_status msi_kv_status(msi_kv* kv, msi_stream stream, int* device_status) {
   if (e == cudaSuccess && word != 0) e = cudaMemsetAsync(kv->c.control + 1, 0, sizeof(int), stream);
   if (e != cudaSuccess) return note_cuda_error(e, "msi_kv_status");
   *device_status = word;
+  return MSI_OK;
+}
+
+msi_status msi_kv_set_wait_cycles(msi_kv* kv, int64_t cycles) {
+  if (kv == nullptr) return MSI_ERR_INVALID_ARG;
+  kv->wait_cycles = cycles > 0 ? (long long)cycles : kKvWaitCycles;
+  return MSI_OK;
+}
+
+msi_status msi_kv_inject_stall(msi_kv* kv, int where) {
+  if (kv == nullptr || where < 0 || where > MSI_KV_STALL_CONVERSION) return MSI_ERR_INVALID_ARG;
+  kv->stall = where;
   return MSI_OK;
 }
 

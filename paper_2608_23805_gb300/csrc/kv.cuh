@@ -9,6 +9,8 @@ namespace msi {
 
 constexpr int kKvMaxSeqs = 1024;
 constexpr int kKvMaxHeads = 64;
+constexpr long long kKvWaitCycles = 4000000000LL;  // default limit of a device wait
+constexpr int kKvStallSoftmax = MSI_KV_STALL_SOFTMAX, kKvStallMma = MSI_KV_STALL_MMA, kKvStallConversion = MSI_KV_STALL_CONVERSION;
 constexpr float kKvTiny = 1e-20f;  // least absolute maximum of a block: its scale stays a normal number
 
 // The cache as the kernels see it (msi_kv_desc).
@@ -65,6 +67,8 @@ struct KvAttnArgs {
   float* lse;
   float scale, softcap;
   int window, observe;
+  int stall;             // chunk form: the kind of warp that waits in vain (msi_kv_inject_stall), 0: none
+  long long wait_limit;  // chunk form: clock64 cycles of a wait
   int ctas;            // CTAs that share the work
   int groups;          // decode form: most groups of rows of a sequence and head
   // workspace
@@ -77,7 +81,7 @@ struct KvAttnArgs {
   // chunk form: the items (sequence, key-value head, row tile) and the prefix of their token tiles
   int4* items;            // [2 max_items] {sequence, first row, rows, held}, {head, row tile, first token tile, 0}
   long long* item_pre;    // [max_items + 1]; decode form: [n + 1] steps before each sequence's (observe)
-  int* plan;              // [4 + ctas] items, whether every sequence is in range, CTAs; then each CTA's first item
+  int* plan;              // [4 + ctas] items, whether every sequence is in range, CTAs, whether a wait ran out; then each CTA's first item
   int max_items;
 };
 

@@ -34,13 +34,12 @@
 // 271 us).
 //
 // Every wait is bounded: on expiry the CTA gives up, drains its MMAs, frees
-// TMEM and raises MSI_ERR_TIMEOUT.
+// TMEM and raises MSI_ERR_TIMEOUT; the join then makes every row of the call NaN.
 #include "kv.cuh"
 
 namespace msi {
 namespace {
 
-constexpr long long kChunkWait = 4000000000LL;  // clock64 cycles of a wait
 constexpr float kChunkTop = 2048.0f;            // sums of 16 weights above it move the reference
 
 template <int D>
@@ -201,6 +200,7 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvAttnArgs a, int rows_tile,
     a.plan[0] = items;
     a.plan[1] = ok;
     a.plan[2] = ctas;
+    a.plan[3] = 0;  // a wait ran out
   }
 }
 
@@ -377,11 +377,24 @@ __device__ __forceinline__ void store_query(uint32_t sq, int row, int c8, const 
                           pack_f16x2(bf16_lo(v.z) * down, bf16_hi(v.z) * down), pack_f16x2(bf16_lo(v.w) * down, bf16_hi(v.w) * down)));
 }
 
+// Fail closed: no row of the call can be read as an answer.  Threads i0, i0 + step, ..
+template <int D>
+__device__ __forceinline__ void chunk_fail(const KvAttnArgs& a, long long i0, long long step) {
+  const long long vecs = (long long)a.n_rows * a.H * (D / 8);
+  for (long long i = i0; i < vecs; i += step) {
+    const long long row = i / (a.H * (D / 8));
+    *reinterpret_cast<uint4*>(a.out + row * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
+        make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+  }
+  if (a.lse != nullptr)
+    for (long long i = i0; i < (long long)a.n_rows * a.H; i += step) a.lse[i] = kv_nan();
+}
+
 template <int D, int FMT, bool CAP>
 __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a) {
   using C = Chunk<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bar[40];
+  __shared__ __align__(8) uint64_t s_bar[40];  // the last: nobody arrives there (KvAttnArgs::stall)
   __shared__ __align__(16) Granule s_info[2 * C::ST][C::NG];
   __shared__ float s_pair[C::NQ == 1 ? 3 : 1][2][128];  // of two warps that share rows: query maximum, reference, sum
   __shared__ uint32_t s_tmem;
@@ -395,7 +408,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   // of each row tile and S: scores, weights and product done; of each row tile:
   // queries there, O free, a part's last product done
   uint64_t *sfull = s_bar + 16, *pfull = s_bar + 20, *ofull = s_bar + 24;
-  uint64_t *qfull = s_bar + 28, *ofree = s_bar + 30, *olast = s_bar + 32, *drain = s_bar + 34;
+  uint64_t *qfull = s_bar + 28, *ofree = s_bar + 30, *olast = s_bar + 32, *drain = s_bar + 34, *never = s_bar + 39;
   // What the MMA warps wait for (kfull, vfull, qfull, pfull, ofree) is counted at
   // the first CTA of a pair, for both; what they signal arrives at both.
   const uint32_t lead = mapa_shared(smem_u32(s_bar), 0);
@@ -423,6 +436,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       mbar_init(olast + i, 1);
       mbar_init(drain + i, 1);
     }
+    mbar_init(never, 1);
     mbar_fence_init();
     s_abort = 0;
   }
@@ -438,18 +452,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   const bool ok = a.plan[1] != 0;
-  if (!ok) {
-    // fail closed: no row of the call can be read as an answer
-    const long long vecs = (long long)a.n_rows * a.H * (D / 8);
-    for (long long i = (long long)blockIdx.x * kChunkThreads + tid; i < vecs; i += (long long)gridDim.x * kChunkThreads) {
-      const long long row = i / (a.H * (D / 8));
-      *reinterpret_cast<uint4*>(a.out + row * a.out_stride + (i - row * a.H * (D / 8)) * 8) =
-          make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
-    }
-    for (long long i = (long long)blockIdx.x * kChunkThreads + tid; i < (long long)a.n_rows * a.H;
-         i += (long long)gridDim.x * kChunkThreads)
-      if (a.lse != nullptr) a.lse[i] = kv_nan();
-  }
+  if (!ok) chunk_fail<D>(a, (long long)blockIdx.x * kChunkThreads + tid, (long long)gridDim.x * kChunkThreads);
   __syncthreads();  // every warp whole again before the register split
   PartWalk walk;
   walk.u = walk.end = 0;
@@ -527,7 +530,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         __syncwarp();
       }
       if (pending) {
-        go = mbar_wait_warp(&olast[q], (parts - 1) & 1, abort_flag, kChunkWait);
+        go = mbar_wait_warp(&olast[q], (parts - 1) & 1, abort_flag, a.wait_limit);
         if (!go) break;
         tc_fence_after();
         if (C::NQ == 1) {
@@ -586,6 +589,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       slot = 2 * run + (part.first > 0 ? 0 : 1);
       m = -INFINITY;
       l = 0.0f;
+      if (a.stall == kKvStallSoftmax && blockIdx.x == 0 && warp == 0) {
+        go = mbar_wait_warp(never, 0, abort_flag, a.wait_limit);
+        if (!go) break;
+      }
       const int see = part.held - part.rows + qi;
       // tiles that every row of this row tile sees whole
       const int r_end = min(rows, part.row_tile * C::ROWS + lr + 128) - 1;
@@ -595,7 +602,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       for (int j = 0; j < n; ++j) {
         const uint32_t mine = ns++;
         const int buf = 2 * q + (mine & 1);
-        go = mbar_wait_warp(&sfull[buf], (mine >> 1) & 1, abort_flag, kChunkWait);
+        go = mbar_wait_warp(&sfull[buf], (mine >> 1) & 1, abort_flag, a.wait_limit);
         if (!go) break;
         tc_fence_after();
         const Granule* info = s_info[(kv + j) & (2 * C::ST - 1)] + half * (C::COLS / 16);
@@ -617,7 +624,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             if (j > 0) {
               // the output so far, once the last product is in it
               const uint32_t last = mine - 1;
-              go = mbar_wait_warp(&ofull[2 * q + (last & 1)], (last >> 1) & 1, abort_flag, kChunkWait);
+              go = mbar_wait_warp(&ofull[2 * q + (last & 1)], (last >> 1) & 1, abort_flag, a.wait_limit);
               if (!go) break;
               tc_fence_after();
               const float f = top == -INFINITY ? 1.0f : ex2(m - top);
@@ -679,7 +686,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     uint32_t kv = 0;            // token tiles before the part's
     uint32_t parts = 0, ns = 0;  // parts begun, and S tiles begun before the part's, of this row tile
     bool go = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, kChunkWait); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, a.wait_limit); };
     auto stage = [](uint32_t t) { return t & (C::ST - 1); };
     auto phase = [](uint32_t t) { return t / C::ST; };
     Part ahead;  // read a part early: its loads take as long as a tile
@@ -687,6 +694,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     while (go && __any_sync(0xffffffffu, more)) {
       part = ahead;
       more = walk.next(a, ahead);
+      if (a.stall == kKvStallMma && blockIdx.x == 0 && q == 0) {
+        go = wait(never, 0);
+        if (!go) break;
+      }
       const uint32_t n = uniform(part.last - part.first), t0 = uniform(kv), n0 = uniform(ns);
       kv += n;
       if (q > 0 && (int)uniform(part.rows * a.G - part.row_tile * C::ROWS) <= C::TROWS) {  // no second row tile
@@ -842,7 +853,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const uint32_t t = k.n / TASKS, idx = k.n % TASKS, st = t & (C::ST - 1), ph = ((t / C::ST) & 1) ^ 1, v = idx >= C::KTASKS;
       const int i = v ? idx - C::KTASKS : idx;
       // s_bar: full and empty barriers of keys, then of values
-      if (!mbar_wait_warp(kempty + v * 2 * C::ST + st, ph, abort_flag, kChunkWait)) return false;
+      if (!mbar_wait_warp(kempty + v * 2 * C::ST + st, ph, abort_flag, a.wait_limit)) return false;
       const uint32_t tile = st * C::KBYTES + (v ? to_v + i * C::VT * C::VROW : to_k + i / C::SUB * 16 * 128 + i % C::SUB * (C::KC / 64) * C::KROWS * 128);
       // the swizzle: chunk ^ (row & 7), the row being its first + a multiple of 4, of
       // 8, or (32 columns, where it has a period of 8) of 16
@@ -864,7 +875,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       if (lane == 0) mbar_arrive_remote(lead + (v * 2 * C::ST + st) * 8);
       return true;
     };
+    const bool stall = a.stall == kKvStallConversion && blockIdx.x == 0 && warp == C::SOFT;
     while (k0.n >= 0) {
+      if (stall && !mbar_wait_warp(never, 0, abort_flag, a.wait_limit)) break;
       if (!turn(k0, x0, ks0, vs0)) break;
       k0 = k2;
       load(k0, x0, ks0, vs0);
@@ -883,7 +896,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   cluster_sync_all();  // neither CTA leaves while the other may still reach it
   tc_fence_after();
   if (warp == C::MMA) tmem_dealloc_pair(tmem, 512);
-  if (tid == 0 && s_abort != 0) kv_raise(c, MSI_ERR_TIMEOUT);
+  if (tid == 0 && s_abort != 0) {
+    kv_raise(c, MSI_ERR_TIMEOUT);
+    a.plan[3] = 1;
+  }
 }
 
 // Joins the parts of each split item: CTA x takes the item that begins in run x
@@ -896,10 +912,16 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   grid_wait();
   grid_release();
   const KvCache& c = a.c;
-  if (a.plan[1] == 0 || a.plan[0] == 0) return;  // every row is NaN already, or there is none
-  const int ctas = a.plan[2];
+  const int4 plan = *reinterpret_cast<const int4*>(a.plan);  // items, in range, CTAs, a wait ran out
+  if (plan.y == 0 || plan.x == 0) return;  // every row is NaN already, or there is none
+  if (plan.w != 0) {  // rows that nobody came to are among those that are not split
+    chunk_fail<D>(a, ((long long)blockIdx.y * gridDim.x + blockIdx.x) * kChunkJoinThreads + threadIdx.x,
+                  (long long)gridDim.x * gridDim.y * kChunkJoinThreads);
+    return;
+  }
+  const int ctas = plan.z;
   if ((int)blockIdx.x + 1 >= ctas) return;
-  const long long total = a.item_pre[a.plan[0]];
+  const long long total = a.item_pre[plan.x];
   const KvRuns runs = {total, ctas};
   const long long begin = runs.begin(blockIdx.x), end = runs.begin(blockIdx.x + 1);
   // the item that the next run begins with, if it has tiles in this one

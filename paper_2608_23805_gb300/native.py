@@ -33,6 +33,7 @@ MSI_TRACE_HIT, MSI_TRACE_STAGE, MSI_TRACE_EVICT, MSI_TRACE_PREFETCH = 0, 1, 2, 3
 MSI_SLOT_VACANT, MSI_SLOT_LOADING, MSI_SLOT_DEVICE_READY, MSI_SLOT_IN_USE, MSI_SLOT_RECYCLABLE = range(5)
 MSI_KV_Q8, MSI_KV_E4M3 = 0, 1
 MSI_KV_OBSERVE = 1
+MSI_KV_STALL_SOFTMAX, MSI_KV_STALL_MMA, MSI_KV_STALL_CONVERSION = 1, 2, 3
 MSI_FWD_RESIDUAL = 1
 MSI_FWD_SINGLE_CTA = 2
 MSI_FWD_SHARED_UNGATED = 4
@@ -163,6 +164,8 @@ _SIGS = {
     "msi_kv_release": (ctypes.c_int, [_P, ctypes.c_int, _P, _P]),
     "msi_kv_read": (ctypes.c_int, [_P, ctypes.c_int, _P, _P, _P, ctypes.c_int, _P, _P, _P]),
     "msi_kv_status": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_int)]),
+    "msi_kv_set_wait_cycles": (ctypes.c_int, [_P, ctypes.c_int64]),
+    "msi_kv_inject_stall": (ctypes.c_int, [_P, ctypes.c_int]),
     "msi_kv_kernel_launches": (ctypes.c_uint64, [_P]),
     "msi_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "msi_last_cuda_error": (ctypes.c_char_p, []),
