@@ -485,26 +485,38 @@ __device__ __forceinline__ void mbar_arrive_expect_tx(uint64_t* bar, uint32_t by
                : "memory");
 }
 
+// CLUSTER: what threads of the other CTA did before they arrived is seen too.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
+  if (CLUSTER)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
   return ok != 0;
 }
 
 // Bounded wait: returns false (and raises the CTA's abort flag) when the wait
 // exceeds `limit` clock64 cycles or another role already aborted.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                           long long limit) {
-  if (mbar_try_wait(bar, parity)) return true;
+  if (mbar_try_wait<CLUSTER>(bar, parity)) return true;
   const long long t0 = clock64();
   while (true) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (mbar_try_wait<CLUSTER>(bar, parity)) return true;
     if (*abort_flag) return false;
     if (clock64() - t0 > limit) {
       *abort_flag = 1;
@@ -587,12 +599,21 @@ __device__ __forceinline__ uint32_t mapa_shared(uint32_t saddr, uint32_t rank) {
   return r;
 }
 // Arrive on a barrier of a CTA of this cluster (shared::cluster address).
-// Default semantics (release, CTA scope), as for a local arrive: the pair
-// protocol orders data through the barriers' own completion mechanisms (TMA
-// transaction counts, tcgen05.commit), so no cluster-wide fence is needed on
-// the per-stage path.
+// Default semantics (release, CTA scope), as for a local arrive: where data come
+// by TMA and go by MMAs, the barriers' own completion mechanisms order them
+// (transaction counts, tcgen05.commit), so no cluster-wide fence is needed on
+// the per-stage path.  Not for data that the arriving threads stored themselves.
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// The same with what this thread stored before it, for threads of either CTA that
+// wait with cluster scope (mbar_try_wait<true>).
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Without any order of memory: for what tcgen05 fences order (TMEM).
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // Every thread of both CTAs of the cluster.
 __device__ __forceinline__ void cluster_sync_all() {
@@ -667,9 +688,10 @@ __device__ __forceinline__ uint32_t uniform(uint32_t v) {
 }
 // A wait of the whole warp, with one answer; the warp is converged after it
 // (what follows may be warp-wide or an aligned TMEM access).
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                                long long limit) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
+  return __all_sync(0xffffffffu, mbar_wait<CLUSTER>(bar, parity, abort_flag, limit));
 }
 
 // D[tmem] (+)= A[smem] * B[smem]^T, bf16 inputs, fp32 accumulate.

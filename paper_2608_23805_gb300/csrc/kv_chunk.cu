@@ -410,9 +410,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   uint64_t *sfull = s_bar + 16, *pfull = s_bar + 20, *ofull = s_bar + 24;
   uint64_t *qfull = s_bar + 28, *ofree = s_bar + 30, *olast = s_bar + 32, *drain = s_bar + 34, *never = s_bar + 39;
   // What the MMA warps wait for (kfull, vfull, qfull, pfull, ofree) is counted at
-  // the first CTA of a pair, for both; what they signal arrives at both.
-  const uint32_t lead = mapa_shared(smem_u32(s_bar), 0);
-  const uint32_t lead_pfull = lead + 20 * 8, lead_qfull = lead + 28 * 8, lead_ofree = lead + 30 * 8;
+  // the first CTA of a pair, for both; what they signal arrives at both.  Weights
+  // and outputs are in TMEM: tcgen05 fences order them.  Queries, keys and values
+  // are ordinary stores to a CTA's own memory.  Those of the second CTA are counted
+  // there, and its MMA warps, which issue nothing, pass the count on with a release
+  // for the cluster: one fence a stage by a warp with nothing else under way.  (A
+  // release by each storing warp waits for its loads ahead: 987 us for 4,096 rows on
+  // 32,768 tokens.)
+  const uint32_t lead_pfull = mapa_shared(smem_u32(pfull), 0), lead_ofree = lead_pfull + 10 * 8;
   volatile int* abort_flag = &s_abort;
   const KvCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -420,9 +425,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   if (tid == 0) {
     const int soft = C::NQ == 2 ? 8 : 16;  // warps of a row tile
     for (int i = 0; i < C::ST; ++i) {
-      mbar_init(kfull + i, 2 * C::KTASKS);
+      mbar_init(kfull + i, C::KTASKS + (rank == 0));
       mbar_init(kempty + i, C::NQ);
-      mbar_init(vfull + i, 2 * C::VTASKS);
+      mbar_init(vfull + i, C::VTASKS + (rank == 0));
       mbar_init(vempty + i, C::NQ);
     }
     for (int i = 0; i < 4; ++i) {
@@ -431,7 +436,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       mbar_init(ofull + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(qfull + i, soft);
+      mbar_init(qfull + i, soft / 2 + (rank == 0));
       mbar_init(ofree + i, soft);
       mbar_init(olast + i, 1);
       mbar_init(drain + i, 1);
@@ -526,7 +531,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         for (int i = 0; i < QV; ++i) store_query(sq, tr, half * QV + i, finite ? v[i] : make_uint4(0, 0, 0, 0), down);
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(lead_qfull + 8 * q);
+        if (lane == 0) mbar_arrive(qfull + q);
         __syncwarp();
       }
       if (pending) {
@@ -565,7 +570,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         __syncwarp();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(lead_ofree + 8 * q);
+        if (lane == 0) mbar_arrive_relaxed(lead_ofree + 8 * q);
         __syncwarp();
         if (valid && half == 0) {
           if (split) {
@@ -658,7 +663,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(lead_pfull + 8 * buf);
+        if (lane == 0) mbar_arrive_relaxed(lead_pfull + 8 * buf);
         __syncwarp();
       }
       kv += n;
@@ -686,9 +691,29 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     uint32_t kv = 0;            // token tiles before the part's
     uint32_t parts = 0, ns = 0;  // parts begun, and S tiles begun before the part's, of this row tile
     bool go = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity & 1, abort_flag, a.wait_limit); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp<true>(bar, parity & 1, abort_flag, a.wait_limit); };
     auto stage = [](uint32_t t) { return t & (C::ST - 1); };
     auto phase = [](uint32_t t) { return t / C::ST; };
+    if (rank != 0) {
+      // Pass the second CTA's queries (of row tile q), keys and values on.  A part's
+      // first keys come before its queries; the next keys are asked for before a
+      // tile's values, as the issuers do.
+      auto pass = [&](uint64_t* bar, uint32_t parity) {
+        go = go && wait(bar, parity);
+        if (go && lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(bar), 0));
+        __syncwarp();
+      };
+      while (go && walk.next(a, part)) {
+        const uint32_t n = part.last - part.first;
+        if (q == 0) pass(&kfull[stage(kv)], phase(kv));
+        if (q == 0 || part.rows * a.G - part.row_tile * C::ROWS > C::TROWS) pass(&qfull[q], parts++);
+        for (uint32_t t = kv; go && t < kv + n; ++t) {
+          if (q == 0 && t + 1 < kv + n) pass(&kfull[stage(t + 1)], phase(t + 1));
+          if (q == C::NQ - 1) pass(&vfull[stage(t)], phase(t));
+        }
+        kv += n;
+      }
+    }
     Part ahead;  // read a part early: its loads take as long as a tile
     bool more = rank == 0 && walk.next(a, ahead);  // the first CTA of a pair issues for both
     while (go && __any_sync(0xffffffffu, more)) {
@@ -872,7 +897,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_remote(lead + (v * 2 * C::ST + st) * 8);
+      if (lane == 0) mbar_arrive(kfull + v * 2 * C::ST + st);
       return true;
     };
     const bool stall = a.stall == kKvStallConversion && blockIdx.x == 0 && warp == C::SOFT;
