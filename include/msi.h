@@ -604,12 +604,13 @@ enum {
 
 /* One attention call (host struct of device pointers and plain values). */
 typedef struct {
-  int n;                /* sequences */
-  const int32_t* seqs;  /* [n] or NULL: 0 .. n-1 */
+  int n;                /* sequences, at most the cache's */
+  const int32_t* seqs;  /* [n] or NULL: 0 .. n-1; distinct with MSI_KV_OBSERVE (device error
+                           MSI_ERR_INVALID_ARG), and no block in two of their tables */
   const int32_t* cu;    /* [n + 1] row offsets of q */
   int n_rows;           /* rows of q and out */
-  int max_rows;         /* most rows of one sequence */
-  int n_heads;          /* query heads, a multiple of K: head h reads key-value head h / (n_heads / K) */
+  int max_rows;         /* most rows of one sequence; <= n_rows */
+  int n_heads;          /* query heads, a multiple of K, at most 128 K: head h reads key-value head h / (n_heads / K) */
   const void* q;        /* bf16 [n_rows, n_heads, D], 16-byte aligned */
   int64_t q_stride;     /* elements between rows, a multiple of 8 */
   void* out;            /* bf16 [n_rows, n_heads, D], 16-byte aligned */

@@ -502,8 +502,9 @@ class KvCache:
                   observe=False, stream=None):
         """Attention of rows cu[b] .. cu[b+1] of q [n, heads, head_dim], the last
         tokens of sequence seqs[b], over what it holds.  max_rows: at least the
-        rows of any one sequence.  scale None: head_dim ** -0.5.  observe: add up
-        each block's attention weight (decode form).  Returns (out, lse)."""
+        rows of any one sequence, at most those of q.  scale None: head_dim ** -0.5.
+        observe: add up each block's attention weight (decode form; no sequence
+        twice).  Returns (out, lse)."""
         if stream is not None:
             return self._elsewhere(stream, self.attention, q, cu, max_rows, seqs, out, lse, scale, softcap, window, observe)
         n, heads = cu.numel() - 1, q.shape[1]

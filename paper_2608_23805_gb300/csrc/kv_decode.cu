@@ -60,16 +60,21 @@ __device__ __forceinline__ int kv_units(const KvWork& w) { return w.steps > 0 ? 
 __device__ __forceinline__ int kv_groups(const KvAttnArgs& a, const KvWork& w, int R) { return (w.rows * a.G + R - 1) / R; }
 
 // The batch's work: s_pre[b] = units of the pairs before sequence b, over all
-// heads.  Returns whether every sequence is in range.  s_pre holds n + 1 words.
-__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, int R, long long* s_pre, long long* s_sum, int* s_bad) {
+// heads.  Returns whether every sequence is in range and, with s_seen (a bit for
+// each sequence of the cache), named once: two entries would add to the weights of
+// the same blocks.  s_pre holds n + 1 words.
+__device__ __forceinline__ bool kv_share(const KvAttnArgs& a, int R, long long* s_pre, long long* s_sum, int* s_bad,
+                                         unsigned* s_seen) {
   const int tid = threadIdx.x, T = blockDim.x, lane = tid & 31, wid = tid >> 5;
   const int per = (a.n + T - 1) / T, b0 = min(a.n, tid * per), b1 = min(a.n, b0 + per);
   if (tid == 0) *s_bad = 0;
+  if (s_seen != nullptr && tid < kKvMaxSeqs / 32) s_seen[tid] = 0;
   __syncthreads();
   long long mine = 0;
   for (int b = b0; b < b1; ++b) {
     const KvWork w = kv_work(a, b);
-    if (!w.ok) *s_bad = 1;
+    if (!w.ok || (s_seen != nullptr && (atomicOr(&s_seen[w.seq >> 5], 1u << (w.seq & 31)) >> (w.seq & 31) & 1) != 0))
+      *s_bad = 1;
     mine += (long long)kv_units(w) * a.c.K * (w.ok ? kv_groups(a, w, R) : 0);
   }
   long long v = mine;
@@ -139,6 +144,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long s_sum[kDecWarps];
   __shared__ int s_bad;
+  __shared__ unsigned s_seen[OBS ? kKvMaxSeqs / 32 : 1];
   __shared__ float s_m[kDecWarps][R], s_l[kDecWarps][R];
   long long* s_pre = reinterpret_cast<long long*>(smem + kDecWarps * RING);
   const KvCache& c = a.c;
@@ -146,7 +152,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
   grid_release();
 
   const int status = c.control[1];
-  const bool ok = kv_share(a, R, s_pre, s_sum, &s_bad);
+  const bool ok = kv_share(a, R, s_pre, s_sum, &s_bad, OBS ? s_seen : nullptr);
   const long long total = s_pre[a.n];
   if (tid == 0) a.split[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (OBS && blockIdx.x == 0)
