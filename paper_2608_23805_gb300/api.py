@@ -510,7 +510,8 @@ class KvCache:
         n, heads = cu.numel() - 1, q.shape[1]
         qp, q_stride, rows = self._rows(q, "q", heads)
         if out is None:
-            out = torch.empty_like(q)  # contiguous: q's rows are
+            # packed either way: empty_like, the shorter call, keeps the order of q's strides, which rows that overlap upset
+            out = torch.empty_like(q) if q_stride >= heads * self.D else q.new_empty(q.shape)
             op, out_stride = out.data_ptr() if rows else None, heads * self.D
         else:
             op, out_stride, out_rows = self._rows(out, "out", heads)
