@@ -677,7 +677,8 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.lse = g->lse;
   a.scale = g->scale;
   a.softcap = g->softcap;
-  a.window = g->window;
+  // as long as a sequence can be, or longer: none (and the kernels' sums with it stay within 32 bits)
+  a.window = g->window >= c.max_blocks << c.logP ? 0 : g->window;
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;
   const int tiles = kv_decode_tiles(a.max_rows * a.G, c.D);
   if (tiles == 0 && a.observe) return MSI_ERR_UNSUPPORTED;
