@@ -530,6 +530,8 @@ class KvCache:
         if need is None:  # a pure function of the cache's and the call's shape
             b = ctypes.c_size_t()
             N.check(N.lib().msi_kv_workspace_size(self.h, ctypes.byref(a), ctypes.byref(b), None), "msi_kv_workspace_size")
+            if len(self._need) >= 256:  # prompts come in any length
+                self._need.clear()
             need = self._need[key] = b.value
         on = self._here()
         ws = self._ws
