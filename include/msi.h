@@ -633,9 +633,14 @@ msi_status msi_kv_workspace_size(const msi_kv* kv, const msi_kv_attention_args* 
  * the tokens up to it (append first, then attend).  A row that sees no token
  * gives 0 and lse -inf.  Scores, sums and statistics are fp32; the attention
  * weights are rounded to fp16 before they multiply the values.  MSI_KV_OBSERVE
- * outside decode form returns MSI_ERR_UNSUPPORTED.  Device error beside those of
- * all calls: MSI_ERR_TIMEOUT, a wait within the chunk form's kernel ran out;
- * every row is NaN then. */
+ * outside decode form returns MSI_ERR_UNSUPPORTED.  A weight times its block's
+ * value scale has fewer bits where it is under 2^-14 of the row's largest such
+ * product: 2^-25 of the largest is its error then.  Device errors beside those of
+ * all calls: MSI_ERR_TIMEOUT, a wait within the chunk form's kernel ran out, and
+ * MSI_ERR_UNSUPPORTED, value scales more than 2^90 apart (values of 4e6 beside a
+ * block of zeros, of 1e27 beside values of 1) were met where they would have
+ * shared a sum; rows are NaN then, in chunk form all of the call, in decode form
+ * those concerned and any others. */
 msi_status msi_kv_attention(msi_kv* kv, const msi_kv_attention_args* args, void* workspace,
                             size_t workspace_bytes, msi_stream stream);
 

@@ -81,7 +81,7 @@ struct KvAttnArgs {
   // chunk form: the items (sequence, key-value head, row tile) and the prefix of their token tiles
   int4* items;            // [2 max_items] {sequence, first row, rows, held}, {head, row tile, first token tile, 0}
   long long* item_pre;    // [max_items + 1]; decode form: [n + 1] steps before each sequence's (observe)
-  int* plan;              // [4 + ctas] items, whether every sequence is in range, CTAs, whether a wait ran out; then each CTA's first item
+  int* plan;              // [4 + ctas] items, whether every sequence is in range, CTAs, whether the call failed; then each CTA's first item
   int max_items;
 };
 
@@ -210,10 +210,34 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 
+// of the normal numbers
 __device__ __forceinline__ float lg2(float x) {
   float r;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+
+// and of the denormal ones too: sums beside the largest value scales
+__device__ __forceinline__ float lg2_any(float x) {
+  float r;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// How far value scales may lie apart.  A weight for the sum is taken from the MMA's
+// operand, 2^(s + log2 sv - M) / sv, and ex2 gives 0 below 2^-126.  The token that
+// set M has the operand 1, so a row's sum is at least 1 / sv of that token: of a
+// token whose sv is 2^90 times smaller less than 2^-36 of the sum can be lost.  The
+// kernels look at the scales of the blocks that share a reference, and beyond that
+// the call fails closed.  (The sum apart from the operand, a second exponential a
+// score in its own loop, cost 2 to 10 % of every call.)
+constexpr float kScaleRange = 1.2379400392853803e27f;  // 2^90
+
+// l 2^d where 2^d by itself may be out of fp32's range: parts with references of
+// their own may have any scales.
+__device__ __forceinline__ float kv_scaled(float l, float d) {
+  const float h = ex2(0.5f * d);
+  return l * h * h;
 }
 
 // softcap * tanh(x / softcap) = softcap (1 - 2 / (e^(2 x / softcap) + 1)); the

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvAttnArgs a, int rows_tile,
     a.plan[0] = items;
     a.plan[1] = ok;
     a.plan[2] = ctas;
-    a.plan[3] = 0;  // a wait ran out
+    a.plan[3] = 0;  // a wait ran out, or value scales lie too far apart
   }
 }
 
@@ -399,6 +399,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   __shared__ float s_pair[C::NQ == 1 ? 3 : 1][2][128];  // of two warps that share rows: query maximum, reference, sum
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
+  __shared__ unsigned s_lo, s_hi;  // bits of the least and the greatest value scale of the CTA's tiles
   uint8_t* sQ = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sK = sQ + C::NQ * C::QBYTES;
   uint8_t* sV = sK + C::ST * C::KBYTES;
@@ -444,6 +445,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     mbar_init(never, 1);
     mbar_fence_init();
     s_abort = 0;
+    s_lo = 0x7f800000u;
+    s_hi = 0;
   }
   if (warp == C::MMA) {
     tmem_alloc_pair(&s_tmem, 512);
@@ -849,7 +852,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       const bool v = idx >= C::KTASKS;
       const int id0 = __shfl_sync(0xffffffffu, k.id, 0), id1 = C::VT == 32 && v ? __shfl_sync(0xffffffffu, k.id, 16) : id0;
       const bool fine = (unsigned)k.id < (unsigned)c.n_blocks;
-      ks = vs = k.id == -2 ? 1.0f : kv_nan();
+      ks = k.id == -2 ? 0.0f : kv_nan();  // past the tokens held: no row sees it
+      vs = k.id == -2 ? 1.0f : kv_nan();
       if (!fine && k.id != -2) kv_raise(c, MSI_ERR_INVALID_ARG);
       const uint32_t z = FMT == MSI_KV_Q8 ? 0x80808080u : 0u;
       const uint8_t* codes = c.codes[v] + k.off;
@@ -872,6 +876,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     Task k0 = look_up(), k1 = look_up(), k2 = look_up();
     uint4 x0[C::LOADS], x1[C::LOADS];
     float ks0, vs0, ks1, vs1;
+    float lo = INFINITY, hi = 0.0f;  // value scales met
     load(k0, x0, ks0, vs0);
     load(k1, x1, ks1, vs1);
     auto turn = [&](const Task& k, uint4 (&x)[C::LOADS], float ks, float vs) {
@@ -890,6 +895,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         st_shared_v4(to, make_uint4(kv_f16x2<FMT, false>(x[i].x), kv_f16x2<FMT, true>(x[i].x), kv_f16x2<FMT, false>(x[i].y), kv_f16x2<FMT, true>(x[i].y)));
         st_shared_v4(to ^ 16, make_uint4(kv_f16x2<FMT, false>(x[i].z), kv_f16x2<FMT, true>(x[i].z), kv_f16x2<FMT, false>(x[i].w), kv_f16x2<FMT, true>(x[i].w)));
       }
+      if (!v && i % C::SUB == 0 && ks != 0.0f) lo = fminf(lo, vs), hi = fmaxf(hi, vs);  // of the numbers
       // the granules' scales: read by softmax after the scores, which follow kfull
       if (!v && i % C::SUB == 0 && (lane & 15) == 0) {
         const int g = i / C::SUB + (rank ^ (lane >> 4)) * (C::KROWS / 16);
@@ -912,6 +918,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       load(k1, x1, ks1, vs1);
       k2 = look_up();
     }
+    __syncwarp();
+    // positive numbers are ordered as their bits are
+    atomicMin(&s_lo, __float_as_uint(lo));
+    atomicMax(&s_hi, __float_as_uint(hi));
   }
   }
 
@@ -921,8 +931,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
   cluster_sync_all();  // neither CTA leaves while the other may still reach it
   tc_fence_after();
   if (warp == C::MMA) tmem_dealloc_pair(tmem, 512);
-  if (tid == 0 && s_abort != 0) {
-    kv_raise(c, MSI_ERR_TIMEOUT);
+  const bool apart = __uint_as_float(s_hi) > __uint_as_float(s_lo) * kScaleRange;
+  if (tid == 0 && (s_abort != 0 || apart)) {
+    kv_raise(c, s_abort != 0 ? MSI_ERR_TIMEOUT : MSI_ERR_UNSUPPORTED);
     a.plan[3] = 1;
   }
 }
@@ -937,9 +948,9 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   grid_wait();
   grid_release();
   const KvCache& c = a.c;
-  const int4 plan = *reinterpret_cast<const int4*>(a.plan);  // items, in range, CTAs, a wait ran out
+  const int4 plan = *reinterpret_cast<const int4*>(a.plan);  // items, in range, CTAs, failed
   if (plan.y == 0 || plan.x == 0) return;  // every row is NaN already, or there is none
-  if (plan.w != 0) {  // rows that nobody came to are among those that are not split
+  if (plan.w != 0) {  // rows that are not split among them
     chunk_fail<D>(a, ((long long)blockIdx.y * gridDim.x + blockIdx.x) * kChunkJoinThreads + threadIdx.x,
                   (long long)gridDim.x * gridDim.y * kChunkJoinThreads);
     return;
@@ -987,7 +998,7 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const float f = mi[b] == -INFINITY ? (li[b] == 0.0f ? 0.0f : li[b]) : ex2(mi[b] - top);
-      sum += mi[b] == -INFINITY ? li[b] : li[b] * f;
+      sum += mi[b] == -INFINITY ? li[b] : kv_scaled(li[b], mi[b] - top);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
         acc[k].x = fmaf(f, v[b][k].x, acc[k].x);

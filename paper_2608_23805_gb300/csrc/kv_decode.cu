@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
     }
     const float two_cap = cap ? 2.0f * kLog2e / a.softcap : 0.0f;
 
+    float lo = INFINITY, hi = 0.0f;  // value scales of the steps that this lane has looked up
     // this warp's steps: first + wid, + kDecWarps, ..
     const int mine = last - first > wid ? (last - first - wid + kDecWarps - 1) / kDecWarps : 0;
     auto info = [&](int i) {  // of the warp's step i
@@ -285,6 +286,8 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
           s.ks = c.scale[0][(size_t)s.blk * c.K + h];
           const float vs = c.scale[1][(size_t)s.blk * c.K + h];
           s.lv = log2f(vs);
+          lo = fminf(lo, vs);  // of the numbers
+          hi = fmaxf(hi, vs);
           // a NaN comes in through the exponents of the tokens that a row sees;
           // rows that see none have weights 0 and must not meet it here
           s.iv = vs > 0.0f ? 1.0f / vs : 1.0f;
@@ -427,7 +430,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
           }
           if (g == 0)
             *reinterpret_cast<float2*>(a.step_lse + (item0 + idx) * R + 8 * nt + 2 * t) =
-                make_float2(mu[nt][0] + lg2(v0), mu[nt][1] + lg2(v1));
+                make_float2(mu[nt][0] + lg2_any(v0), mu[nt][1] + lg2_any(v1));
         }
         pf[nt][0] = transpose8x8(pack_f16x2(p[0], p[1]));
         pf[nt][1] = transpose8x8(pack_f16x2(p[2], p[3]));
@@ -470,6 +473,14 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
       __syncwarp();  // the stage is read: the next turn's fetch writes it
     }
     cp_async_wait<0>();
+    // positive numbers are ordered as their bits are
+    lo = __uint_as_float(__reduce_min_sync(0xffffffffu, __float_as_uint(lo)));
+    hi = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(hi)));
+    if (hi > lo * kScaleRange) {
+      if (lane == 0) kv_raise(c, MSI_ERR_UNSUPPORTED);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) l[nt][0] = l[nt][1] = kv_nan();
+    }
 
     // the warps' parts: reference and sum per row, then the outputs
 #pragma unroll
@@ -511,7 +522,7 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
       float sum = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
       for (int i = 0; i < kDecWarps; ++i) {
-        sum += s_m[i][r] == -INFINITY ? s_l[i][r] : s_l[i][r] * ex2(s_m[i][r] - top);
+        sum += s_m[i][r] == -INFINITY ? s_l[i][r] : kv_scaled(s_l[i][r], s_m[i][r] - top);
         const float2 v = reinterpret_cast<const float2*>(smem)[((size_t)i * R + r) * RS + p];
         x += v.x;
         y += v.y;
@@ -570,7 +581,7 @@ __device__ __forceinline__ void kv_join_few(const KvAttnArgs& a, int R, int x, i
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   const float f = pm == -INFINITY ? (pl == 0.0f ? 0.0f : pl) : ex2(pm - top);
-  float sum = pm == -INFINITY ? pl : pl * f;
+  float sum = pm == -INFINITY ? pl : kv_scaled(pl, pm - top);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
 #pragma unroll
@@ -645,7 +656,7 @@ __device__ __forceinline__ void kv_join_many(const KvAttnArgs& a, int R, int n, 
     const int i = k * kJoinThreads + tid;
     const float f = mi[k] == -INFINITY ? (li[k] == 0.0f ? 0.0f : li[k]) : ex2(mi[k] - top);
     if (i < parts) s_f[i] = f;
-    sum += mi[k] == -INFINITY ? li[k] : li[k] * f;
+    sum += mi[k] == -INFINITY ? li[k] : kv_scaled(li[k], mi[k] - top);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -755,13 +766,13 @@ __global__ void __launch_bounds__(kJoinThreads) kv_finish_kernel(KvAttnArgs a, i
         for (int x = c0 + lane; x <= c1; x += 32) {
           const float* ml = a.part_ml + (size_t)(2 * x + (x == c0 ? 1 : 0)) * 2 * R + r;
           const float m = ml[0], l = ml[R];
-          if (m > top) sum = top == -INFINITY ? sum : sum * ex2(top - m), top = m;
-          sum += m == -INFINITY ? l : l * ex2(m - top);
+          if (m > top) sum = top == -INFINITY ? sum : kv_scaled(sum, top - m), top = m;
+          sum += m == -INFINITY ? l : kv_scaled(l, m - top);
         }
         float all = top;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-        if (top != -INFINITY) sum *= ex2(top - all);
+        if (top != -INFINITY) sum = kv_scaled(sum, top - all);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         l2 = sum == 0.0f ? -INFINITY : all + log2f(sum);
