@@ -478,6 +478,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
     constexpr int kTopAt = C::NQ == 1 ? 1 : 0, kSumAt = C::NQ == 1 ? 2 : 0;
     // a vote (D = 256): whether any lane says so, or kPairLeave
     auto vote = [&](bool v) { return pair_vote(pair, __any_sync(0xffffffffu, v) && lane == 0); };
+    // a wait that runs out comes to the next vote with all lanes
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      const bool there = mbar_wait_warp(bar, parity & 1, abort_flag, a.wait_limit);
+      if (C::NQ == 1 && !there) pair_vote(pair, true);
+      return there;
+    };
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float two_cap = CAP ? 2.0f * kLog2e / a.softcap : 0.0f;
     uint32_t kv = 0, ns = 0, parts = 0;  // token tiles before the part's; S tiles and parts of this row tile
@@ -491,7 +497,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
 #pragma unroll 1
     while (true) {
       bool have = false;
-      while (go && walk.next(a, part)) {
+      while (walk.next(a, part)) {
         if (q > 0 && part.rows * a.G - part.row_tile * C::ROWS <= C::TROWS) {  // no second row tile
           kv += part.last - part.first;
           continue;
@@ -522,7 +528,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         }
         if (C::NQ == 1) {
           s_pair[0][half][tr] = __uint_as_float(amax);
-          if (vote(false) >= kPairLeave) goto left;
+          if (vote(false) >= kPairLeave) break;
           amax = max(amax, __float_as_uint(s_pair[0][half ^ 1][tr]));
         }
         const uint32_t e = kv_row_exp(amax);
@@ -538,12 +544,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
         __syncwarp();
       }
       if (pending) {
-        go = mbar_wait_warp(&olast[q], (parts - 1) & 1, abort_flag, a.wait_limit);
-        if (!go) break;
+        if (!wait(&olast[q], parts - 1)) break;
         tc_fence_after();
         if (C::NQ == 1) {
           s_pair[kSumAt][half][tr] = l;
-          if (vote(false) >= kPairLeave) goto left;
+          if (vote(false) >= kPairLeave) break;
           l = s_pair[kSumAt][0][tr] + s_pair[kSumAt][1][tr];
         }
         const float f = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
@@ -597,10 +602,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       slot = 2 * run + (part.first > 0 ? 0 : 1);
       m = -INFINITY;
       l = 0.0f;
-      if (a.stall == kKvStallSoftmax && blockIdx.x == 0 && warp == 0) {
-        go = mbar_wait_warp(never, 0, abort_flag, a.wait_limit);
-        if (!go) break;
-      }
+      if (a.stall == kKvStallSoftmax && blockIdx.x == 0 && warp == 0 && !wait(never, 0)) break;
       const int see = part.held - part.rows + qi;
       // tiles that every row of this row tile sees whole
       const int r_end = min(rows, part.row_tile * C::ROWS + lr + 128) - 1;
@@ -610,7 +612,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       for (int j = 0; j < n; ++j) {
         const uint32_t mine = ns++;
         const int buf = 2 * q + (mine & 1);
-        go = mbar_wait_warp(&sfull[buf], (mine >> 1) & 1, abort_flag, a.wait_limit);
+        go = wait(&sfull[buf], mine >> 1);
         if (!go) break;
         tc_fence_after();
         const Granule* info = s_info[(kv + j) & (2 * C::ST - 1)] + half * (C::COLS / 16);
@@ -626,13 +628,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             float top = fmaxf(m, chunk_max<D, CAP, true>(ts + half * C::COLS, info, crow, a.softcap, two_cap, lim, low));
             if (C::NQ == 1) {
               s_pair[kTopAt][half][tr] = top;
-              if (vote(false) >= kPairLeave) goto left;
+              go = vote(false) < kPairLeave;
+              if (!go) break;
               top = fmaxf(top, s_pair[kTopAt][half ^ 1][tr]);
             }
             if (j > 0) {
               // the output so far, once the last product is in it
               const uint32_t last = mine - 1;
-              go = mbar_wait_warp(&ofull[2 * q + (last & 1)], (last >> 1) & 1, abort_flag, a.wait_limit);
+              go = wait(&ofull[2 * q + (last & 1)], last >> 1);
               if (!go) break;
               tc_fence_after();
               const float f = top == -INFINITY ? 1.0f : ex2(m - top);
@@ -657,8 +660,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
           over = over && pass == 0;
           // both warps of a pair are through with S here: P goes over it
           const uint32_t again = C::NQ == 1 ? vote(over) : __any_sync(0xffffffffu, over);
-          if (C::NQ == 1 && again >= kPairLeave) goto left;
-          if (again == 0) break;
+          go = C::NQ == 2 || again < kPairLeave;
+          if (!go || again == 0) break;
         }
         if (!go) break;
         l += sum;
@@ -672,8 +675,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       kv += n;
       if (!go) break;
     }
-    if (C::NQ == 1 && !go) pair_vote(pair, true);  // a wait ran out: the partner learns of it at its next vote
-  left:;
   } else {
   set_regs<kConvRegs, false>();  // one instruction for the whole warpgroup
   if (warp >= C::MMA) {
