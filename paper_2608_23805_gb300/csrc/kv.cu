@@ -676,7 +676,7 @@ msi_status attention_args(const msi_kv* kv, const msi_kv_attention_args* g, char
   a.out_stride = g->out_stride;
   a.lse = g->lse;
   a.scale = g->scale;
-  a.softcap = g->softcap;
+  a.softcap = g->softcap > 0.0f && g->softcap < 1e-30f ? 1e-30f : g->softcap;  // scores of 0 all the same; 1 / cap stays finite
   // as long as a sequence can be, or longer: none (and the kernels' sums with it stay within 32 bits)
   a.window = g->window >= c.max_blocks << c.logP ? 0 : g->window;
   a.observe = (g->flags & MSI_KV_OBSERVE) != 0;

@@ -242,9 +242,18 @@ __device__ __forceinline__ float kv_scaled(float l, float d) {
 
 // softcap * tanh(x / softcap) = softcap (1 - 2 / (e^(2 x / softcap) + 1)); the
 // quotient's limits are those of the formula.  two_log2e_cap = 2 log2(e) / cap.
+// The difference leaves an error of 2^-23 of the cap, whatever the score: up to
+// caps of 64 that is no more than the scores' own roundings.  WIDE: any cap, with
+// tanh's series (up to z^9) where the score is under a quarter of it.
+constexpr float kSmallCap = 64.0f;
+template <bool WIDE>
 __device__ __forceinline__ float kv_softcap(float x, float cap, float two_log2e_cap) {
   const float y = x * two_log2e_cap;
-  return cap * (1.0f - __fdividef(2.0f, ex2(y > 80.0f ? 80.0f : y) + 1.0f));  // a NaN stays one
+  const float far = cap * (1.0f - __fdividef(2.0f, ex2(y > 80.0f ? 80.0f : y) + 1.0f));  // a NaN stays one
+  if (!WIDE) return far;
+  const float z = y * (0.5f * kLn2), z2 = z * z;
+  const float near = fmaf(z2, fmaf(z2, fmaf(z2, fmaf(z2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+  return fabsf(z) < 0.25f ? x * near : far;
 }
 
 #endif  // __CUDACC__

@@ -248,11 +248,11 @@ struct PartWalk {
   }
 };
 
-// log2 weights of 16 scores: c s + ad, or its capped form, masked beyond `lim`
-// and at or before `low` (columns of the granule)
-template <bool CAP, bool MASK>
+// log2 weights of 16 scores: c s + ad, or its capped form (CAP 1: caps up to
+// kSmallCap, 2: any), masked beyond `lim` and at or before `low` (columns of the granule)
+template <int CAP, bool MASK>
 __device__ __forceinline__ float chunk_exp(float s, float c, float ad, float cap, float two_cap, int col, int lim, int low) {
-  float e = CAP ? fmaf(kv_softcap(s * c, cap, two_cap), kLog2e, ad) : fmaf(s, c, ad);
+  float e = CAP != 0 ? fmaf(kv_softcap<CAP == 2>(s * c, cap, two_cap), kLog2e, ad) : fmaf(s, c, ad);
   if (MASK) e = col > lim || col <= low ? -INFINITY : e;
   return e;
 }
@@ -263,7 +263,7 @@ struct Granule {
   float ks, lv, iv, pad;
 };
 
-template <int D, bool CAP, bool MASK>
+template <int D, int CAP, bool MASK>
 __device__ __forceinline__ float chunk_max(uint32_t ts, const Granule* info, float crow, float cap, float two_cap, int lim, int low) {
   float m = -INFINITY;
 #pragma unroll 1
@@ -306,7 +306,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // P of a tile in registers (two a word) and the row's sum; over: some sum of 16
 // is above kChunkTop.  The next 16 scores are on their way while 16 are worked
 // on; products and sums go two at a time.
-template <int D, bool CAP, bool MASK>
+template <int D, int CAP, bool MASK>
 __device__ __forceinline__ float chunk_weights(uint32_t ts, const Granule* info, float crow, float m, float cap, float two_cap,
                                                int lim, int low, uint32_t (&p)[Chunk<D>::COLS / 2], bool& over) {
   constexpr int N = Chunk<D>::COLS / 16;
@@ -390,7 +390,7 @@ __device__ __forceinline__ void chunk_fail(const KvAttnArgs& a, long long i0, lo
     for (long long i = i0; i < (long long)a.n_rows * a.H; i += step) a.lse[i] = kv_nan();
 }
 
-template <int D, int FMT, bool CAP>
+template <int D, int FMT, int CAP>
 __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a) {
   using C = Chunk<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -655,8 +655,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
             m = top;
           }
           bool over;
-          sum = mask ? chunk_weights<D, CAP, true>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over)
-                     : chunk_weights<D, CAP, false>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over);
+          // caps above kSmallCap are rare: one form of the loop (their kernel of both crashed ptxas on an Arm host)
+          sum = CAP == 2 || mask
+                    ? chunk_weights<D, CAP, true>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over)
+                    : chunk_weights<D, CAP, false>(ts + half * C::COLS, info, crow, m, a.softcap, two_cap, lim, low, p, over);
           over = over && pass == 0;
           // both warps of a pair are through with S here: P goes over it
           const uint32_t again = C::NQ == 1 ? vote(over) : __any_sync(0xffffffffu, over);
@@ -1017,7 +1019,7 @@ __global__ void __launch_bounds__(kChunkJoinThreads) kv_chunk_join_kernel(KvAttn
   if (dw == 0 && a.lse != nullptr) a.lse[row * a.H + qh] = failed ? kv_nan() : sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-template <int D, int FMT, bool CAP>
+template <int D, int FMT, int CAP>
 cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   using C = Chunk<D>;
   static std::atomic<unsigned long long> done{0};
@@ -1047,11 +1049,16 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   return e;
 }
 
+template <int D, int FMT>
+cudaError_t chunk_fmt(const KvAttnArgs& a, int* launches, cudaStream_t s) {
+  return a.softcap == 0.0f         ? chunk_as<D, FMT, 0>(a, launches, s)
+         : a.softcap <= kSmallCap ? chunk_as<D, FMT, 1>(a, launches, s)
+                                  : chunk_as<D, FMT, 2>(a, launches, s);
+}
+
 template <int D>
 cudaError_t chunk_d(const KvAttnArgs& a, int* launches, cudaStream_t s) {
-  if (a.c.fmt == MSI_KV_Q8)
-    return a.softcap > 0.0f ? chunk_as<D, MSI_KV_Q8, true>(a, launches, s) : chunk_as<D, MSI_KV_Q8, false>(a, launches, s);
-  return a.softcap > 0.0f ? chunk_as<D, MSI_KV_E4M3, true>(a, launches, s) : chunk_as<D, MSI_KV_E4M3, false>(a, launches, s);
+  return a.c.fmt == MSI_KV_Q8 ? chunk_fmt<D, MSI_KV_Q8>(a, launches, s) : chunk_fmt<D, MSI_KV_E4M3>(a, launches, s);
 }
 
 }  // namespace

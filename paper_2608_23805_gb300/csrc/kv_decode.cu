@@ -365,12 +365,18 @@ __global__ void __launch_bounds__(32 * dec_warps(D, NT), 2) kv_decode_kernel(KvA
       // exponents: [0], [1] token g, [2], [3] token g + 8; rows 2t, 2t + 1
       const bool whole = tok0 + 16 <= w.held - w.rows + 1 &&
                          (a.window == 0 || tok0 > w.held - 1 - a.window);
-      if (cap) {
+      if (cap && a.softcap <= kSmallCap) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            sc[nt][q] = fmaf(kv_softcap(sc[nt][q] * (cs[nt][q & 1] * ks), a.softcap, two_cap), kLog2e, lv);
+            sc[nt][q] = fmaf(kv_softcap<false>(sc[nt][q] * (cs[nt][q & 1] * ks), a.softcap, two_cap), kLog2e, lv);
+      } else if (cap) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            sc[nt][q] = fmaf(kv_softcap<true>(sc[nt][q] * (cs[nt][q & 1] * ks), a.softcap, two_cap), kLog2e, lv);
       } else {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
