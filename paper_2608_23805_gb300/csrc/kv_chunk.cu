@@ -705,7 +705,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) kv_chunk_kernel(KvAttnArgs a
       // first keys come before its queries; the next keys are asked for before a
       // tile's values, as the issuers do.
       auto pass = [&](uint64_t* bar, uint32_t parity) {
-        go = go && wait(bar, parity);
+        go = go && mbar_wait_warp(bar, parity & 1, abort_flag, a.wait_limit);  // arrivals of this CTA
         if (go && lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(bar), 0));
         __syncwarp();
       };

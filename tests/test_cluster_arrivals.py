@@ -25,7 +25,7 @@ def test_chunk_kernel_orders_what_it_stores():
     crossing = re.findall(r"mbar_arrive_cluster\(", text)
     assert len(crossing) == 1
     at = text.index("mbar_arrive_cluster(")
-    assert "wait(bar, parity)" in text[at - 120:at]
+    assert "mbar_wait_warp(bar, parity & 1" in text[at - 200:at]
     # and the MMA warps acquire for the cluster
     assert re.search(r"auto wait = \[&\]\(uint64_t\* bar, uint32_t parity\) \{ return mbar_wait_warp<true>\(", text)
 
