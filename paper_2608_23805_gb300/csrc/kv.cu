@@ -1,6 +1,6 @@
 // Key-value cache in 8 bits: append (rows rounded into their blocks), eviction
 // by the attention weight received, release, read back, and the host side of
-// every msi_kv_* call.  The attention itself: kv_decode.cu.
+// every msi_kv_* call.  The attention itself: kv_decode.cu, kv_chunk.cu.
 //
 // The cache's state is on the device and changes there, so every CTA of an
 // append or an eviction works out the whole batch's bookkeeping for itself (a
@@ -89,9 +89,10 @@ __device__ __forceinline__ uint32_t round_e4m3(uint32_t a, uint32_t b, float inv
 // A block of one head, keys or values, is a task: rounded in one pass over its
 // rows, which stay in registers between the maximum and the rounding.  A CTA
 // takes every gridDim-th task, so that the bookkeeping is paid for once in
-// several blocks.  Bound: memory (16-bit rows in, codes out) for prompts (32,768
-// tokens of 2 heads of 128: 14 us, 3.6 TB/s), latency for single tokens (64
-// sequences: 6 us).
+// several blocks.  Bound: for prompts the chain of a task (look-up, rows, maximum,
+// codes, with barriers between them) beside memory (32,768 tokens of 2 heads of
+// 128: 16 us, 3.2 TB/s of rows in and codes out), latency for single tokens (64
+// sequences: 8 us).
 constexpr int kWrongBlock = 1 << 16;  // in the ticket: CTAs that met a wrong block number, above those that are done
 constexpr int append_threads(int vpt) { return vpt <= 4 ? 1024 : 512; }  // of an SM, by the registers a thread takes
 
@@ -306,10 +307,14 @@ __device__ __forceinline__ unsigned kv_key(float w) {
 // then the later block), which takes two barriers each, and the entries after
 // them move down.  More: the threshold weight by a radix selection (four passes
 // over 8 bits, whole-number histograms, so the result does not depend on any
-// order), then one pass over the table in order that keeps or frees.  64 sequences
-// of 257 blocks that give up one, with the append before: 13.0 us, 17.1 by the
-// radix selection; three of 4,004 that give up four: 14.5 and 21.6.  Bound:
-// latency (dependent passes over a few KB).
+// order), then one pass over the table in order that keeps or frees.  With the
+// append before, us one by one / by radix selection: 64 sequences of 256 blocks
+// that give up one 11.8 / 15.4, four 13.9 / 15.9, six 16.4 / 16.9, eight 18.5 / 17.4;
+// three of 4,000 that give up one 11.7 / 19.0, four 13.8 / 19.0, eight 17.5 / 19.1,
+// twelve 21.5 / 20.0; one of 100, four 13.3 / 15.4, eight 16.2 / 14.9.  (The two meet
+// at six to ten; beyond 4,096 candidates a thread would hold more than four: two
+// sequences of 8,000, eight candidates a thread, one 12.3 / 23.1.)  Bound: latency
+// (dependent passes over a few KB).
 __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(KvEvictArgs a) {
   extern __shared__ unsigned s_key[];
   __shared__ int s_scan[32], s_hist[8][256], s_pick[2];
@@ -501,9 +506,10 @@ constexpr int kReadThreads = 256, kReadRows = 64;
 
 // `per` (at most 64) rows a CTA: their blocks looked up by a thread each, then 16
 // codes a thread and step to two 16-byte stores.  16 rows where that leaves an
-// SM no more than four CTAs, so that short calls fill the GPU (65 rows of 64
-// sequences: 6 us against 10), 64 for the rest.  Bound: memory (codes in, twice
-// as many bytes out).
+// SM no more than four CTAs, so that short calls fill the GPU (us with 16 / 64 rows:
+// the last blocks of 64 sequences 4.1 / 7.2, 8,741 rows of 2 x 256 7.7 / 10.3), 64 for
+// the rest (32,768 rows of 2 x 128 11.4 / 11.6).  Bound: memory (codes in, twice as
+// many bytes out: 4.4 TB/s at 32,768 rows) and the CTAs' two dependent loads.
 __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(KvReadArgs a, int per) {
   const KvCache& c = a.c;
   __shared__ long long s_at[kReadRows];  // element of the row in a head-0 block, or -1

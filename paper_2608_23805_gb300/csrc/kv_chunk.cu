@@ -25,13 +25,15 @@
 // The work is the list of all token tiles of all items; each pair takes an
 // equal run, parts of split items are joined by kv_chunk_join_kernel in order.
 //
-// Measured: 4,096 rows on 32,768 tokens, 16 heads of 128 over 2: 692 us,
-// 1,490 TFLOP/s, 0.77 of a large library product; four chunks of 3,000 on
-// themselves, D = 256, capped: 331 us.  Single CTAs with one S a row tile had 790
+// Measured: 4,096 rows on 32,768 tokens, 16 heads of 128 over 2: 697 us,
+// 1,480 TFLOP/s, 0.76 of a large library product; four chunks of 3,000 on
+// themselves, D = 256, capped: 343 us.  Single CTAs with one S a row tile had 790
 // and 457 us (conversion and operand reads filled shared memory), pairs with one S
 // 770 and 364 (a row tile's softmax, its products and the signals between them
 // follow one another).  Bound: the softmax warps (without their arithmetic 566 and
-// 271 us).
+// 271 us) and, for short items at D = 256, the items' fixed cost: O and two S fill
+// TMEM, so that a product waits for the output before it.  Few rows: a tile's chain
+// through the pair (72 rows of 64 sequences of 8,192, D = 128: 182 us).
 //
 // Every wait is bounded: on expiry the CTA gives up, drains its MMAs, frees
 // TMEM and raises MSI_ERR_TIMEOUT; the join then makes every row of the call NaN.
@@ -73,9 +75,11 @@ struct Chunk {
 constexpr int kChunkThreads = 512;
 constexpr int kSoftRegs = 144, kConvRegs = 112;
 static_assert(2 * kSoftRegs + 2 * kConvRegs <= 512, "registers of the launch");
-// What an item costs beside its tiles (queries, first scores, output), in tiles.
-// D = 256, four chunks of 3,000: 399, 360, 331, 328, 353 us at 2, 3, 4, 5, 6; 8 of
-// 500, D = 64: 24.1, 24.5, 25.5 us at 3, 4, 5; a long item hides it.
+// What an item costs beside its tiles (queries, first scores, output), in tiles; us
+// at 2, 3, 4, 5, 6: four chunks of 3,000 at D = 64 132, 127, 121, 119, 119, D = 128
+// 185, 180, 168, 165, 157, D = 256 355, 326, 303, 307, 313; 8 of 500 at D = 64 26.0,
+// 25.9, 25.8, 27.5, 27.7, D = 128 37.1, 36.4, 36.2, 36.3, 35.4, D = 256 53.2, 49.9, 47.7,
+// 48.6, 49.8; long items within 1 %.
 constexpr int kItemCost = 4;
 
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) {
@@ -1025,7 +1029,7 @@ cudaError_t chunk_as(const KvAttnArgs& a, int* launches, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = smem_attr_once(kv_chunk_kernel<D, FMT, CAP>, C::SMEM, done);
   if (e != cudaSuccess) return e;
-  // few warps scan sooner: 8 sequences of 500 take 24.8 us in all, 25.6 with 1,024 threads
+  // few warps scan sooner: 8 sequences of 500 take 25.7 us in all, 26.6 with 1,024 threads
   const bool few = a.n <= 256 && a.max_items <= 512;
   e = launch_after(false, few ? kv_plan_kernel<256> : kv_plan_kernel<1024>, dim3(1), dim3(few ? 256 : 1024), 0, s, a, C::ROWS, C::NT);
   if (e != cudaSuccess) return e;

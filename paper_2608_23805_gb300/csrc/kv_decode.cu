@@ -20,17 +20,19 @@
 // are 16 consecutive bytes of a code row, and V^T needs only byte interleaving
 // of two tokens' words.  Codes go to a ring of shared memory per warp by
 // 16-byte asynchronous copies, chunks XOR-swizzled by row.  The legacy MMA is
-// enough: 2 R flops a byte (110 TFLOP/s at 8 rows and 6.8 TB/s).
+// enough at 8 and 16 rows: 2 R flops a byte (110 TFLOP/s at 8 rows and 6.8 TB/s);
+// with more, each group of a head converts the codes again.
 //
 // Split.  The work is the list of all 16-token steps of all (sequence, head)
 // pairs; each CTA takes an equal run of it, whatever the lengths.  A pair that
 // lies in one CTA is finished there; parts of split ones are joined by
 // kv_finish_kernel in the CTAs' order, so results do not depend on timing.
 //
-// Measured: 64 sequences of 8,192, 2 heads of 128 with 8 query heads each, block
-// weights added up: 44 us, 3.6 TB/s of codes and scales; one of 32,768: 15 us.
-// Bound: issue slots and latency (about 500 instructions a step, half of them
-// conversions and byte interleaving; without the copies 0.86 of the time).
+// Measured: 64 sequences of up to 8,192, 2 heads of 128 with 8 query heads each,
+// block weights added up: 45 us, 3.6 TB/s of codes and scales; one of 32,768: 15 us.
+// Bound: the latency of a step's dependent instructions (about 500, half of them
+// conversions and byte interleaving) at 16 warps an SM, 8 at D = 256: issue slots
+// are 41 and 29 % busy, DRAM 54 and 47 %; without the copies it takes 0.86 of the time.
 #include "kv.cuh"
 
 namespace msi {
@@ -44,8 +46,10 @@ constexpr float kLazy = 8.0f;  // P may reach 2^8
 // CTAs share an SM, so that one reads while the other begins or ends a pair.
 __host__ __device__ constexpr int dec_warps(int D, int NT) { return D * NT <= 128 ? 8 : 4; }
 // What a pair costs a CTA beside its steps (queries, first loads, the warps'
-// sums), in steps.  12 sequences of 20,000, D = 256, 4 tokens: 56.6, 55.2, 49.6,
-// 46.7, 47.6 us at 0, 8, 32, 48, 96; 64 of 8,192: 45.7, 45.6, 46.0, 44.4, 45.9.
+// sums), in steps; us at 16, 32, 48, 64, 96: 64 sequences of up to 8,192, D = 64
+// 22.6, 22.0, 21.6, 22.1, 22.9, D = 128 38.8, 38.8, 37.3, 37.3, 37.9, 64 of 4,096 at
+// D = 256 39.9, 38.7, 39.1, 40.0, 42.4; 12 of 20,000, 4 tokens, D = 128 39.4, 37.2,
+// 37.0, 37.5, 38.5, D = 256 71.2, 68.2, 68.2, 69.9, 71.6; one of 32,768 within 0.5.
 constexpr int kPairCost = 48;
 __host__ __device__ constexpr int dec_stage_bytes(int D) { return 16 * 2 * D; }
 // Stages of a warp's ring: 96 KB a CTA, at most 8.
@@ -823,12 +827,12 @@ cudaError_t decode_fmt(const KvAttnArgs& a, cudaStream_t s) {
 int kv_decode_pair_cost() { return kPairCost; }
 
 // More rows than a group holds are several pairs: each reads the codes again, but
-// mostly from L2 (64 sequences of 8,192, D = 128: 63 us for 16 rows, 101 for 32 in
-// two groups, against 157 in one group of 32, whose registers spill; D = 64: 60
+// mostly from L2 (64 sequences of 8,192, D = 128: 59 us for 16 rows, 97 for 32 in
+// two groups, against 157 in one group of 32, whose registers spill; D = 64: 56
 // for 32 in one).  Chunk form takes over about where it is as fast for many
 // sequences and the gap for one is small (decode form at its most rows, chunk form
-// just above; 64 sequences of 8,192 / one of 32,768): D = 64 95 and 142 / 19 and
-// 33 us, D = 128 181 and 167 / 23 and 33, D = 256 267 and 276 / 32 and 45.
+// with 8 more; 64 sequences of 8,192 / one of 32,768): D = 64 97 and 160 / 19 and
+// 31 us, D = 128 184 and 182 / 24 and 36, D = 256 272 and 288 / 33 and 46.
 int kv_decode_tiles(int rows, int D) {
   return rows > (D == 256 ? 48 : 64) ? 0 : rows <= 8 ? 1 : rows <= 16 || D > 64 ? 2 : 4;
 }
