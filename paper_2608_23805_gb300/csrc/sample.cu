@@ -75,12 +75,12 @@ __constant__ uint32_t kPow32[32] = {
     134217728u, 137156714u, 140160054u, 143229160u, 146365470u, 149570457u, 152845623u, 156192507u, 159612677u, 163107740u, 166679334u,
     170329136u, 174058859u, 177870251u, 181765103u, 185745240u, 189812531u, 193968884u, 198216250u, 202556621u, 206992033u, 211524568u,
     216156353u, 220889561u, 225726413u, 230669177u, 235720175u, 240881774u, 246156398u, 251546522u, 257054673u, 262683438u};
-constexpr uint32_t kMostMant = 66385968u;  // of a code's lower 26 bits: 2^(63 / 64) 2^25
 
 // 2^(a + e) as a code, |a| up to 4,096 and |e| up to 2^-11; whole: (44 - what a's
 // whole part counts from) << 26.  a's nearest 32nd is split off, the rest goes
 // through the series of 2^r - 1 (the next term is under 2^-39); off by 2^-27 before
-// the rounding to 26 bits, whose leading one stands for 2^25.
+// the rounding to 26 bits, whose leading one stands for 2^25: 2^25 2^(-1 / 64) to 2^25
+// 2^(63 / 64), past either end by what e adds.
 __device__ __forceinline__ uint32_t power_code(float a, float e, uint32_t whole, const uint2* tab) {
   const float n = fmaf(a, 32.0f, kRoundMagic);
   const float r = fmaf(__fadd_rn(n, -kRoundMagic), -1.0f / 32.0f, a) + e;  // exact but for e; about 1/64 at most
@@ -120,15 +120,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 __device__ __forceinline__ u64 code_weight(uint32_t code) {
   return ((u64)(code & 0x3ffffffu) << 19) >> (44 - (code >> 26));  // of code 0: 0
-}
-
-// The least code that weighs `weight` (1 or more).
-__device__ __forceinline__ uint32_t least_code(u64 weight) {
-  for (int e = 1; e < 45; ++e) {
-    const u64 mant = e <= 25 ? weight << (25 - e) : (weight + (1ull << (e - 25)) - 1) >> (e - 25);
-    if (mant <= kMostMant) return (uint32_t)e << 26 | (uint32_t)mant;
-  }
-  return 0xffffffffu;
 }
 
 // What the weight is proportional to, of codes with the same upper 6 bits.
@@ -905,8 +896,18 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const __grid_
       };
       if (r.step<true>(0, mass, target, &b)) r.settle<true>(b);
     }
-    if (light > 0) r.least = max(r.least, least_code(light));
-    if (!plain || light > 0) {
+    if (light > 0) {
+      // Weights are compared, not codes: next to a power of two a code of one exponent
+      // may stand for as much as the next one's codes, or more (power_code).
+      const auto heavy = [&](uint32_t v) { return v >= r.least && code_weight(v) >= light ? v : 0u; };
+      sum = 0;
+      for (int g = 0; g < groups; ++g) {
+        uint4 c = mine[g * 32];
+        c.x = heavy(c.x), c.y = heavy(c.y), c.z = heavy(c.z), c.w = heavy(c.w);
+        mine[g * 32] = c;
+        sum += code_weight(c.x) + code_weight(c.y) + code_weight(c.z) + code_weight(c.w);
+      }
+    } else if (!plain) {
       sum = 0;
       r.each([&](uint32_t v) { sum += kept(v); });
     }
