@@ -630,6 +630,7 @@ class KvCache:
     def __init__(self, *, n_seqs, max_blocks, n_blocks, n_kv_heads, head_dim, block_tokens=32, fmt=N.MSI_KV_Q8,
                  buffers=None, stream=None):
         lib = N.lib()
+        dev = _current_device()  # the handle's
         K, P, D = n_kv_heads, block_tokens, head_dim
         self.n_seqs, self.K, self.P, self.D, self.fmt = n_seqs, K, P, D, fmt
         shapes = {"k_codes": ((n_blocks, K, P, D), torch.uint8), "v_codes": ((n_blocks, K, P, D), torch.uint8),
@@ -643,8 +644,8 @@ class KvCache:
                     t = torch.empty(shape, dtype=dtype, device="cuda")
                 else:
                     t = buffers[name]
-                    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-                        raise ValueError("%s: a contiguous CUDA tensor %s of %s is needed" % (name, shape, dtype))
+                    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+                        raise ValueError("%s: a contiguous tensor %s of %s on the current CUDA device is needed" % (name, shape, dtype))
                 setattr(self, name, t)
         d = N.msi_kv_desc(n_seqs, max_blocks, n_blocks, K, D, P, fmt, *[getattr(self, n).data_ptr() for n in self.BUFFERS])
         h = ctypes.c_void_p()
@@ -663,14 +664,13 @@ class KvCache:
 
     # A decode step's calls are short: the checks read each attribute once.
 
-    @staticmethod
-    def _index(t, name, n=None):
+    def _index(self, t, name, n=None):
         if t is None:
             return None
         shape = t.shape
-        if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 1 or (n is not None and shape[0] != n)
+        if (t.dtype is not torch.int32 or t.get_device() != self._device_index or len(shape) != 1 or (n is not None and shape[0] != n)
                 or not t.is_contiguous()):
-            raise ValueError("%s: a contiguous int32 CUDA vector%s is needed" % (name, "" if n is None else " of %d" % n))
+            raise ValueError("%s: a contiguous int32 vector%s on the cache's device is needed" % (name, "" if n is None else " of %d" % n))
         return t.data_ptr()
 
     def _rows(self, t, name, heads):
@@ -787,8 +787,8 @@ class KvCache:
                 raise ValueError("out: the shape of q is needed")
         if lse is None:
             lse = torch.empty((rows, heads), dtype=torch.float32, device=self._device)
-        elif tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
-            raise ValueError("lse: a contiguous fp32 CUDA tensor [n, heads] is needed")
+        elif tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != self._device_index:
+            raise ValueError("lse: a contiguous fp32 tensor [n, heads] on the cache's device is needed")
         a = N.msi_kv_attention_args(n, self._index(seqs, "seqs", n), self._index(cu, "cu"), rows, max_rows, heads, qp,
                                     q_stride, op, out_stride, lse.data_ptr() if rows else None,
                                     self.D ** -0.5 if scale is None else scale, softcap, window,
