@@ -747,6 +747,19 @@ typedef struct {
  * (about 2 s) makes the outputs concerned NaN. */
 msi_status msi_q4_linear(const msi_q4_linear_args* args, msi_stream stream);
 
+/* Limit of those waits, in SM clock cycles (clock64), for all later calls of the
+ * process; cycles <= 0 restores the default of 4e9 (~2 s at GB300 clocks).  A kernel
+ * whose wait runs out still waits, with its own ~10 ms bound each, for its copies in
+ * flight, and returns: the context stays usable. */
+msi_status msi_q4_set_wait_cycles(int64_t cycles);
+
+/* For tests of that path (no GPU fault): in the process's next msi_q4_linear a barrier
+ * expects an arrival that does not come, for a warp's codes or for the rows that a
+ * CTA's warps share (where they share none, codes all the same).  0 takes the request
+ * back. */
+enum { MSI_Q4_STALL_CODES = 1, MSI_Q4_STALL_ROWS = 2 };
+msi_status msi_q4_inject_stall(int where);
+
 /* Rotation of rows by position.  Pair j of a head's columns, j < dims / 2, is
  * (j, j + dims / 2), or (2 j, 2 j + 1) where interleaved; it turns by freqs[j]
  * radians for each position along axis[j]; columns from dims on stay.  A handle

@@ -492,6 +492,16 @@ class Q4Linear:
             N.check(rc, "msi_q4_linear")
         return out
 
+    @staticmethod
+    def set_wait_cycles(cycles: int):
+        """Limit of the products' device waits (msi_q4_set_wait_cycles); 0: the default."""
+        N.check(N.lib().msi_q4_set_wait_cycles(int(cycles)), "msi_q4_set_wait_cycles")
+
+    @staticmethod
+    def inject_stall(where: int):
+        """The next product waits in vain (msi_q4_inject_stall)."""
+        N.check(N.lib().msi_q4_inject_stall(int(where)), "msi_q4_inject_stall")
+
 
 class Rotary:
     """Rotation of heads by position (see include/msi.h, msi_rotary_desc).  Pair j

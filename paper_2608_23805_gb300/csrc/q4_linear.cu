@@ -48,6 +48,8 @@ struct Q4Args {
   void* out;
   long long out_stride;
   int out_f32;
+  int stall;             // what CTA (0, 0) waits for in vain (msi_q4_inject_stall), 0: nothing
+  long long wait_limit;  // cycles
 };
 
 constexpr int kQ4Warps = 8;  // most warps of a CTA
@@ -141,6 +143,7 @@ __device__ __forceinline__ void q4_store(const Q4Args& a, int row, int to, float
 // 32,768 takes 62 us or more).  GN: groups of a step.
 //
 // A copy that does not arrive within the wait's limit makes the CTA's outputs NaN.
+// (An injected stall: the first CTA's first warp, at its second turn if it has one.)
 template <int NT, int GN, int STAGES>
 __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) q4_linear_kernel(const __grid_constant__ Q4Args a) {
   constexpr int kCols = NT * 8, kPitch = kQ4Rows + 1;
@@ -166,7 +169,8 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) q4_linear_
     x[n] = a.x + (size_t)min(row0 + n * 8 + g, a.rows - 1) * a.x_stride + 8 * t;
   uint64_t* full = reinterpret_cast<uint64_t*>(s_ring + warps * (STAGES * kTurn)) + warp * STAGES;
   if (lane == 0) {
-    for (int d = 0; d < STAGES; ++d) mbar_init(full + d, 1);
+    const int stall = a.stall != 0 && tile + row0 + warp == 0 ? min(turns, STAGES) - 1 : -1;
+    for (int d = 0; d < STAGES; ++d) mbar_init(full + d, d == stall ? 2 : 1);
     mbar_fence_init();
   }
   __syncwarp();
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) q4_linear_
   load_x(b0, 2 * t0);
   int slot = 0, phase = 0, late = 0;
   for (int i = 0; i < turns; ++i) {
-    if (!mbar_wait_warp(full + slot, phase, &late, kQ4WaitCycles)) break;
+    if (!mbar_wait_warp(full + slot, phase, &late, a.wait_limit)) break;
     fetch(slot == 0 ? STAGES - 1 : slot - 1);  // what was read before the wait, by all lanes
     const uint8_t* at = ring + slot * kTurn;
     const int step = 2 * (t0 + i), live = (a.n_in - step * kQ4Step) >> 5;  // the same for the warp
@@ -250,6 +254,11 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) q4_linear_
 // part's first warp; a tile a warp.  (Through L1, as above, 16 rows are 16 cache
 // lines a load: its tags, not memory, bound them: 16 x 8,192 to 32,768 54 us.  Two
 // tiles a warp, which have a row of x in registers for both but half the warps: 47.)
+//
+// A warp whose wait runs out frees no more slots, so that the part's first warp and then
+// all others of the part run out as well, each once, unless they have all they need: the
+// tiles of those that did are NaN.  (An injected stall: the first CTA's first part, its
+// last warp at the first turn's codes, or all its warps at the second turn's rows.)
 constexpr int kQ4XPitch = 576;  // bytes of a row of x in a slot: 512, and 64 so that eight rows' parts lie in other banks
 constexpr int kQ4Parts = 2, kQ4Slots = 2;
 // Most tiles of a CTA, and CTAs of an SM: with 32 rows the rings leave room for one.
@@ -266,6 +275,7 @@ __global__ void __launch_bounds__(kQ4Parts * q4_same(NT) * 32, q4_ctas(NT)) q4_w
   const int g = lane >> 2, t = lane & 3;
   const int tile = blockIdx.x * same + own, row0 = blockIdx.y * kCols;
   const int rows = min(kCols, a.rows - row0);
+  const int t0 = a.turns * part / KS, turns = a.turns * (part + 1) / KS - t0;
   uint8_t* ring = s_ring + warp * (SLOTS * kTurn);
   uint8_t* s_x = s_ring + warps * SLOTS * kTurn + part * SLOTS * kX;
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_ring + warps * SLOTS * kTurn + KS * SLOTS * kX);
@@ -277,15 +287,15 @@ __global__ void __launch_bounds__(kQ4Parts * q4_same(NT) * 32, q4_ctas(NT)) q4_w
 #pragma unroll
       for (int i = 0; i < 4; ++i) total[n][i] = 0.0f;
   if (lane < SLOTS) {
-    mbar_init(full + lane, 1);
+    const int stall = blockIdx.x + blockIdx.y + part == 0 ? a.stall : 0;
+    mbar_init(full + lane, stall == MSI_Q4_STALL_CODES && own + 1 == same && lane == 0 ? 2 : 1);
     if (own == 0) {
-      mbar_init(x_full + lane, 1);
+      mbar_init(x_full + lane, stall == MSI_Q4_STALL_ROWS && lane == min(turns, SLOTS) - 1 ? 2 : 1);
       mbar_init(x_free + lane, same);
     }
     mbar_fence_init();
   }
   __syncthreads();
-  const int t0 = a.turns * part / KS, turns = a.turns * (part + 1) / KS - t0;
   const size_t pitch = (size_t)a.tiles * kTurn;  // of a turn
   const uint8_t* w = a.packed + t0 * pitch + (size_t)min(tile, a.tiles - 1) * kTurn;  // past the last tile: the last one again, not stored
   const __nv_bfloat16* x = a.x + (size_t)(row0 + min(lane, rows - 1)) * a.x_stride;
@@ -308,7 +318,7 @@ __global__ void __launch_bounds__(kQ4Parts * q4_same(NT) * 32, q4_ctas(NT)) q4_w
     if (d < turns) fetch(d, d);
   int slot = 0, phase = 0, late = 0;
   for (int i = 0; i < turns; ++i) {
-    if (!mbar_wait_warp(x_full + slot, phase, &late, kQ4WaitCycles) || !mbar_wait_warp(full + slot, phase, &late, kQ4WaitCycles)) break;
+    if (!mbar_wait_warp(x_full + slot, phase, &late, a.wait_limit) || !mbar_wait_warp(full + slot, phase, &late, a.wait_limit)) break;
     const uint8_t* at = ring + slot * kTurn;
     const uint8_t* xs = s_x + slot * kX + g * kQ4XPitch + t * 16;
     const int live = (a.n_in - (t0 + i) * 2 * kQ4Step) >> 5;
@@ -321,7 +331,7 @@ __global__ void __launch_bounds__(kQ4Parts * q4_same(NT) * 32, q4_ctas(NT)) q4_w
     __syncwarp();  // the slots are read by all lanes
     if (lane == 0) mbar_arrive(x_free + slot);
     if (i + SLOTS < turns) {
-      if (own == 0 && !mbar_wait_warp(x_free + slot, phase, &late, kQ4WaitCycles)) break;
+      if (own == 0 && !mbar_wait_warp(x_free + slot, phase, &late, a.wait_limit)) break;
       fetch(i + SLOTS, slot);
     }
     if (++slot == SLOTS) slot = 0, phase ^= 1;
@@ -450,6 +460,9 @@ msi_status q4_shape(int n_out, int n_in, int group) {
   return MSI_OK;
 }
 
+std::atomic<long long> q4_wait_limit{kQ4WaitCycles};
+std::atomic<int> q4_stall{0};
+
 bool aligned(const void* p, unsigned bytes) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace
@@ -504,6 +517,8 @@ msi_status msi_q4_linear(const msi_q4_linear_args* g, msi_stream stream) {
   a.out = g->out;
   a.out_stride = g->out_stride;
   a.out_f32 = g->out_type == MSI_F32;
+  a.wait_limit = q4_wait_limit.load(std::memory_order_relaxed);
+  if (q4_stall.load(std::memory_order_relaxed) != 0) a.stall = q4_stall.exchange(0);
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -513,6 +528,17 @@ msi_status msi_q4_linear(const msi_q4_linear_args* g, msi_stream stream) {
     else e = q4_as<4, 2>(a, g->group, sms, stream);
   }
   return e == cudaSuccess ? MSI_OK : note_cuda_error(e, "msi_q4_linear");
+}
+
+msi_status msi_q4_set_wait_cycles(int64_t cycles) {
+  q4_wait_limit = cycles > 0 ? (long long)cycles : kQ4WaitCycles;
+  return MSI_OK;
+}
+
+msi_status msi_q4_inject_stall(int where) {
+  if (where < 0 || where > MSI_Q4_STALL_ROWS) return MSI_ERR_INVALID_ARG;
+  q4_stall = where;
+  return MSI_OK;
 }
 
 }  // extern "C"

@@ -36,6 +36,7 @@ MSI_KV_Q8, MSI_KV_E4M3 = 0, 1
 MSI_KV_OBSERVE = 1
 MSI_KV_STALL_SOFTMAX, MSI_KV_STALL_MMA, MSI_KV_STALL_CONVERSION = 1, 2, 3
 MSI_BF16, MSI_F32 = 0, 1
+MSI_Q4_STALL_CODES, MSI_Q4_STALL_ROWS = 1, 2
 MSI_FWD_RESIDUAL = 1
 MSI_FWD_SINGLE_CTA = 2
 MSI_FWD_SHARED_UNGATED = 4
@@ -227,6 +228,8 @@ _SIGS = {
     "msi_q4_packed_bytes": (ctypes.c_uint64, [ctypes.c_int, ctypes.c_int, ctypes.c_int]),
     "msi_q4_pack": (ctypes.c_int, [_P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int, _P, ctypes.c_uint64, _P]),
     "msi_q4_linear": (ctypes.c_int, [_P, _P]),
+    "msi_q4_set_wait_cycles": (ctypes.c_int, [ctypes.c_int64]),
+    "msi_q4_inject_stall": (ctypes.c_int, [ctypes.c_int]),
     "msi_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "msi_last_cuda_error": (ctypes.c_char_p, []),
 }
