@@ -63,10 +63,11 @@ constexpr float kRoundMagic = 12582912.0f;  // 1.5 2^23: a sum with it is rounde
 constexpr uint32_t kRoundBits = 0x4B400000u;
 constexpr float kLeast = -42.9f;  // log2 of the least weight, beside the greatest, that has a code: its share is 1 or more
 
-// How a row's logits become codes: ch + cl = log2(e) / T; y = top ch of the greatest
-// logit.
+// How a row's logits become codes: ch + cl = log2(e) / (before after T); y = top ch of
+// the greatest logit, top: times `before`.
 struct RowScale {
   float top, ch, cl, y;
+  float before, after;  // powers of two, 1 but for the least and greatest temperatures
   uint32_t whole;  // (44 - the whole part of y) << 26
 };
 
@@ -95,8 +96,11 @@ __device__ __forceinline__ uint2 power_entry(int j) {
 }
 
 // The code of logit x.  0: a weight under 2^kLeast of the greatest, or none.
-// Codes ascend with x.  NEAR (top ch is 4,096 at most): x ch is split as it stands;
-// else x - top first, as the sum of two numbers (any temperature, any logits).
+// Codes ascend with x.  NEAR (top ch is 4,096 at most, T within 2^-96 .. 2^96): x ch is
+// split as it stands; else x - top first, as the sum of two numbers (any logits).  At
+// temperatures beyond, log2(e) / T is no normal fp32 number, or leaves no room for cl:
+// the least ones are scaled up after that difference, which is exact at any size, the
+// greatest ones down before it, where it could overflow.
 template <bool NEAR>
 __device__ __forceinline__ uint32_t weight_code(float x, const RowScale& s, const uint2* tab) {
   if (NEAR) {
@@ -104,8 +108,11 @@ __device__ __forceinline__ uint32_t weight_code(float x, const RowScale& s, cons
     const float e = fmaf(x, s.cl, fmaf(x, s.ch, -y));
     return y > s.y + kLeast ? power_code(y, e, s.whole, tab) : 0u;
   }
-  const float d = __fadd_rn(x, -s.top), b = __fadd_rn(d, -x);
-  const float t = __fadd_rn(__fadd_rn(x, -__fadd_rn(d, -b)), -__fadd_rn(s.top, b));
+  x *= s.before;
+  float d = __fadd_rn(x, -s.top);
+  const float b = __fadd_rn(d, -x);
+  const float t = __fadd_rn(__fadd_rn(x, -__fadd_rn(d, -b)), -__fadd_rn(s.top, b)) * s.after;
+  d *= s.after;
   const float a = __fmul_rn(d, s.ch);
   const float e = fmaf(t, s.ch, fmaf(d, s.cl, fmaf(d, s.ch, -a)));
   return a > kLeast ? power_code(a, e, 44u << 26, tab) : 0u;  // no number (an infinity times 0): 0
@@ -192,7 +199,7 @@ struct SampleShared {
   int listed[2][8], mine, few;
   u64 key[kFew], share[kFew];       // own: a few codes with their places, and their weights
   u64 warp[kSampleWarps];
-  float scale[2];
+  float scale[4];
   int found, ties, tied[8];
   uint32_t lowest, highest;         // code that was picked
   uint2 pow[32];
@@ -737,9 +744,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const __grid_
   int top_k = a.top_k == nullptr ? a.top_k0 : a.top_k[row];
   if (temperature == 0.0f) top_k = 1;
   if (tid == kSampleThreads - 1) {  // double precision is slow: by one thread, beside the others' loads
-    const double c = 1.4426950408889634 / fmax((double)temperature, 1e-30);
+    const float before = temperature > 0x1p96f ? 0x1p-64f : 1.0f, after = temperature < 0x1p-96f ? 0x1p64f : 1.0f;
+    const double c = 1.4426950408889634 / (double)(temperature * before * after);  // exact; T = 0: not used
     sh.scale[0] = (float)c;
     sh.scale[1] = (float)(c - (double)sh.scale[0]);
+    sh.scale[2] = before;
+    sh.scale[3] = after;
   }
   if (top_k >= a.vocab || top_k < 0) top_k = 0;
   if (a.vocab == 1) top_k = 1;
@@ -830,13 +840,15 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const __grid_
     }
   } else {
     RowScale s;
-    s.top = top;
+    s.before = sh.scale[2];
+    s.after = sh.scale[3];
+    s.top = top * s.before;
     s.ch = sh.scale[0];
     s.cl = sh.scale[1];
     s.y = __fmul_rn(top, s.ch);
     s.whole = (44u << 26) - ((__float_as_uint(fmaf(s.y, 32.0f, kRoundMagic)) - kRoundBits) * (1u << 21) & 0xfc000000u);
     const bool mass = top_k == 0 && top_p < 1.0f, plain = top_k == 0 && !mass, bounded = bound > -INFINITY;
-    const bool near = fabsf(s.y) <= 4096.0f;
+    const bool near = fabsf(s.y) <= 4096.0f && temperature >= 0x1p-96f && temperature <= 0x1p96f;
     const auto each_code = [&](auto is_near, auto is_bounded, auto take) {
       constexpr bool NEAR = decltype(is_near)::value, BOUNDED = decltype(is_bounded)::value;
 #pragma unroll 2
