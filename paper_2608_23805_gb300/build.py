@@ -44,7 +44,7 @@ def _stale(obj: str, src: str) -> bool:
         return True
     deps = [src, os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "permute.cuh"),
             os.path.join(CSRC, "kv.cuh"), os.path.join(CSRC, "rotary.cuh"),
-            os.path.join(CSRC, "source.h"),
+            os.path.join(CSRC, "source.h"), os.path.join(CSRC, "per_device.h"),
             os.path.join(ROOT, "include", "msi.h")]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps)
 

@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "kernels.cuh"
+#include "per_device.h"
 
 namespace msi {
 namespace {
@@ -979,17 +980,18 @@ cudaError_t sample_any(const SampleArgs& a, cudaStream_t s) {
   // so the next wave begins before one ends: a third whole waves, two thirds parts
   // of them.  250 rows of 32,000 by 1, 2, 3, 4, 8 CTAs: 81, 64, 79, 81, 129 us; one
   // row by 2, 4, 8: 14.1, 12.1, 11.3.
-  static std::atomic<int> at_once[2][9];  // clusters of so many CTAs, one or two an SM, that run together; 0: not asked yet
+  static PerDevice<2 * 9> at_once;  // clusters of so many CTAs, one or two an SM, that run together
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
   const auto ask = [&](int two, int ctas, int* clusters) {
-    *clusters = at_once[two][ctas].load(std::memory_order_relaxed);
-    if (*clusters != 0) return cudaSuccess;
-    const cudaError_t e = sample_at_once<T>(ctas, two ? kSampleTwoGroups : kSampleMaxGroups, clusters);
-    if (*clusters < 1) *clusters = 1;
-    if (e == cudaSuccess) at_once[two][ctas].store(*clusters, std::memory_order_relaxed);
-    return e;
+    return at_once.get(dev, two * 9 + ctas, clusters, [&](int* n) {
+      const cudaError_t e = sample_at_once<T>(ctas, two ? kSampleTwoGroups : kSampleMaxGroups, n);
+      if (*n < 1) *n = 1;
+      return e;
+    });
   };
-  int sms = 0;
-  cudaError_t e = ask(0, 1, &sms);
+  e = ask(0, 1, &sms);
   if (e != cudaSuccess) return e;
   const int most = a.vocab + (even ? 0 : kVec - 1);  // with what a row's first vector skips
   const int unit = 32 * kVec;                        // of a warp
