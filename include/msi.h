@@ -731,7 +731,8 @@ msi_status msi_q4_pack(const void* codes, const void* scales, int n_out, int n_i
 typedef struct {
   const void* packed;
   int n_out, n_in, group;
-  int rows;             /* <= 2^20 (else MSI_ERR_UNSUPPORTED); made for up to 16, right for any number */
+  int rows;             /* <= 2^20 (else MSI_ERR_UNSUPPORTED); made for up to 16: more than 32 go through in
+                           groups of 32 that read the weights again (80 to 215 TFLOP/s) */
   int out_type;         /* MSI_BF16 or MSI_F32 */
   const void* x;        /* bf16 [rows, n_in], 16-byte aligned */
   int64_t x_stride;     /* elements between rows, a multiple of 8 */
@@ -743,7 +744,7 @@ typedef struct {
 
 /* out = x W^T (+ add).  Products are exact, sums fp32 (a group's first, without
  * its scale: |x| up to 2^117 cannot overflow there; then times the scale), one rounding to the output's type; the order of a sum
- * depends on the shape alone.  A wait for a copy within the kernel that runs out
+ * depends on the shape (the number of rows too) and the device's number of SMs alone.  A wait for a copy within the kernel that runs out
  * (about 2 s) makes the outputs concerned NaN. */
 msi_status msi_q4_linear(const msi_q4_linear_args* args, msi_stream stream);
 
@@ -787,8 +788,9 @@ typedef struct {
   int64_t out_stride;        /* >= n_heads * head_dim */
 } msi_rotary_args;
 
-/* Angles are exact to 2^-24 of a half turn at any position, cos, sin and products
- * fp32, one rounding to bf16.  Rows of any alignment (interleaved: x, out and
+/* The whole and quarter turns of an angle are exact at any position, what is left of
+ * it (an eighth of a turn at most) is off by 3 2^-24 of itself and 2^-32 of a turn; cos,
+ * sin and products fp32, one rounding to bf16.  Rows of any alignment (interleaved: x, out and
  * strides a multiple of 2 elements, head_dim even); those at multiples of 16 bytes
  * with dims a multiple of 16 (interleaved: 8) move in wide vectors. */
 msi_status msi_rotary_apply(const msi_rotary* rotary, const msi_rotary_args* args, msi_stream stream);

@@ -5,17 +5,25 @@
 // instruction multiplies them exactly; a group's G products are added in fp32,
 // the sum is multiplied by the group's scale (fp16, exact in fp32) and added to
 // the row's total, also fp32.  Nothing is rounded to fewer bits before the
-// output.  The order of the sums is fixed by the shape.
+// output.  The order of the sums is fixed by the shape, the number of rows among it,
+// and by the number of SMs (how many warps share a tile's columns).
 //
-// Floor: the codes and scales, read once (n_out n_in (1/2 + 2/G) bytes).  Bound:
-// what an SM can issue.  For each 2,048 weights 56 shifts and logic operations and
-// 32 bf16 pairs to make operands of them, at 2 cycles each on two pipes of their
-// own, and 8 matrix instructions for 8 rows, at 8 cycles: 112 cycles at best where
-// memory would need 90.  4 rows, 2,048 to 100,003: 25 us, 4.3 TB/s; 16 rows, 8,192
-// to 32,768: 43.3 us, 3.3 TB/s; small matrices 3.3 us, a launch and two dependent
-// loads.  (mma.sync rather than tcgen05: the operands are made in registers and
-// the rows are few; as bf16 in shared memory the weights would go through it at four
-// times their size.)
+// Floor: the codes and scales, read once (n_out n_in (1/2 + 2/G) bytes), for 2,048
+// weights (a step) 181 to 198 cycles of a quarter of an SM's share of memory (6,790
+// GB/s, 1.92 GHz).  Beside it, up to 8 rows, 175 instructions, of them 92 on the integer
+// pipe at 2 cycles: 56 shifts and logic operations that make operands of the codes, the
+// rest addresses.  Neither is busy throughout: 4 rows, 2,048 to 100,003 take 25 us, 4.3
+// TB/s, 290 cycles a step, the integer pipe busy for 58 % of them; the rest is waiting.
+// 16 rows, 8,192 to 32,768: 43.3 us, 3.3 TB/s, 386 cycles a step, no pipe busy for more
+// than half; what they wait for the counters do not show.  Small matrices 3.3 us, a
+// launch and two dependent loads.  (mma.sync rather than tcgen05: the operands are made
+// in registers and the rows are few; as bf16 in shared memory the weights would go
+// through it at four times their size.)
+//
+// More than 32 rows go through in groups of 32, each of which reads and unpacks all
+// weights again, and mma.sync is no more than 0.3 of the tensor cores' rate: 4,096 to
+// 2,048 with 64, 512, 4,096 rows 13, 80, 593 us (80, 108, 116 TFLOP/s), 8,192 to 32,768
+// with 512 1.32 ms (208 TFLOP/s).
 #include "kernels.cuh"
 
 #include <cuda_fp16.h>
@@ -60,7 +68,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-// Codes of columns 2 i, 2 i + 1 less 8, as bf16: under the high byte 0x43 a code is 128 + q.
+// Codes of columns 2 i, 2 i + 1 less 8, as bf16, the well-known way: a code as the last
+// bits of a number whose unit they are (under the high byte 0x43 it is 128 + q), less
+// what was added.
 __device__ __forceinline__ uint32_t q4_pair(uint32_t w, int i) {
   uint32_t v, r;
   asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));  // (a & b) | c
@@ -435,7 +445,13 @@ cudaError_t q4_launch_wide(const Q4Args& a, int sms, cudaStream_t s) {
 template <int NT, int STAGES>
 cudaError_t q4_as(const Q4Args& a, int group, int sms, cudaStream_t s) {
   // Up to 8 rows the loads of x are few, and the tiles by themselves are faster (one
-  // row, 8,192 to 32,768: 33 us, with shared rows 35).
+  // row, 8,192 to 32,768: 33 us, with shared rows 35).  From 9 on, by themselves / with
+  // shared rows, weights from memory, us:
+  //             2,048 columns to 600, 912, 2,048 tiles    8,192 columns
+  //   9 rows    8.0/7.4   11.6/9.2   18.9/15.4            18.1/21.1  25.2/24.3  49.7/40.5
+  //   17        15.8/11.4 22.7/12.7  34.5/23.6            32.5/38.5  46.6/41.3  87.0/67.2
+  //   512       236/125   356/216    547/361              465/419    736/754    1344/1154
+  // and with 300 tiles 4.8/6.6 (9 rows, 2,048 columns), 10.4/18.7 (8,192).
   if constexpr (NT > 1) {
     if (a.tiles >= sms * 6) {
       if (group == 32) return q4_launch_wide<NT, 4>(a, sms, s);
@@ -443,8 +459,11 @@ cudaError_t q4_as(const Q4Args& a, int group, int sms, cudaStream_t s) {
       return q4_launch_wide<NT, 1>(a, sms, s);
     }
   }
-  // warps enough to cover the latency of a step's chain: 16,384 to 1,000 by 2, 4, 8
-  // warps a tile 19, 13, 8.6 us
+  // Warps enough to cover the latency of a step's chain: 16,384 to 1,000 by 2, 4, 8
+  // warps a tile 19, 13, 8.6 us.  The limit at 12, 24, 48, 96 warps an SM (one row): 2,048
+  // to 14,400 6.3, 8.0, 8.0, 8.0; to 40,000 13.6, 13.2, 14.0, 18.1; to 100,003 24.8, 24.9,
+  // 25.3, 28.8; 8,192 to 32,768 41.3, 38.9, 33.0, 35.0 (8 rows 52, 49, 38.5, 37.9).  Groups
+  // of rows beyond the first do not count.
   int warps = 1;
   while (warps < kQ4Warps && warps < a.turns && (long long)a.tiles * warps < (long long)sms * 48) warps *= 2;
   const dim3 grid(a.tiles, (a.rows + NT * 8 - 1) / (NT * 8));
