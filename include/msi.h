@@ -712,7 +712,8 @@ uint64_t msi_kv_kernel_launches(const msi_kv* kv);
  * What a decode step needs beside the MoE layer and the attention (a library
  * convenience: the paper leaves the rest of the model to the native runtime):
  * products with weights in 4 bits, rotation by position, the choice of a token.
- * These calls hold no state; they run on the current device, whose memory all
+ * These calls hold no state (the products' wait limit apart, which is the
+ * process's); they run on the current device, whose memory all
  * pointers are in, asynchronously on `stream`, and can be captured in a graph.
  * ------------------------------------------------------------------------- */
 enum { MSI_BF16 = 0, MSI_F32 = 1 };
